@@ -76,7 +76,8 @@ typedef enum {
     MF_ESCRATCH = 7       /* mf_search_noalloc: the search needs more than MF_NOALLOC_SCRATCH_BYTES */
 } mf_status;
 
-typedef enum { MF_F32 = 0, MF_BF16 = 1 } mf_dtype;
+/* MF_F16 (binary16) is a type of the served steps' operators only. */
+typedef enum { MF_F32 = 0, MF_BF16 = 1, MF_F16 = 2 } mf_dtype;
 
 typedef enum { MF_ACT_IDENTITY = 0, MF_ACT_SIGMOID = 1 } mf_activation;
 
@@ -385,6 +386,151 @@ mf_status mf_ga_workspace_size(const mf_problem *p, const mf_ga_args *args, size
  * VRAM cap.  Blocking (one synchronisation, at the end). */
 mf_status mf_ga_run(mf_problem *p, const mf_ga_args *args, void *d_ws, size_t ws_bytes,
                     void *stream, uint64_t *h_best_idx, double *h_best_J, uint64_t *d_final_pop);
+
+/* ------------------------------------------------------------ served steps
+ *
+ * The operators of the step that an option stands for.  The options of the
+ * paper's LLMs are {16-bit, 4-bit} variants x concurrency; a decode step of a
+ * 4-bit variant is products with 4-bit weights, the append of the new keys and
+ * values (rotated by their positions) to a cache held in 4 bits, and attention
+ * over that cache.  They run (and profile) what the searches above decide on.
+ *
+ * Conventions as above; all of these calls only enqueue work on `stream`, take
+ * caller-owned device memory and allocate nothing, so they may be captured into
+ * a HIP graph.  Arguments are checked on the host; what only the device can
+ * see (lengths, page numbers) is bounded by the kernels: see mf_kv4_batch.
+ * Activations, keys, values and results are MF_BF16 or MF_F16, with 32-bit
+ * accumulation; strides are in elements and may be any that fit the shape, the
+ * innermost dimension is contiguous, and pointers need the alignment of their
+ * elements only, where no other is named. */
+
+/* --- products with 4-bit weights
+ *
+ * y[m][n] = sum_k x[m][k] s[n][k / G] (c[n][k] - z[n][k / G]) + bias[n],
+ * c and z in 0..15, summed in fp32 and rounded once. */
+typedef struct {
+    int64_t n_out, n_in;    /* 1 <= N <= 2^31 - 16, 1 <= K <= 2^24, K a multiple of G */
+    int32_t group;          /* G: weights that share a scale, 32, 64 or 128 */
+    mf_dtype dtype;         /* MF_BF16 or MF_F16: of the scales, x, bias and y */
+} mf_w4_desc;
+
+/* Bytes of the packed weights. */
+mf_status mf_w4_pack_bytes(const mf_w4_desc *desc, size_t *bytes);
+
+/* Lays weights out for mf_w4_matmul, once, when they are loaded.  d_codes:
+ * uint8 [N][K / 2], the even k in the low four bits; d_scales [N][K / G];
+ * d_zeros uint8 [N][K / G], low four bits read, or NULL: 8 everywhere.
+ * d_packed: mf_w4_pack_bytes, 256-byte aligned. */
+mf_status mf_w4_pack(const mf_w4_desc *desc, const uint8_t *d_codes, const void *d_scales, const uint8_t *d_zeros,
+                     void *d_packed, size_t packed_bytes, void *stream);
+
+typedef struct {
+    mf_w4_desc w;
+    const void *d_packed;   /* as mf_w4_pack wrote it */
+    const void *d_x;        /* [rows][K], row stride x_stride >= K */
+    const void *d_bias;     /* [N] or NULL */
+    void *d_y;              /* [rows][N], row stride y_stride >= N */
+    int64_t rows;           /* 0 (nothing is done) .. 2^24 */
+    int64_t x_stride, y_stride;
+} mf_w4_args;
+
+/* Any number of rows; made for the few (up to 64) of a decode step, which read
+ * the weights once.  Deterministic. */
+mf_status mf_w4_matmul(const mf_w4_args *args, void *stream);
+
+/* --- the paged cache in 4 bits
+ *
+ * A cache is n_pages pages of page_size tokens, for n_kv_heads heads of
+ * head_dim values, keys and values alike.  G neighbouring values of a row share
+ * a binary16 scale and offset and are held as codes 0..15:
+ *   x limited to +-65504 (binary16's largest; a NaN makes its whole group NaN),
+ *   lo = min x, hi = max x, scale = f16((hi - lo) * (float)(1 / 15.)), off = f16(lo),
+ *   code = rint((x - off) * (1 / scale)) limited to 0..15 (0 when scale is 0),
+ *   in fp32, each step rounded; the value held is off + scale * code.
+ * Per token and head: D bytes of codes and 8 D / G of scales and offsets. */
+typedef struct {
+    int32_t n_pages;        /* >= 1 */
+    int32_t page_size;      /* tokens, a multiple of 16, 16..1024 */
+    int32_t n_kv_heads;     /* 1..1024 */
+    int32_t head_dim;       /* D: 64, 128 or 256 */
+    int32_t group;          /* G: 32, 64 or 128, at most D */
+    void *d_pages;          /* mf_kv4_cache_bytes, 256-byte aligned; need not be initialised */
+} mf_kv4_cache;
+
+/* Bytes of d_pages. */
+mf_status mf_kv4_cache_bytes(const mf_kv4_cache *cache, size_t *bytes);
+
+/* The sequences of one step, shared by its append, its attention and its
+ * reads.  Sequence s has rows q_start[s] .. q_start[s + 1) of the step's row
+ * tensors: its newest n_s tokens, at positions kv_len[s] - n_s .. kv_len[s] - 1
+ * (kv_len counts them).  Token j of s is in page page_table[s][j / page_size].
+ * A page that is written must belong to one sequence.
+ * The kernels read and write nothing outside the buffers whatever the device
+ * arrays hold: rows past `rows`, tokens at negative positions or at positions
+ * from max_kv on, and tokens whose page number is not in 0..n_pages are left
+ * out (not written; read as zeros; invisible to attention). */
+typedef struct {
+    int32_t n_seq;          /* 0 .. 2^20 */
+    int32_t max_new;        /* the largest n_s, >= 0: sizes the launch */
+    int32_t max_kv;         /* the largest kv_len, <= table_cols * page_size and 2^30: sizes the launch */
+    int64_t rows;           /* rows of the step's tensors, q_start[n_seq] <= rows <= 2^30 */
+    const int32_t *d_q_start;     /* [n_seq + 1], ascending from 0 */
+    const int32_t *d_kv_len;      /* [n_seq] */
+    const int32_t *d_page_table;  /* [n_seq][table_cols], row stride table_stride */
+    int64_t table_stride;
+    int32_t table_cols;
+} mf_kv4_batch;
+
+/* Writes the rows of k and v into the cache.  With d_cos / d_sin every key is
+ * first turned by its position p (in fp32, each step rounded): for pair t of
+ * rot_dim / 2, (a, b) -> (a cos[p][t] - b sin[p][t], b cos[p][t] + a sin[p][t]),
+ * the pair being dims (t, t + rot_dim / 2), or (2t, 2t + 1) when interleaved;
+ * dims from rot_dim on stay.  With d_q the queries are turned the same way into
+ * d_q_out (rounded once; may be d_q itself with the same strides). */
+typedef struct {
+    mf_dtype dtype;         /* MF_BF16 or MF_F16 */
+    const void *d_k, *d_v;  /* [rows][n_kv_heads][D] */
+    int64_t k_stride, k_head_stride, v_stride, v_head_stride;
+    const float *d_cos, *d_sin;  /* [n_pos][rot_dim / 2], or both NULL: no rotation */
+    int32_t n_pos;          /* >= max_kv */
+    int32_t rot_dim;        /* a multiple of 16, 16..D */
+    int32_t interleaved;
+    int32_t n_heads;        /* query heads, any; 0 without d_q */
+    const void *d_q;        /* [rows][n_heads][D] or NULL; needs d_cos */
+    void *d_q_out;
+    int64_t q_stride, q_head_stride, qo_stride, qo_head_stride;
+} mf_kv4_append_args;
+mf_status mf_kv4_append(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_append_args *args,
+                        void *stream);
+
+/* The values that the cache holds for the rows of a batch (n_s = kv_len[s]:
+ * whole sequences), rounded to dtype (MF_F32, MF_BF16 or MF_F16): d_k and d_v
+ * [rows][n_kv_heads][D], contiguous; either may be NULL. */
+mf_status mf_kv4_read(const mf_kv4_cache *cache, const mf_kv4_batch *batch, mf_dtype dtype, void *d_k, void *d_v,
+                      void *stream);
+
+/* Attention of the rows of q over their sequence's cached tokens.  Query head h
+ * reads key head h / (n_heads / n_kv_heads).  Row i of a sequence sees the
+ * tokens j <= p_i = kv_len - n_s + i, with window > 0 only those > p_i - window;
+ * out = sum_j softmax(scale q.k_j) v_j, lse = log sum_j exp(scale q.k_j).  A row
+ * that sees no token gives 0 and -inf.  Sums and softmax in fp32; the weights of
+ * the values are rounded to bfloat16.  Deterministic. */
+typedef struct {
+    mf_dtype dtype;         /* MF_BF16 or MF_F16: of q and out */
+    int32_t n_heads;        /* a multiple of n_kv_heads, at most 4096 */
+    const void *d_q;        /* [rows][n_heads][D] */
+    void *d_out;            /* [rows][n_heads][D] */
+    float *d_lse;           /* [rows][n_heads] contiguous, or NULL */
+    int64_t q_stride, q_head_stride, out_stride, out_head_stride;
+    float scale;            /* finite, > 0 */
+    int32_t window;         /* 0: every earlier token */
+} mf_kv4_attn_args;
+
+/* Bytes of workspace (possibly 0), a function of the sizes, not of pointers. */
+mf_status mf_kv4_workspace_size(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args,
+                                size_t *bytes);
+mf_status mf_kv4_attention(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args,
+                           void *d_ws, size_t ws_bytes, void *stream);
 
 /* Human-readable status name. */
 const char *mf_status_string(mf_status s);

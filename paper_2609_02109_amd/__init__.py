@@ -1,12 +1,13 @@
 """MI355X-native MeanField joint-configuration search.
 
 `synth` draws seeded instances; `mf` is the binding to the HIP library
-(libmf.so), imported on first use so that instance generation works on hosts
-without the built library.
+(libmf.so), `serve` the operators of the served models' 4-bit variants in the
+same library; both are imported on first use so that instance generation works
+on hosts without the built library.
 """
 import importlib
 
-__all__ = ["synth", "mf"]
+__all__ = ["synth", "mf", "serve"]
 
 
 def __getattr__(name):

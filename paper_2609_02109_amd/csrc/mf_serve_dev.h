@@ -1,0 +1,108 @@
+// Device helpers of the served steps' operators: 16-bit types, codes to matrix
+// operands, loads that need no more than their elements' alignment.
+#pragma once
+
+#include <string.h>
+
+#include "mf_serve.h"
+
+namespace mfs {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+template <typename To, typename From>
+__device__ __forceinline__ To bits(const From &v)
+{
+    static_assert(sizeof(To) == sizeof(From), "same size");
+    To r;
+    __builtin_memcpy(&r, &v, sizeof r);
+    return r;
+}
+
+// 16 bytes from an address aligned to 2.
+__device__ __forceinline__ u32x4 load16(const void *p)
+{
+    u32x4 v;
+    __builtin_memcpy(&v, __builtin_assume_aligned(p, 2), 16);
+    return v;
+}
+
+template <bool F16>
+__device__ __forceinline__ float to_float(uint16_t h)
+{
+    if (F16) return (float)bits<_Float16>(h);
+    return __uint_as_float((uint32_t)h << 16);
+}
+template <bool F16>
+__device__ __forceinline__ uint16_t from_float(float x)
+{
+    if (F16) return bits<uint16_t>((_Float16)x);
+    return bits<uint16_t>((__bf16)x);
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    if (F16) {
+        const f16x2 v = {(_Float16)a, (_Float16)b};
+        return bits<uint32_t>(v);
+    }
+    const bf16x2 v = __builtin_convertvector((f32x2){a, b}, bf16x2);
+    return bits<uint32_t>(v);
+}
+
+// Codes 2 s, 2 s + 1 of a dword as two values 16 + c of the 16-bit type.
+template <bool F16, int S>
+__device__ __forceinline__ uint32_t codes2(uint32_t w)
+{
+    if (F16) return ((S < 2 ? w << (6 - 4 * S) : w >> (4 * S - 6)) & 0x03c003c0u) | 0x4c004c00u;
+    return ((S < 1 ? w << 3 : w >> (4 * S - 3)) & 0x00780078u) | 0x41804180u;
+}
+template <bool F16>
+__device__ __forceinline__ u32x4 codes8(uint32_t w)
+{
+    return (u32x4){codes2<F16, 0>(w), codes2<F16, 1>(w), codes2<F16, 2>(w), codes2<F16, 3>(w)};
+}
+
+// D += A B, 16 x 16 x 32: lane l holds A[l % 16][8 (l / 16) ..+8], B[8 (l / 16) ..+8][l % 16], D[4 (l / 16) + r][l % 16].
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
+{
+    if (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(bits<f16x8>(a), bits<f16x8>(b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(bits<bf16x8>(a), bits<bf16x8>(b), c, 0, 0, 0);
+}
+// A matrix of ones as an A operand.
+template <bool F16>
+__device__ __forceinline__ u32x4 ones8()
+{
+    const uint32_t o = F16 ? 0x3c003c00u : 0x3f803f80u;
+    return (u32x4){o, o, o, o};
+}
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (the contraction index of an operand).
+__device__ __forceinline__ float quarters_max(float x)
+{
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float quarters_min(float x) { return -quarters_max(-x); }
+__device__ __forceinline__ float quarters_sum(float x)
+{
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+}  // namespace mfs

@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(HERE, "libmf.so")
 
 MF_OK, MF_EINVAL, MF_ENOMEM, MF_EDEVICE, MF_EUNSUPPORTED, MF_EOVERFLOW, MF_EINTERNAL, MF_ESCRATCH = range(8)
 NOALLOC_SCRATCH_BYTES = 128 << 20
-MF_F32, MF_BF16 = 0, 1
+MF_F32, MF_BF16, MF_F16 = 0, 1, 2
 MF_ACT_IDENTITY, MF_ACT_SIGMOID = 0, 1
 MF_DUMP = 1
 MF_FIXED_STATE = 2
@@ -32,7 +32,9 @@ MAX_MODELS = 16
 EXPORTS = ["mf_problem_bytes", "mf_problem_create", "mf_problem_destroy", "mf_space_size", "mf_decode",
            "mf_workspace_size", "mf_search", "mf_search_noalloc", "mf_eval_fast", "mf_eval_canonical",
            "mf_static_workspace_size", "mf_search_static", "mf_eval_static",
-           "mf_ga_workspace_size", "mf_ga_run", "mf_status_string"]
+           "mf_ga_workspace_size", "mf_ga_run",
+           "mf_w4_pack_bytes", "mf_w4_pack", "mf_w4_matmul", "mf_kv4_cache_bytes", "mf_kv4_append", "mf_kv4_read",
+           "mf_kv4_workspace_size", "mf_kv4_attention", "mf_status_string"]
 
 
 class MfError(RuntimeError):
@@ -132,6 +134,14 @@ def _load():
         "mf_eval_static": (S, [P, P, P, C.c_int64, P, P, P, P, C.c_size_t, P]),
         "mf_ga_workspace_size": (S, [P, P, P]),
         "mf_ga_run": (S, [P, P, P, C.c_size_t, P, P, P, P]),
+        "mf_w4_pack_bytes": (S, [P, P]),
+        "mf_w4_pack": (S, [P, P, P, P, P, C.c_size_t, P]),
+        "mf_w4_matmul": (S, [P, P]),
+        "mf_kv4_cache_bytes": (S, [P, P]),
+        "mf_kv4_append": (S, [P, P, P, P]),
+        "mf_kv4_read": (S, [P, P, S, P, P, P]),
+        "mf_kv4_workspace_size": (S, [P, P, P, P]),
+        "mf_kv4_attention": (S, [P, P, P, P, C.c_size_t, P]),
         "mf_status_string": (C.c_char_p, [S]),
     }
     for name, (res, args) in sig.items():

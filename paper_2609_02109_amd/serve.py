@@ -1,0 +1,256 @@
+"""The operators of a served model's 4-bit variant, over the C ABI.
+
+The options that a search chooses from are variants (16-bit or 4-bit) and
+runtime parameters of the co-running models.  These are the operators of the
+step that a 4-bit option stands for, to run it or to profile it into an option
+table: products with 4-bit weights (`W4Weight`), and a paged key/value cache
+held in 4 bits (`KV4Cache`) with its append, which turns keys and queries by
+their positions on the way, and its attention.
+
+As in `mf`, this is marshalling only: torch supplies device memory and the
+stream, the kernels of libmf.so do the work.  Calls enqueue on `stream` (None:
+torch's current one) and do not synchronise; include/mf.h has the definitions.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+import threading
+
+import torch
+
+from . import mf
+from .mf import _check, _keep_for, _ptr, _stream
+
+_DTYPES = {torch.float32: mf.MF_F32, torch.bfloat16: mf.MF_BF16, torch.float16: mf.MF_F16}
+_HALF = (torch.bfloat16, torch.float16)
+_p, _i32, _i64 = C.c_void_p, C.c_int32, C.c_int64
+
+
+class W4Desc(C.Structure):
+    _fields_ = [("n_out", _i64), ("n_in", _i64), ("group", _i32), ("dtype", _i32)]
+
+
+class W4Args(C.Structure):
+    _fields_ = [("w", W4Desc), ("d_packed", _p), ("d_x", _p), ("d_bias", _p), ("d_y", _p), ("rows", _i64),
+                ("x_stride", _i64), ("y_stride", _i64)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("n_pages", _i32), ("page_size", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("group", _i32),
+                ("d_pages", _p)]
+
+
+class Batch(C.Structure):
+    _fields_ = [("n_seq", _i32), ("max_new", _i32), ("max_kv", _i32), ("rows", _i64), ("d_q_start", _p), ("d_kv_len", _p),
+                ("d_page_table", _p), ("table_stride", _i64), ("table_cols", _i32)]
+
+
+class AppendArgs(C.Structure):
+    _fields_ = [("dtype", _i32), ("d_k", _p), ("d_v", _p), ("k_stride", _i64), ("k_head_stride", _i64), ("v_stride", _i64),
+                ("v_head_stride", _i64), ("d_cos", _p), ("d_sin", _p), ("n_pos", _i32), ("rot_dim", _i32),
+                ("interleaved", _i32), ("n_heads", _i32), ("d_q", _p), ("d_q_out", _p), ("q_stride", _i64),
+                ("q_head_stride", _i64), ("qo_stride", _i64), ("qo_head_stride", _i64)]
+
+
+class AttnArgs(C.Structure):
+    _fields_ = [("dtype", _i32), ("n_heads", _i32), ("d_q", _p), ("d_out", _p), ("d_lse", _p), ("q_stride", _i64),
+                ("q_head_stride", _i64), ("out_stride", _i64), ("out_head_stride", _i64), ("scale", C.c_float), ("window", _i32)]
+
+
+def _require(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(t, name, shape, dtype, device):
+    """A tensor of `shape` whose last dimension is contiguous (a copy where it is not)."""
+    _require(isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device,
+             f"{name}: {tuple(shape)} {dtype} on {device} is wanted")
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+def _into(t, name, shape, dtype, device):
+    """An output: a new tensor, or the caller's."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _require(isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device
+             and (t.stride(-1) == 1 or t.shape[-1] <= 1), f"{name}: {tuple(shape)} {dtype} on {device} with a contiguous last dimension is wanted")
+    return t
+
+
+class W4Weight:
+    """Packed 4-bit weights [N, K] with a scale (and a zero point) for every
+    `K // scales.shape[1]` weights of a row: w = scale * (code - zero).
+
+    codes: uint8 [N, K // 2], the even column in the low four bits; scales:
+    bfloat16 or float16 [N, K // G], G 32, 64 or 128; zeros: uint8 [N, K // G],
+    0..15, or None (8).  Laid out once, here; the arguments may be freed after."""
+
+    def __init__(self, codes, scales, zeros=None, stream=None):
+        _require(isinstance(codes, torch.Tensor) and codes.dtype is torch.uint8 and codes.dim() == 2 and codes.is_cuda,
+                 "codes: a uint8 [N, K // 2] tensor on the GPU is wanted")
+        _require(isinstance(scales, torch.Tensor) and scales.dtype in _HALF and scales.dim() == 2
+                 and scales.shape[0] == codes.shape[0] and scales.device == codes.device and scales.shape[1] > 0
+                 and (2 * codes.shape[1]) % scales.shape[1] == 0,
+                 "scales: bfloat16 or float16 [N, K // G] beside the codes is wanted")
+        _require(zeros is None or (isinstance(zeros, torch.Tensor) and zeros.dtype is torch.uint8
+                                   and zeros.shape == scales.shape and zeros.device == codes.device),
+                 "zeros: uint8 of the scales' shape is wanted")
+        self.n_out, self.n_in = int(codes.shape[0]), 2 * int(codes.shape[1])
+        self.group, self.dtype, self.device = self.n_in // int(scales.shape[1]), scales.dtype, codes.device
+        self.desc = W4Desc(self.n_out, self.n_in, self.group, _DTYPES[self.dtype])
+        nb = C.c_size_t()
+        _check(mf.lib.mf_w4_pack_bytes(C.byref(self.desc), C.byref(nb)), "mf_w4_pack_bytes")
+        codes, scales = codes.contiguous(), scales.contiguous()
+        zeros = zeros if zeros is None else zeros.contiguous()
+        self.packed = torch.empty(int(nb.value), dtype=torch.uint8, device=self.device)
+        _keep_for(stream, codes, scales, zeros, self.packed)
+        _check(mf.lib.mf_w4_pack(C.byref(self.desc), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(self.packed),
+                                 C.c_size_t(self.packed.numel()), _stream(stream)), "mf_w4_pack")
+
+    def matmul(self, x, bias=None, out=None, stream=None):
+        """x [.., K] @ W.T + bias [N] -> [.., N], in the scales' type."""
+        _require(x.dim() >= 1 and x.shape[-1] == self.n_in and x.dtype is self.dtype and x.device == self.device,
+                 f"x: [.., {self.n_in}] {self.dtype} on {self.device} is wanted")
+        _require(bias is None or (bias.dtype is self.dtype and bias.device == self.device and tuple(bias.shape) == (self.n_out,)
+                                  and bias.is_contiguous()), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
+        lead = x.shape[:-1]
+        if x.dim() != 2:
+            x = x.reshape(-1, self.n_in)
+        if x.stride(1) != 1:
+            x = x.contiguous()
+        if out is None:
+            y = torch.empty((x.shape[0], self.n_out), dtype=self.dtype, device=self.device)
+            out = y if len(lead) == 1 else y.view(*lead, self.n_out)
+        else:
+            _into(out, "out", (*lead, self.n_out), self.dtype, self.device)
+            y = out if out.dim() == 2 else out.view(-1, self.n_out)
+        args = W4Args(self.desc, self.packed.data_ptr(), x.data_ptr(), bias.data_ptr() if bias is not None else None, y.data_ptr(),
+                      x.shape[0], x.stride(0), y.stride(0))
+        _keep_for(stream, x, bias, y, self.packed)
+        _check(mf.lib.mf_w4_matmul(C.byref(args), _stream(stream)), "mf_w4_matmul")
+        return out
+
+
+def rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, device="cuda"):
+    """(cos, sin) [n_pos, rot_dim // 2] float32 for `KV4Cache.append`, computed in 64 bits."""
+    half = rot_dim // 2
+    inv = base ** (-torch.arange(half, dtype=torch.float64, device=device) / half)
+    a = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * inv
+    return a.cos().float(), a.sin().float()
+
+
+class KV4Batch:
+    """The sequences of one step (mf_kv4_batch), shared by its append, reads
+    and attention; made by `KV4Cache.batch`.  The device tensors are read by
+    every call, so a server may update them in place between steps."""
+
+    def __init__(self, q_start, kv_len, page_table, rows, max_new, max_kv):
+        for t, name in ((q_start, "q_start"), (kv_len, "kv_len"), (page_table, "page_table")):
+            _require(isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.is_cuda, f"{name}: int32 on the GPU is wanted")
+        n = int(kv_len.shape[0])
+        _require(kv_len.dim() == 1 and kv_len.is_contiguous(), "kv_len: contiguous [n_seq] is wanted")
+        _require(tuple(q_start.shape) == (n + 1,) and q_start.is_contiguous(), "q_start: contiguous [n_seq + 1] is wanted")
+        _require(page_table.dim() == 2 and page_table.shape[0] == n and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
+                 "page_table: [n_seq, pages] with a contiguous last dimension is wanted")
+        self.tensors = (q_start, kv_len, page_table)
+        self.rows = int(rows)
+        self.raw = Batch(n, int(max_new), int(max_kv), self.rows, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                         page_table.stride(0), int(page_table.shape[1]))
+
+
+class KV4Cache:
+    """A paged key/value cache in 4 bits: n_pages pages of page_size tokens for
+    n_kv_heads heads of head_dim values; `group` neighbouring values share a
+    scale and an offset.  `bytes_per_token` is what a token costs."""
+
+    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, group=64, device="cuda"):
+        self.device = torch.device(device)
+        self.raw = Cache(int(n_pages), int(page_size), int(n_kv_heads), int(head_dim), int(group), None)
+        nb = C.c_size_t()
+        _check(mf.lib.mf_kv4_cache_bytes(C.byref(self.raw), C.byref(nb)), "mf_kv4_cache_bytes")
+        self.pages = torch.empty(int(nb.value), dtype=torch.uint8, device=self.device)
+        self.device = self.pages.device
+        self.raw.d_pages = self.pages.data_ptr()
+        self.n_kv_heads, self.head_dim, self.page_size = int(n_kv_heads), int(head_dim), int(page_size)
+        self.bytes_per_token = int(nb.value) // (int(n_pages) * self.page_size)
+        # one workspace per (thread, stream), as a problem's
+        self._ws = {}
+        self._ws_lock = threading.Lock()
+
+    def batch(self, q_start, kv_len, page_table, rows, max_new, max_kv) -> KV4Batch:
+        """q_start int32 [n_seq + 1], kv_len int32 [n_seq] (tokens of each
+        sequence, the step's new ones included), page_table int32 [n_seq, ..];
+        rows: of the step's tensors; max_new, max_kv: the largest number of new
+        tokens and of tokens of a sequence, known on the host."""
+        b = KV4Batch(q_start, kv_len, page_table, rows, max_new, max_kv)
+        _require(all(t.device == self.device for t in b.tensors), f"the batch's tensors: on {self.device} is wanted")
+        return b
+
+    def append(self, batch: KV4Batch, k, v, cos=None, sin=None, q=None, interleaved=False, q_out=None, stream=None):
+        """Writes k and v [rows, n_kv_heads, head_dim] into the cache, the keys
+        turned by their positions when cos / sin [n_pos, rot_dim // 2] are given;
+        with q [rows, n_heads, head_dim] also returns the queries turned the
+        same way (q_out: where to, e.g. q itself)."""
+        _require(isinstance(k, torch.Tensor) and k.dtype in _HALF, "k: bfloat16 or float16 is wanted")
+        shape, dt, dev = (batch.rows, self.n_kv_heads, self.head_dim), k.dtype, self.device
+        k, v = _rows(k, "k", shape, dt, dev), _rows(v, "v", shape, dt, dev)
+        _require((cos is None) == (sin is None), "cos and sin: both or neither are wanted")
+        a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+        if cos is not None:
+            _require(cos.dim() == 2 and all(t.shape == cos.shape and t.dtype is torch.float32 and t.device == dev and t.is_contiguous()
+                                            for t in (cos, sin)), f"cos, sin: contiguous float32 [n_pos, rot_dim // 2] on {dev} is wanted")
+            a.d_cos, a.d_sin, a.n_pos, a.rot_dim = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1]
+            a.interleaved = int(bool(interleaved))
+        if q is not None:
+            _require(cos is not None, "q: only turned here, so cos and sin are wanted with it")
+            _require(q.dim() == 3, "q: [rows, n_heads, head_dim] is wanted")
+            q = _rows(q, "q", (batch.rows, q.shape[1], self.head_dim), dt, dev)
+            q_out = _into(q_out, "q_out", q.shape, dt, dev)
+            a.n_heads, a.d_q, a.d_q_out = q.shape[1], q.data_ptr(), q_out.data_ptr()
+            a.q_stride, a.q_head_stride, a.qo_stride, a.qo_head_stride = q.stride(0), q.stride(1), q_out.stride(0), q_out.stride(1)
+        _keep_for(stream, k, v, cos, sin, q, q_out, self.pages, *batch.tensors)
+        _check(mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream(stream)), "mf_kv4_append")
+        return q_out
+
+    def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
+        """(keys, values) [rows, n_kv_heads, head_dim] that the cache holds for the batch's rows."""
+        _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
+        shape = (batch.rows, self.n_kv_heads, self.head_dim)
+        k, v = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
+        _keep_for(stream, k, v, self.pages, *batch.tensors)
+        _check(mf.lib.mf_kv4_read(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(), _stream(stream)),
+               "mf_kv4_read")
+        return k, v
+
+    def _workspace(self, nbytes: int, stream):
+        s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        key = (threading.get_ident(), s.cuda_stream)
+        with self._ws_lock:
+            ws = self._ws.get(key)
+            if ws is None or ws.numel() < nbytes:
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+                _keep_for(stream, ws)
+                self._ws[key] = ws
+        return ws
+
+    def attention(self, batch: KV4Batch, q, scale=None, window=0, lse=False, out=None, stream=None):
+        """Causal attention of q [rows, n_heads, head_dim] over the cached
+        tokens: [rows, n_heads, head_dim], with lse=True also the log of the
+        softmax sums [rows, n_heads] float32.  scale: 1 / sqrt(head_dim) by
+        default; window > 0: only the newest `window` tokens up to each row's."""
+        _require(isinstance(q, torch.Tensor) and q.dtype in _HALF and q.dim() == 3, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
+        q = _rows(q, "q", (batch.rows, q.shape[1], self.head_dim), q.dtype, self.device)
+        out = _into(out, "out", q.shape, q.dtype, self.device)
+        ls = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device) if lse else None
+        a = AttnArgs(_DTYPES[q.dtype], q.shape[1], q.data_ptr(), out.data_ptr(), ls.data_ptr() if lse else None, q.stride(0),
+                     q.stride(1), out.stride(0), out.stride(1), 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
+                     int(window))
+        nb = C.c_size_t()
+        _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
+        ws = self._workspace(nb.value, stream) if nb.value else None
+        _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
+        _check(mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _ptr(ws), nb, _stream(stream)),
+               "mf_kv4_attention")
+        return (out, ls) if lse else out
