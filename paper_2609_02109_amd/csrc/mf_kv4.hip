@@ -105,7 +105,11 @@ __device__ __forceinline__ uint32_t pack_codes(const uint32_t *c)
 }
 
 // Bit of token t % 4 and dim d of a value dword (mf_serve.h).
-__device__ __forceinline__ int value_bit(int t, int d) { return 16 * (t & 1) + 4 * (2 * ((d >> 4) & 1) + ((t >> 1) & 1)); }
+__device__ __forceinline__ int value_bit(int t, int d) { return 16 * (t & 1) + 4 * (2 * ((t >> 1) & 1) + ((d >> 4) & 1)); }
+
+// Where token t's scale of a group of the keys (0) or values (1) is in a record's tables.
+template <int NG>
+__device__ __forceinline__ int scale_at(int t, int kv, int g) { return (t >> 2) * 8 * NG + kv * 4 * NG + g * 4 + (t & 3); }
 
 template <bool F16, int D, int G>
 __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h, int blk, const Span &p, uint8_t *lds)
@@ -118,7 +122,7 @@ __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h
     const long long row = pos + p.shift;
     float v[NS][8];
     uint32_t code[NS][8], meta[NG];
-    uint16_t *table = (uint16_t *)(rec + 16 * D);   // 16 NG each: key scales, key offsets, value scales, value offsets
+    uint16_t *table = (uint16_t *)(rec + 16 * D);   // scales, key offsets, value offsets (mf_serve.h)
     if (live) {
         const uint16_t *k = (const uint16_t *)a.k + row * a.k_stride + h * a.k_head;
         const float *cos = a.cos ? a.cos + (long long)pos * (a.rot >> 1) : nullptr;
@@ -140,8 +144,8 @@ __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h
 #pragma unroll
         for (int g = 0; g < NG; g++)
             if ((g & 3) == qt) {
-                table[g * 16 + tok] = (uint16_t)meta[g];
-                table[16 * NG + tok * NG + g] = (uint16_t)(meta[g] >> 16);
+                table[scale_at<NG>(tok, 0, g)] = (uint16_t)meta[g];
+                table[32 * NG + tok * NG + g] = (uint16_t)(meta[g] >> 16);
             }
         const uint16_t *x = (const uint16_t *)a.v + row * a.v_stride + h * a.v_head;
 #pragma unroll
@@ -152,7 +156,7 @@ __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h
 #pragma unroll
         for (int g = 0; g < NG; g++)
             if ((g & 3) == qt) {
-                table[32 * NG + g * 16 + tok] = (uint16_t)meta[g];
+                table[scale_at<NG>(tok, 1, g)] = (uint16_t)meta[g];
                 table[48 * NG + g * 16 + tok] = (uint16_t)(meta[g] >> 16);
             }
     }
@@ -263,9 +267,10 @@ __global__ __launch_bounds__(64) void read_kernel(KvReadArgs a, int blocks)
 #pragma unroll
                 for (int j = 0; j < 8; j++) v[j] = 0.f;
                 if (rec) {
-                    const uint16_t *table = (const uint16_t *)(rec + 16 * D) + 32 * NG * kv;
+                    const uint16_t *table = (const uint16_t *)(rec + 16 * D);
                     const int g = d / G;
-                    const float sc = to_float<true>(table[g * 16 + in]), off = to_float<true>(table[16 * NG + (kv ? g * 16 + in : in * NG + g)]);
+                    const float sc = to_float<true>(table[scale_at<NG>(in, kv, g)]),
+                                off = to_float<true>(table[kv ? 48 * NG + g * 16 + in : 32 * NG + in * NG + g]);
                     const uint32_t w = kv ? 0u : ((const uint32_t *)(rec + (qt * 16 + in) * (D / 8)))[i];
 #pragma unroll
                     for (int j = 0; j < 8; j++) {

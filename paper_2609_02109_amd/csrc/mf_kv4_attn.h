@@ -2,24 +2,32 @@
 // launches it).  One pass over the tokens with a running maximum and sum.
 //
 // A wave holds RT tiles of 16 rows (row = query token x head of the group that
-// shares a key head).  Per 16 tokens it computes S^T = K Q^T with the key codes
-// as they are, 16 + c, and per group of G dims
-//   s = sum_g scale_g (sum_d (16 + c) q - 16 sum_d q) + off_g sum_d q:
-// -16 sum q is the product's starting value, and the last sum over g is a matrix
+// shares a key head).  The codes are matrix operands as they are: a 16-bit float
+// whose bits are the whole number c is the subnormal c 2^-24 (binary16, up to c =
+// 2047) or c 2^-133 (bfloat16, up to 255), which the matrix instructions take
+// exactly and at full rate.  So one and makes two operands of a dword, the codes
+// at bits 0.. of each half, and one more those at bits 4.., 16 times as large: 5
+// operations for 8 codes where a conversion to 16 + c took 8 and a sum to take the
+// 16 out again.  Per 16 tokens S^T = K Q^T, and per group of G dims
+//   s = sum_g scale_g sum_d c q + off_g sum_d q,
+// the queries taken 2^e times first (their largest at the top of the type's range;
+// 2^-4 of that where they meet the larger codes), and the last sum over g a matrix
 // product itself (sum q in two binary16 pieces, 22 bits).  S^T comes out with the
 // tokens 4 (l / 16) + r of row l % 16 in lane l, which is how the next product
 // O^T = V^T P^T takes its right operand: softmax weights stay in their lane.
-//   o = sum_t w (16 + c) - 16 sum_t w + sum_t p off_g,   w = p scale_g,
-// p and w rounded to binary16 (11 bits; everything else is fp32), the second sum
-// from the same instruction with ones for codes, so that the 16 cancels exactly.
-// Weights are kept relative to 2^base, base = the largest s so far (in powers of
-// two) less 14, more where a step has scales of 2 and above, so that p, w <
-// 2^15: binary16 then holds weights down to 2^-38 of the largest, and the small
-// weights of long contexts are not lost.
+//   o = sum_t w c + sum_t p off_g,   w = p scale_g,
+// p and w rounded to binary16 (11 bits; everything else is fp32).  Weights are
+// kept relative to 2^base, base = the largest s so far (in powers of two) less 14,
+// more where a step has scales of 2 and above, so that p, w < 2^15: binary16 then
+// holds weights down to 2^-38 of the largest, and the small weights of long
+// contexts are not lost.
 #pragma once
 
 #include "mf_serve_dev.h"
 
+#ifndef WPE_
+#define WPE_ 2
+#endif
 namespace mfs {
 
 // What a row sees: tokens lo .. hi.
@@ -63,8 +71,7 @@ __device__ __forceinline__ Words<N> load_words(const uint8_t *p)
 template <int D, int G, int RT>
 struct AttnState {
     static constexpr int DT = D / 16, NG = D / G;
-    f32x4 o[RT][DT];      // sum w (16 + c): dims 16 t + 4 (l / 16) + r
-    f32x4 ow[RT][NG];     // sum w, in every element
+    f32x4 o[RT][DT];      // sum w c, 2^-24 (even t) or 2^-20 times: dims 16 t + 4 (l / 16) + r
     f32x4 om[RT];         // sum p off: element r is group (4 (l / 16) + r) % NG
     float base[RT], l[RT];   // weights are relative to 2^base; sum of p over the lane's tokens
 };
@@ -74,9 +81,11 @@ template <int D, int G>
 struct AttnTokens {
     static constexpr int NS = D / 32, NG = D / G;
     Words<NS> kc[2], vc[2];      // codes
-    u32x2 ks[2][NG], vs[2][NG];  // scales of tokens 4 (l / 16) .. + 3
-    u32x2 ko[2];                 // key offsets of token l % 16: a right operand's pairs of groups
+    Words<4 * NG> sc[2];         // scales of tokens 4 (l / 16) .. + 3: of the keys' groups, then of the values'
+    u32x2 ko[2];                 // key offsets of token l % 16: a left operand's pairs of groups
     u32x2 vo[2];                 // value offsets of group l % NG, tokens 4 (l / 16) .. + 3
+    __device__ __forceinline__ uint32_t key_scales(int u, int g, int pair) const { return sc[u].w[2 * g + pair]; }
+    __device__ __forceinline__ uint32_t value_scales(int u, int g, int pair) const { return sc[u].w[2 * NG + 2 * g + pair]; }
 };
 
 template <int D, int G>
@@ -87,12 +96,8 @@ __device__ __forceinline__ void load_tokens(AttnTokens<D, G> &x, int u, const ui
     x.kc[u] = load_words<NS>(rec + lane * (D / 8));
     x.vc[u] = load_words<NS>(rec + 8 * D + lane * (D / 8));
     const uint8_t *t = rec + 16 * D;
-#pragma unroll
-    for (int g = 0; g < NG; g++) {
-        x.ks[u][g] = *(const u32x2 *)(t + g * 32 + qt * 8);
-        x.vs[u][g] = *(const u32x2 *)(t + 64 * NG + g * 32 + qt * 8);
-    }
-    const uint8_t *ko = t + 32 * NG + col * 2 * NG;
+    x.sc[u] = load_words<4 * NG>(t + qt * 16 * NG);
+    const uint8_t *ko = t + 64 * NG + col * 2 * NG;
     if constexpr (NG == 1) x.ko[u] = (u32x2){*(const uint16_t *)ko, 0};
     if constexpr (NG == 2) x.ko[u] = (u32x2){*(const uint32_t *)ko, 0};
     if constexpr (NG == 4) x.ko[u] = *(const u32x2 *)ko;
@@ -100,64 +105,80 @@ __device__ __forceinline__ void load_tokens(AttnTokens<D, G> &x, int u, const ui
     x.vo[u] = *(const u32x2 *)(t + 96 * NG + (col & (NG - 1)) * 32 + qt * 8);
 }
 
+// A dword's codes as an operand: pairs 0 and 2 as they are, pairs 1 and 3 16 times.
+__device__ __forceinline__ u32x4 code_operand(uint32_t w)
+{
+    const uint32_t v = w >> 8;
+    return (u32x4){w & 0x000f000fu, w & 0x00f000f0u, v & 0x000f000fu, v & 0x00f000f0u};
+}
+// A score in the units of the products, over its true value, is 2^-L times this; 2^L <= the row's largest query < 2^(L + 1).
+template <bool F16>
+constexpr float kQueryUnit = F16 ? 0x1p-9f : 0x1p-7f;   // 2^(15 - 24), 2^(126 - 133)
+
 __device__ __forceinline__ float half_of(uint32_t w, int hi) { return (float)bits<f16x2>(w)[hi]; }
 
-// limit: tokens from it on were never written; c: softmax scale times log2 e (and the row's power of two).
-template <bool F16, int D, int G, int RT, bool MASK>
-__device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (&q)[RT][D / 32], const f32x4 (&start)[RT][D / G],
-                                          const u32x2 (&qsum)[RT], const AttnTokens<D, G> &x, const Sight (&see)[RT],
-                                          const bool (&ok)[2], int limit, int t0, const float (&c)[RT])
+// Whether a row sees the lane's token e (0..7) of a step; ok: bit u says that block u lies in a page of the cache.
+__device__ __forceinline__ bool sees(const Sight &v, int ok, int t0, int qt, int e)
+{
+    const int tok = t0 + 16 * (e >> 2) + 4 * qt + (e & 3);
+    return (ok >> (e >> 2) & 1) && tok >= v.lo && tok <= v.hi;
+}
+
+// full: every row sees every token; limit: tokens from it on were never written; c: softmax scale times log2 e (and the row's power of two).
+template <bool F16, int D, int G, int RT>
+__device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (&q)[RT][D / 32], const u32x2 (&qsum)[RT],
+                                          const AttnTokens<D, G> &x, const Sight (&see)[RT],
+                                          bool full, int ok, int limit, int t0, const float (&c)[RT])
 {
     constexpr int NG = D / G, IPG = G / 32;
     const int qt = (threadIdx.x & 63) >> 4;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     float p[RT][2][4];
-    uint32_t keep[RT][2][2];   // halves of the weights that the row sees
 #pragma unroll
     for (int u = 0; u < 2; u++) {
         f32x4 sc[RT];
 #pragma unroll
-        for (int t = 0; t < RT; t++)
+        for (int t = 0; t < RT; t++) {
             sc[t] = __builtin_amdgcn_mfma_f32_16x16x16f16(bits<f16x4>(x.ko[u]), bits<f16x4>(qsum[t]), zero, 0, 0, 0);
+            if (F16) sc[t] *= kQueryUnit<true>;
+        }
 #pragma unroll
         for (int g = 0; g < NG; g++) {
             f32x4 P[RT];
 #pragma unroll
             for (int i = 0; i < IPG; i++) {
-                const u32x4 A = codes8<F16>(x.kc[u].w[g * IPG + i]);
+                const u32x4 A = code_operand(x.kc[u].w[g * IPG + i]);
 #pragma unroll
-                for (int t = 0; t < RT; t++) P[t] = mfma<F16>(A, q[t][g * IPG + i], i ? P[t] : start[t][g]);
+                for (int t = 0; t < RT; t++) P[t] = mfma<F16>(A, q[t][g * IPG + i], i ? P[t] : zero);
             }
 #pragma unroll
             for (int t = 0; t < RT; t++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) sc[t][r] = fmaf(half_of(x.ks[u][g][r >> 1], r & 1), P[t][r], sc[t][r]);
+                for (int r = 0; r < 4; r++) sc[t][r] = fmaf(half_of(x.key_scales(u, g, r >> 1), r & 1), P[t][r], sc[t][r]);
         }
 #pragma unroll
-        for (int t = 0; t < RT; t++) {
-            keep[t][u][0] = keep[t][u][1] = 0;
+        for (int t = 0; t < RT; t++)
 #pragma unroll
-            for (int r = 0; r < 4; r++) {
-                p[t][u][r] = sc[t][r];
-                if (MASK) {
-                    const int tok = t0 + 16 * u + 4 * qt + r;
-                    if (ok[u] && tok >= see[t].lo && tok <= see[t].hi) keep[t][u][r >> 1] |= r & 1 ? 0xffff0000u : 0xffffu;
-                    else p[t][u][r] = -INFINITY;
-                }
-            }
-        }
+            for (int r = 0; r < 4; r++) p[t][u][r] = sc[t][r];
+    }
+    if (!full) {
+#pragma unroll
+        for (int t = 0; t < RT; t++)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (!sees(see[t], ok, t0, qt, e)) p[t][e >> 2][e & 3] = -INFINITY;
     }
     // scales of 2 and above (bit 14) are rare, and cost a lower start of the weights
     uint32_t any = 0;
 #pragma unroll
-    for (int g = 0; g < NG; g++) any |= x.vs[0][g][0] | x.vs[0][g][1] | x.vs[1][g][0] | x.vs[1][g][1];
+    for (int g = 0; g < NG; g++) any |= x.value_scales(0, g, 0) | x.value_scales(0, g, 1) | x.value_scales(1, g, 0) | x.value_scales(1, g, 1);
     float room = 14.f;
     if (__any(any & 0x40004000u)) {
         float v = 1.f;
 #pragma unroll
         for (int g = 0; g < NG; g++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) v = fmaxf(v, half_of(x.vs[e >> 2][g][(e >> 1) & 1], e & 1));
+            for (int e = 0; e < 8; e++) v = fmaxf(v, half_of(x.value_scales(e >> 2, g, (e >> 1) & 1), e & 1));
         v = fminf(quarters_max(v), 65504.f);
         room = 14.f - (float)((__float_as_uint(v) >> 23) - 127u);
     }
@@ -174,8 +195,6 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
             st.l[t] *= a;
             st.om[t] *= a;
 #pragma unroll
-            for (int g = 0; g < NG; g++) st.ow[t][g] *= a;
-#pragma unroll
             for (int d = 0; d < D / 16; d++) st.o[t][d] *= a;
         }
         const float base = st.base[t] == -INFINITY ? 0.f : st.base[t];
@@ -191,12 +210,13 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
         }
     }
     u32x4 vo = {x.vo[0][0], x.vo[0][1], x.vo[1][0], x.vo[1][1]};
-    if (MASK) {
+    if (!full) {
         // what was never written may be anything; a zero weight does not make it zero
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int tok = t0 + 16 * (e >> 1) + 4 * qt + 2 * (e & 1);
-            vo[e] &= (ok[e >> 1] && tok < limit ? 0xffffu : 0u) | (ok[e >> 1] && tok + 1 < limit ? 0xffff0000u : 0u);
+            const bool page = ok >> (e >> 1) & 1;
+            vo[e] &= (page && tok < limit ? 0xffffu : 0u) | (page && tok + 1 < limit ? 0xffff0000u : 0u);
         }
     }
 #pragma unroll
@@ -207,46 +227,110 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(x.vs[e >> 1][g][e & 1]));
-                if (MASK) wg[t][e] &= keep[t][e >> 1][e & 1];
-            }
+            for (int e = 0; e < 4; e++) wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(x.value_scales(e >> 1, g, e & 1)));
+        if (!full) {   // nor do scales of tokens that the row does not see
+#pragma unroll
+            for (int t = 0; t < RT; t++)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    wg[t][e] &= (sees(see[t], ok, t0, qt, 2 * e) ? 0xffffu : 0u) | (sees(see[t], ok, t0, qt, 2 * e + 1) ? 0xffff0000u : 0u);
+        }
 #pragma unroll
         for (int i = g * IPG; i < (g + 1) * IPG; i++) {
-            const uint32_t a = x.vc[0].w[i], b = x.vc[1].w[i];
-            const u32x4 lo = {codes2<true, 0>(a), codes2<true, 1>(a), codes2<true, 0>(b), codes2<true, 1>(b)};
-            const u32x4 hi = {codes2<true, 2>(a), codes2<true, 3>(a), codes2<true, 2>(b), codes2<true, 3>(b)};
+            const u32x4 a = code_operand(x.vc[0].w[i]), b = code_operand(x.vc[1].w[i]);
+            const u32x4 lo = {a[0], a[2], b[0], b[2]}, hi = {a[1], a[3], b[1], b[3]};
 #pragma unroll
             for (int t = 0; t < RT; t++) {
                 st.o[t][2 * i] = mfma<true>(lo, wg[t], st.o[t][2 * i]);
                 st.o[t][2 * i + 1] = mfma<true>(hi, wg[t], st.o[t][2 * i + 1]);
             }
         }
-#pragma unroll
-        for (int t = 0; t < RT; t++) st.ow[t][g] = mfma<true>(ones8<true>(), wg[t], st.ow[t][g]);
     }
 }
 
-// Work item: (sequence, key head, tile of attn_rows rows); splits workgroups take
-// parts of its tokens.  ROWS: the waves take different rows, all tokens each;
-// otherwise the same rows, every fourth step of tokens each, joined in LDS.
-template <bool F16, int D, int G, int RT, bool ROWS>
-__global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
+// A sequence of the batch as far as it lies in the step's rows and the cache,
+// whatever the device arrays hold.
+struct SeqRows {
+    int q0, n;            // first row, rows
+    int limit;            // tokens of the cache that may be read
+    long long first_p;    // position of the first row
+};
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x)
 {
-    constexpr int NS = D / 32, NG = D / G, IPG = G / 32, DT = D / 16, WG_ROWS = attn_rows(RT, ROWS);
+    return (long long)((unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
+}
+// The batch's numbers of a sequence, and what they come to.
+struct SeqRaw {
+    int q0, q1, kv;
+};
+__device__ __forceinline__ SeqRaw seq_raw(const KvBatch &b, int s) { return {b.q_start[s], b.q_start[s + 1], b.kv_len[s]}; }
+__device__ __forceinline__ SeqRows seq_rows(const KvBatch &b, const SeqRaw &w)
+{
+    SeqRows r;
+    r.q0 = w.q0;
+    r.limit = max(0, min(w.kv, b.max_kv));
+    r.first_p = (long long)w.kv - ((long long)w.q1 - w.q0);
+    r.n = w.q0 < 0 || w.q0 >= b.rows || w.q1 <= w.q0 ? 0 : min(w.q1, b.rows) - w.q0;
+    return r;
+}
+
+// Tokens [from, to) that rows i0 .. i1 of a sequence see, from on a step's bound.
+struct Range {
+    int from, to;
+};
+__device__ __forceinline__ Range range_of(const SeqRows &r, int i0, int i1, int window)
+{
+    return {sight_of(r.first_p + i0, window, r.limit).lo & ~(kAttnStep - 1), sight_of(r.first_p + i1, window, r.limit).hi + 1};
+}
+
+// Units of kAttnUnit tokens that one head of a sequence takes: one at least
+// where there are rows, for someone has to write them.
+__device__ __forceinline__ int units_of(const KvAttnArgs &a, const SeqRaw &w)
+{
+    const SeqRows r = seq_rows(a.b, w);
+    if (r.n == 0) return 0;
+    const Range t = range_of(r, 0, r.n - 1, a.window);
+    return t.to > t.from ? (t.to - t.from + kAttnUnit - 1) / kAttnUnit : 1;
+}
+
+__device__ __forceinline__ int wave_scan(int x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
+// 64 sequences as the lanes hold them: units of one head, and those up to and with the lane's.
+struct Lanes {
+    SeqRaw raw;
+    int units, upto, all;
+};
+__device__ __forceinline__ Lanes lanes_at(const KvAttnArgs &a, int s0, int lane)
+{
+    Lanes l = {{0, 0, 0}, 0, 0, 0};
+    if (s0 + lane < a.b.n_seq) {
+        l.raw = seq_raw(a.b, s0 + lane);
+        l.units = units_of(a, l.raw);
+    }
+    l.upto = wave_scan(l.units, lane);
+    l.all = __builtin_amdgcn_readlane(l.upto, 63);
+    return l;
+}
+
+// Rows row0 .. of one sequence and key head over its tokens [begin, end):
+// into the output (slot < 0) or a slot of the parts.
+// NW: waves that share the rows and take different tokens; 0: the wave has rows of its own.
+template <bool F16, int D, int G, int RT, int NW>
+__device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, const SeqRows &sr, int row0, int row_end, int begin, int end,
+                                          long long slot)
+{
+    constexpr int NS = D / 32, NG = D / G, IPG = G / 32, DT = D / 16;
     const int lane = threadIdx.x & 63, wave = wave_id(), col = lane & 15, qt = lane >> 4;
-    const int split = (int)(blockIdx.x % a.splits), item = (int)(blockIdx.x / a.splits);
-    const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
-    const int q0 = a.b.q_start[s];
-    const long long q1 = a.b.q_start[s + 1], kv = a.b.kv_len[s];
-    const int limit = kv < 0 ? 0 : kv < a.b.max_kv ? (int)kv : a.b.max_kv;
-    const long long first_p = kv - (q1 - q0);   // position of the sequence's first row
-    const int n = q0 < 0 || q0 >= a.b.rows || q1 <= q0 ? 0 : (int)((q1 < a.b.rows ? q1 : a.b.rows) - q0);
-    const int row_end = (int)min((long long)n * a.per_kv, (long long)(tile + 1) * WG_ROWS);
-    const int row0 = tile * WG_ROWS + (ROWS ? wave * RT * 16 : 0);
-    if (tile * WG_ROWS >= row_end) return;          // the whole workgroup
-    if (ROWS && row0 >= row_end) return;            // waves that take rows of their own never meet again
-    const int last = min(row_end, row0 + RT * 16) - 1;
+    const int last = min(row_end, row0 + RT * 16) - 1, limit = sr.limit;
 
     // rows past the last are computed as the last and not stored
     u32x4 q[RT][NS];
@@ -256,19 +340,54 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
     for (int t = 0; t < RT; t++) {
         const int r = min(row0 + 16 * t + col, last);
         const int i = r / a.per_kv;
-        qrow[t] = q0 + i;
+        qrow[t] = sr.q0 + i;
         qhead[t] = h * a.per_kv + (r - i * a.per_kv);
-        see[t] = sight_of(first_p + i, a.window, limit);
+        see[t] = sight_of(sr.first_p + i, a.window, limit);
         const uint16_t *x = (const uint16_t *)a.q + (long long)qrow[t] * a.q_stride + (long long)qhead[t] * a.q_head + qt * 8;
 #pragma unroll
         for (int d = 0; d < NS; d++) q[t][d] = load16(x + 32 * d);
     }
-    const Sight see0 = sight_of(first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(first_p + last / a.per_kv, a.window, limit);
-    const int from = see0.lo & ~(kAttnStep - 1), to = see1.hi + 1;   // tokens that some row sees, and none after
-    const long long part = from + (long long)split * a.chunk;
-    const int begin = (int)min(part, (long long)to), end = split + 1 == a.splits ? to : (int)min(part + a.chunk, (long long)to);
+    const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
 
-    f32x4 start[RT][NG];   // -16 sum q of a group
+    const int *table = a.b.table + (long long)s * a.b.table_stride;
+    constexpr bool ROWS = NW == 0;
+    constexpr int STRIDE = kAttnStep * (ROWS ? 1 : NW);
+    // Where the records of the next 32 steps start, in bytes: lane 2 i + u has block u
+    // of step i, -1 where there is none.  One gather for 32 steps: a page number
+    // that is fetched for the step at hand costs it a trip to memory.
+    long long starts;
+    const auto find = [&](int t0) {
+        const int at = t0 + (lane >> 1) * STRIDE, blk = (at >> 4) + (lane & 1);
+        starts = -1;
+        if (at < end && blk * kKvBlock < limit) {
+            const int pc = page_of_block(a.g, blk), page = table[pc];
+            if ((unsigned)page < (unsigned)a.g.n_pages)
+                starts = (((long long)page * a.g.n_kv_heads + h) * a.g.blocks_per_page + (blk - pc * a.g.blocks_per_page)) * a.g.rec;
+        }
+    };
+    const auto start_of = [&](int l) {
+        return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(starts >> 32), l) << 32 |
+                           (unsigned)__builtin_amdgcn_readlane((int)starts, l));
+    };
+    const auto load = [&](AttnTokens<D, G> &x, int i) {
+        // where there is none the first record is read, and masked
+        int ok = 0;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const long long at = start_of(2 * i + u);
+            ok |= (at >= 0) << u;
+            load_tokens(x, u, a.g.pages + (at < 0 ? 0 : at), lane);
+        }
+        return ok;
+    };
+    // the first step's records are on their way while the queries are made ready
+    int t0 = begin + (ROWS ? 0 : wave * kAttnStep), i = 0, ok = 0;
+    AttnTokens<D, G> x;
+    if (t0 < end) {
+        find(t0);
+        ok = load(x, 0);
+    }
+
     u32x2 qsum[RT];        // sum q as the right operand of the offsets' product: its pieces
     float c[RT];
     AttnState<D, G, RT> st;
@@ -281,28 +400,25 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
 #pragma unroll
             for (int i = 0; i < IPG; i++) x = mfma<F16>(ones8<F16>(), q[t][g * IPG + i], x);
             qs[g] = x[0];
-            big = fmaxf(big, fabsf(qs[g]));
         }
-        // queries whose sums binary16 may not hold are taken 2^-e times, and their products' scale 2^e
-        float down = 1.f;
-        c[t] = a.scale_log2;
-        if (big >= 16384.f) {
-            const int e = (int)(__float_as_uint(big) >> 23) - 127 - 13;
-            down = __uint_as_float((uint32_t)(127 - e) << 23);
-            c[t] *= __uint_as_float((uint32_t)(127 + e) << 23);
-        }
-        if (__any(down != 1.f)) {
 #pragma unroll
-            for (int d = 0; d < NS; d++)
+        for (int d = 0; d < NS; d++)
 #pragma unroll
-                for (int j = 0; j < 4; j++)
-                    q[t][d][j] = pack2<F16>(to_float<F16>((uint16_t)q[t][d][j]) * down, to_float<F16>((uint16_t)(q[t][d][j] >> 16)) * down);
-        }
+            for (int j = 0; j < 4; j++)
+                big = fmaxf(big, fmaxf(fabsf(to_float<F16>((uint16_t)q[t][d][j])), fabsf(to_float<F16>((uint16_t)(q[t][d][j] >> 16)))));
+        const int L = max((int)(__float_as_uint(quarters_max(big)) >> 23), 1) - 127, up = (F16 ? 15 : 126) - L;
+#pragma unroll
+        for (int d = 0; d < NS; d++)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                q[t][d][j] = pack2<F16>(__builtin_amdgcn_ldexpf(to_float<F16>((uint16_t)q[t][d][j]), up - 4 * (j & 1)),
+                                        __builtin_amdgcn_ldexpf(to_float<F16>((uint16_t)(q[t][d][j] >> 16)), up - 4 * (j & 1)));
+        c[t] = __builtin_amdgcn_ldexpf(a.scale_log2 / kQueryUnit<F16>, L);
         f16x4 piece = {(_Float16)0.f, (_Float16)0.f, (_Float16)0.f, (_Float16)0.f};
 #pragma unroll
         for (int g = 0; g < NG; g++) {
-            const float x = qs[g] * down;
-            start[t][g] = (f32x4){-16.f * x, -16.f * x, -16.f * x, -16.f * x};
+            // binary16's sums in units of 2^L (a piece of 2^-9 of them would be subnormal; attn_step makes up for it)
+            const float x = __builtin_amdgcn_ldexpf(F16 ? qs[g] : qs[g] * kQueryUnit<false>, -L);
             const _Float16 hi = (_Float16)x, lo = (_Float16)(x - (float)hi);
             if (NG <= 4) {
                 if (qt == 0) piece[g & 3] = hi;
@@ -311,7 +427,6 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
                 if (qt == g / 4) piece[g & 3] = hi;
                 if (qt == 2 + g / 4) piece[g & 3] = lo;
             }
-            st.ow[t][g] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
         qsum[t] = bits<u32x2>(piece);
         st.om[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -321,27 +436,19 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
         for (int d = 0; d < DT; d++) st.o[t][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
 
-    const int *table = a.b.table + (long long)s * a.b.table_stride;
-    for (int t0 = begin + (ROWS ? 0 : wave * kAttnStep); t0 < end; t0 += kAttnStep * (ROWS ? 1 : kAttnWaves)) {
-        AttnTokens<D, G> x;
-        bool ok[2];
-#pragma unroll
-        for (int u = 0; u < 2; u++) {
-            const int blk = (t0 >> 4) + u;
-            int page = -1, in = 0;
-            if (blk * kKvBlock < limit) {
-                const int pc = page_of_block(a.g, blk);
-                page = table[pc];
-                in = blk - pc * a.g.blocks_per_page;
-            }
-            ok[u] = (unsigned)page < (unsigned)a.g.n_pages;
-            // a page that is none of the cache's: the first record is read and masked
-            const long long at = ok[u] ? ((long long)page * a.g.n_kv_heads + h) * a.g.blocks_per_page + in : 0;
-            load_tokens(x, u, a.g.pages + at * a.g.rec, lane);
+    const auto step = [&](int ok, const AttnTokens<D, G> &x, int t0) {
+        const bool full = ok == 3 && t0 >= see1.lo && t0 + kAttnStep - 1 <= see0.hi;
+        attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, ok, limit, t0, c);
+    };
+    while (t0 < end) {
+        step(ok, x, t0);
+        t0 += STRIDE;
+        if (t0 >= end) break;
+        if (++i == 32) {
+            find(t0);
+            i = 0;
         }
-        const bool full = ok[0] && ok[1] && t0 >= see1.lo && t0 + kAttnStep - 1 <= see0.hi;
-        if (full) attn_step<F16, D, G, RT, false>(st, q, start, qsum, x, see, ok, limit, t0, c);
-        else attn_step<F16, D, G, RT, true>(st, q, start, qsum, x, see, ok, limit, t0, c);
+        ok = load(x, i);
     }
 
     // the lanes' own sums together; o: the values' weighted sum
@@ -355,17 +462,18 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
                 const float far = __shfl_xor(om, 16);
                 if ((qt & 1) != g / 4) om = far;
             }
-            const float add = om - 16.f * st.ow[t][g][0];
 #pragma unroll
-            for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++) st.o[t][d] += add;
+            for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) st.o[t][d][r] = fmaf(st.o[t][d][r], d & 1 ? 0x1p20f : 0x1p24f, om);
         }
     }
     if constexpr (!ROWS) {
-        // waves 2 and 3 hand over to 0 and 1, then 1 to 0
-        __shared__ f32x4 so[2][RT * DT][64];
-        __shared__ f32x2 sm[2][RT][64];
+        // the upper half of the waves hands over to the lower, and so on
+        __shared__ f32x4 so[NW / 2][RT * DT][64];
+        __shared__ f32x2 sm[NW / 2][RT][64];
 #pragma unroll
-        for (int half = 2; half >= 1; half >>= 1) {
+        for (int half = NW / 2; half >= 1; half >>= 1) {
             if (wave >= half && wave < 2 * half) {
 #pragma unroll
                 for (int t = 0; t < RT; t++) {
@@ -400,7 +508,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
     for (int t = 0; t < RT; t++) {
         const int r = row0 + 16 * t + col;
         if (r > last) continue;
-        if (a.splits == 1) {
+        if (slot < 0) {
             const bool none = st.l[t] == 0.f;   // no token; a NaN stays one
             const float inv = none ? 0.f : 1.f / st.l[t];
             uint16_t *y = (uint16_t *)a.out + (long long)qrow[t] * a.out_stride + (long long)qhead[t] * a.out_head + qt * 4;
@@ -414,30 +522,109 @@ __global__ __launch_bounds__(kAttnWaves * 64) void attn_kernel(KvAttnArgs a)
                 a.lse[(long long)qrow[t] * a.n_heads + qhead[t]] =
                     none ? -INFINITY : (st.base[t] + __builtin_amdgcn_logf(st.l[t])) * 0.69314718055994531f;
         } else {
-            const long long at = ((long long)item * a.splits + split) * WG_ROWS + (r - tile * WG_ROWS);
+            const long long at = slot * a.slot_rows + (ROWS ? r % a.slot_rows : r);
             float *y = a.part + at * D + qt * 4;
 #pragma unroll
             for (int d = 0; d < DT; d++) *(f32x4 *)(y + 16 * d) = st.o[t][d];
-            if (qt == 0) ((f32x2 *)(a.part + (long long)a.items * a.splits * WG_ROWS * D))[at] = (f32x2){st.base[t], st.l[t]};
+            if (qt == 0) ((f32x2 *)(a.part + (long long)a.slots * a.slot_rows * D))[at] = (f32x2){st.base[t], st.l[t]};
         }
     }
 }
 
-template <bool F16, int D, int G, int RT, bool ROWS>
-hipError_t go_attn(const KvAttnArgs &a, hipStream_t s)
+// By rows (many query tokens): a workgroup takes a tile of attn_rows rows, its
+// waves 16 RT of them each, over a part of their tokens.
+template <bool F16, int D, int G, int RT>
+__global__ __launch_bounds__(kAttnWaves * 64, D < 256 ? 2 : 1) void attn_rows_kernel(KvAttnArgs a)
 {
-    hipLaunchKernelGGL((attn_kernel<F16, D, G, RT, ROWS>), dim3((unsigned)((long long)a.items * a.splits)), dim3(kAttnWaves * 64), 0, s, a);
-    return hipGetLastError();
+    constexpr int WG_ROWS = attn_rows(RT, true);
+    const int split = (int)(blockIdx.x % a.splits), item = (int)(blockIdx.x / a.splits);
+    const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
+    const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
+    const int row_end = (int)min((long long)sr.n * a.per_kv, (long long)(tile + 1) * WG_ROWS);
+    const int row0 = tile * WG_ROWS + wave_id() * RT * 16;
+    if (row0 >= row_end) return;
+    const Range t = range_of(sr, row0 / a.per_kv, (min(row_end, row0 + RT * 16) - 1) / a.per_kv, a.window);
+    const long long part = t.from + (long long)split * a.chunk;
+    const int begin = (int)min(part, (long long)t.to), end = split + 1 == a.splits ? t.to : (int)min(part + a.chunk, (long long)t.to);
+    attn_item<F16, D, G, RT, 0>(a, s, h, sr, row0, row_end, begin, end, a.splits == 1 ? -1 : (long long)item * a.splits + split);
+}
+
+// By tokens (few rows: 16 RT at most of a sequence and key head): the waves of a
+// workgroup take every fourth step each.  Whole: a workgroup per sequence and
+// head.  Otherwise a.workgroups of them, as many as the card holds, take equal
+// shares of all sequences' tokens: a share may end inside a head, whose parts
+// the join adds up; slot 2 w is for a head that workgroup w found begun, 2 w + 1
+// for one that it leaves unfinished.
+template <bool F16, int D, int G, int RT, int NW, bool WHOLE>
+__global__ __launch_bounds__(NW * 64, WPE_) void attn_tokens_kernel(KvAttnArgs a)
+{
+    if constexpr (WHOLE) {
+        const int h = (int)(blockIdx.x % a.g.n_kv_heads), s = (int)(blockIdx.x / a.g.n_kv_heads);
+        const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
+        if (sr.n == 0) return;
+        const Range t = range_of(sr, 0, sr.n - 1, a.window);
+        attn_item<F16, D, G, RT, NW>(a, s, h, sr, 0, sr.n * a.per_kv, t.from, t.to, -1);
+        return;
+    }
+    const int lane = threadIdx.x & 63, heads = a.g.n_kv_heads;
+    Lanes l = lanes_at(a, 0, lane);
+    long long total = l.all;
+    for (int s0 = 64; s0 < a.b.n_seq; s0 += 64) total += lanes_at(a, s0, lane).all;
+    // units of all sequences (the outer order) and heads (the inner) in a row, `share` of them to a workgroup
+    const long long all = total * heads, share = (all + a.workgroups - 1) / a.workgroups, p = blockIdx.x * share;
+    if (p >= all) return;
+    long long todo = min(share, all - p), before = 0;
+    int s0 = 0;
+    while (p >= (before + l.all) * heads) {   // there is such a sequence: p < all
+        before += l.all;
+        s0 += 64;
+        l = lanes_at(a, s0, lane);
+    }
+    int i = __popcll(__ballot((before + l.upto) * heads <= p));   // a prefix of the lanes
+    int units = __builtin_amdgcn_readlane(l.units, i);
+    const long long in = p - (before + __builtin_amdgcn_readlane(l.upto, i) - units) * heads;
+    int h = (int)(in / units), off = (int)(in - (long long)h * units);
+    while (todo > 0) {
+        const SeqRaw raw = {__builtin_amdgcn_readlane(l.raw.q0, i), __builtin_amdgcn_readlane(l.raw.q1, i), __builtin_amdgcn_readlane(l.raw.kv, i)};
+        const SeqRows sr = seq_rows(a.b, raw);
+        const Range t = range_of(sr, 0, sr.n - 1, a.window);
+        const int take = (int)min((long long)(units - off), todo);
+        const bool begun = off > 0, ends = off + take == units;
+        const int begin = t.from + off * kAttnUnit, end = min(t.to, begin + take * kAttnUnit);
+        attn_item<F16, D, G, RT, NW>(a, s0 + i, h, sr, 0, sr.n * a.per_kv, begin, end, !begun && ends ? -1ll : 2ll * blockIdx.x + (begun ? 0 : 1));
+        todo -= take;
+        off = 0;
+        if (todo > 0 && ++h == heads) {
+            h = 0;
+            do {   // the next sequence with rows: there is one, units are left
+                if (++i == 64) {
+                    i = 0;
+                    s0 += 64;
+                    l = lanes_at(a, s0, lane);
+                }
+                units = __builtin_amdgcn_readlane(l.units, i);
+            } while (units == 0);
+        }
+    }
 }
 
 // One head size's kernels (mf_kv4_attn_d*.hip).
 template <bool F16, int D, int G>
 hipError_t pick_attn(const KvAttnArgs &a, const KvPlan &p, hipStream_t s)
 {
-    if (p.rows_by_wave) return go_attn<F16, D, G, 2, true>(a, s);
-    if constexpr (D < 256)
-        if (p.rt == 2) return go_attn<F16, D, G, 2, false>(a, s);
-    return go_attn<F16, D, G, 1, false>(a, s);
+    const dim3 grid((unsigned)p.workgroups);
+    if (p.rows_by_wave) hipLaunchKernelGGL((attn_rows_kernel<F16, D, G, 2>), grid, dim3(kAttnWaves * 64), 0, s, a);
+    else if (D < 256 && p.rt == 2) {
+        constexpr int RT = D < 256 ? 2 : 1;
+        if (!p.whole) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 4, false>), grid, dim3(256), 0, s, a);
+        else if (p.waves == 8) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 8, true>), grid, dim3(512), 0, s, a);
+        else hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 4, true>), grid, dim3(256), 0, s, a);
+    } else {
+        if (!p.whole) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, 1, 4, false>), grid, dim3(256), 0, s, a);
+        else if (p.waves == 8) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, 1, 8, true>), grid, dim3(512), 0, s, a);
+        else hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, 1, 4, true>), grid, dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace mfs

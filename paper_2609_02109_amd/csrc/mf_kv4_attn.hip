@@ -14,66 +14,149 @@ KvPlan kv4_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window)
     const long long rows = (long long)b.max_new * (n_heads / g.n_kv_heads);   // of a sequence and key head, at most
     p.rows_by_wave = rows > (g.head_dim < 256 ? 32 : 16);
     p.rt = p.rows_by_wave || rows > 16 ? 2 : 1;
-    const int wg_rows = attn_rows(p.rt, p.rows_by_wave);
-    p.row_tiles = (rows + wg_rows - 1) / wg_rows;
-    p.items = p.row_tiles * b.n_seq * g.n_kv_heads;
-    long long span = b.max_kv;   // tokens that a work item goes over, at most
+    long long span = b.max_kv;   // tokens that rows of an item go over, at most
     if (window > 0 && (long long)window + b.max_new + kAttnStep < span) span = (long long)window + b.max_new + kAttnStep;
-    const long long steps = (span + kAttnStep - 1) / kAttnStep;
-    // some 1024 workgroups in all, eight steps each at least
-    long long splits = p.items > 0 ? (1024 + p.items - 1) / p.items : 1;
-    if (splits > (steps + 7) / 8) splits = (steps + 7) / 8;
-    if (splits < 1) splits = 1;
-    const long long per = (steps + splits - 1) / splits;
-    p.chunk = (int)(per * kAttnStep);
-    p.splits = per > 0 ? (int)((steps + per - 1) / per) : 1;
-    if (p.splits < 1) p.splits = 1;
-    p.ws_bytes = p.splits > 1 ? (size_t)p.items * p.splits * wg_rows * (g.head_dim + 2) * sizeof(float) : 0;
+    const long long heads = (long long)b.n_seq * g.n_kv_heads;
+    p.splits = 1;
+    p.chunk = 0;
+    p.slots = 0;
+    p.whole = false;
+    p.waves = kAttnWaves;
+    if (p.rows_by_wave) {
+        const int wg_rows = attn_rows(p.rt, true);
+        p.row_tiles = (rows + wg_rows - 1) / wg_rows;
+        const long long items = p.row_tiles * heads, steps = (span + kAttnStep - 1) / kAttnStep;
+        long long splits = items > 0 ? (512 + items - 1) / items : 1;
+        if (splits > (steps + 31) / 32) splits = (steps + 31) / 32;
+        if (splits > 1) {
+            const long long per = (steps + splits - 1) / splits;
+            p.chunk = (int)(per * kAttnStep);
+            p.splits = (int)((steps + per - 1) / per);
+        }
+        p.workgroups = items * p.splits;
+        p.slots = p.splits > 1 ? p.workgroups : 0;
+        p.slot_rows = wg_rows;
+    } else {
+        p.row_tiles = 1;
+        // Whole heads have neither shares to find nor parts to join, which is some 10 us,
+        // but the longest decides (own heads of 64, 16 x 16 of them, up to 4000 tokens: 22.8
+        // us, shares 21.8; one request of 8 heads and 1000 tokens: 10.5 and 11.5, of 4000:
+        // 23.5 and 11.9; 200 x 8 heads of up to 600: 27 and 59).
+        const long long longest = heads * 16 < 1024 ? 1024 : heads * 16 < 4096 ? heads * 16 : 4096;
+        p.whole = span <= longest;
+        if (p.whole) {
+            // few heads: more waves to each (1 x 8 of 1000: 8 waves 10.5, 4 11.5; 200 x 8 of 600: 47 and 27)
+            p.waves = heads < 512 ? 8 : 4;
+            p.workgroups = heads;
+        } else {
+            // as many as are on the card at once, by the kernels' registers; two units each at least
+            const int per_cu = p.rt == 2 || g.head_dim == 256 ? 2 : g.head_dim == 64 ? 4 : g.group == 32 ? 2 : 3;
+            const long long units = (span + kAttnUnit - 1) / kAttnUnit, most = (units * heads + 1) / 2;
+            p.workgroups = most < 256 * per_cu ? most : 256 * per_cu;
+            p.slots = 2 * p.workgroups;
+        }
+        p.slot_rows = (int)rows;
+    }
+    p.ws_bytes = (size_t)(p.slots * p.slot_rows) * (g.head_dim + 2) * sizeof(float);
     return p;
 }
 
 namespace {
 
-// A wave per row: the parts' sums, each scaled to the common maximum, in order.
+constexpr int kJoinWaves = 4;
+
+// Adds up `parts` parts of a row: part i is in slot first (i = 0) or rest + i * step.
+// The workgroup's threads take four dims and every so many parts each.
 template <bool F16, int D>
-__global__ __launch_bounds__(64) void attn_join_kernel(KvAttnArgs a, int wg_rows)
+__device__ __forceinline__ void join_row(const KvAttnArgs &a, long long first, long long rest, long long step, int parts, int srow,
+                                         long long qrow, int head)
 {
-    const int item = (int)(blockIdx.x / wg_rows), rr = (int)(blockIdx.x % wg_rows);
-    const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
-    const int q0 = a.b.q_start[s];
-    const long long q1 = a.b.q_start[s + 1];
-    const int n = q0 < 0 || q0 >= a.b.rows || q1 <= q0 ? 0 : (int)((q1 < a.b.rows ? q1 : a.b.rows) - q0);
-    const long long row = (long long)tile * wg_rows + rr;
-    if (row >= (long long)n * a.per_kv) return;
-    const int i = (int)(row / a.per_kv), head = h * a.per_kv + (int)(row - (long long)i * a.per_kv), lane = threadIdx.x;
-    const f32x2 *ml = (const f32x2 *)(a.part + (long long)a.items * a.splits * wg_rows * D);
-    const long long at = (long long)item * a.splits * wg_rows + rr;
-    float m = -INFINITY;
-    for (int p = 0; p < a.splits; p++) m = fmaxf(m, ml[at + (long long)p * wg_rows][0]);
-    float l = 0.f, o[D / 64] = {};
-    for (int p = 0; p < a.splits; p++) {
-        const f32x2 part = ml[at + (long long)p * wg_rows];
-        const float x = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(part[0] - m);
-        l += part[1] * x;
-        const float *y = a.part + (at + (long long)p * wg_rows) * D;
+    constexpr int T = D / 4, PG = kJoinWaves * 64 / T;   // threads over a row, parts at a time
+    __shared__ f32x4 so[PG][T];
+    __shared__ f32x2 sm[PG];
+    const int t = threadIdx.x % T, g = threadIdx.x / T;
+    const f32x2 *ml = (const f32x2 *)(a.part + (long long)a.slots * a.slot_rows * D);
+    float base = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i = g; i < parts; i += PG) {
+        const long long at = (i ? rest + i * step : first) * a.slot_rows + srow;
+        const f32x2 m = ml[at];
+        const f32x4 v = *(const f32x4 *)(a.part + at * D + 4 * t);
+        const float to = fmaxf(base, m[0]), x = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(base - to),
+                    y = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[0] - to);
+        base = to;
+        l = l * x + m[1] * y;
 #pragma unroll
-        for (int d = 0; d < D / 64; d++) o[d] += y[d * 64 + lane] * x;
+        for (int r = 0; r < 4; r++) o[r] = o[r] * x + v[r] * y;
     }
-    uint16_t *out = (uint16_t *)a.out + (long long)(q0 + i) * a.out_stride + (long long)head * a.out_head;
+    so[g][t] = o;
+    if (t == 0) sm[g] = (f32x2){base, l};
+    __syncthreads();
+    if (g != 0) return;
+    const int n = parts < PG ? parts : PG;
+    for (int i = 0; i < n; i++) base = fmaxf(base, sm[i][0]);
+    l = 0.f;
+    o = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; i++) {
+        const float x = base == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[i][0] - base);
+        l += sm[i][1] * x;
+        o += so[i][t] * x;
+    }
+    uint16_t *out = (uint16_t *)a.out + qrow * a.out_stride + (long long)head * a.out_head + 4 * t;
     const float inv = l == 0.f ? 0.f : 1.f / l;   // no token; a NaN stays one
 #pragma unroll
-    for (int d = 0; d < D / 64; d++) out[d * 64 + lane] = from_float<F16>(o[d] * inv);
-    if (a.lse && lane == 0)
-        a.lse[(long long)(q0 + i) * a.n_heads + head] =
-            l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    for (int r = 0; r < 4; r++) out[r] = from_float<F16>(o[r] * inv);
+    if (a.lse && t == 0) a.lse[qrow * a.n_heads + head] = l == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+
+// A workgroup per row that work items may have.
+template <bool F16, int D>
+__global__ __launch_bounds__(kJoinWaves * 64) void join_rows_kernel(KvAttnArgs a)
+{
+    const int item = (int)(blockIdx.x / a.slot_rows), rr = (int)(blockIdx.x % a.slot_rows);
+    const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
+    const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
+    const long long row = (long long)tile * a.slot_rows + rr;
+    if (row >= (long long)sr.n * a.per_kv) return;
+    const int i = (int)(row / a.per_kv);
+    join_row<F16, D>(a, (long long)item * a.splits, (long long)item * a.splits, 1, a.splits, rr, sr.q0 + i,
+                     h * a.per_kv + (int)(row - (long long)i * a.per_kv));
+}
+
+// A workgroup per row of a sequence and head: its parts are those of the workgroups
+// whose shares the head's units lie in.
+template <bool F16, int D>
+__global__ __launch_bounds__(kJoinWaves * 64) void join_tokens_kernel(KvAttnArgs a)
+{
+    const int item = (int)(blockIdx.x / a.slot_rows), rr = (int)(blockIdx.x % a.slot_rows);
+    const int h = item % a.g.n_kv_heads, s = item / a.g.n_kv_heads, lane = threadIdx.x & 63;
+    const SeqRaw raw = seq_raw(a.b, s);
+    const SeqRows sr = seq_rows(a.b, raw);
+    if (rr >= (long long)sr.n * a.per_kv) return;
+    long long total = 0, before = 0;
+    for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
+        const Lanes l = lanes_at(a, s0, lane);
+        if (s >= s0 && s < s0 + 64) before = total + __builtin_amdgcn_readlane(l.upto - l.units, s - s0);
+        total += l.all;
+    }
+    const long long share = (total * a.g.n_kv_heads + a.workgroups - 1) / a.workgroups, units = units_of(a, raw);
+    const long long b0 = before * a.g.n_kv_heads + h * units, w0 = b0 / share, w1 = (b0 + units - 1) / share;
+    if (w0 == w1) return;   // one workgroup had it whole
+    const int i = rr / a.per_kv;
+    join_row<F16, D>(a, 2 * w0 + 1, 2 * w0, 2, (int)(w1 - w0 + 1), rr, sr.q0 + i, h * a.per_kv + rr - i * a.per_kv);
 }
 
 template <int D>
-void go_join(const KvAttnArgs &a, int wg_rows, bool f16, hipStream_t s)
+void go_join(const KvAttnArgs &a, const KvPlan &p, bool f16, long long items, hipStream_t s)
 {
-    const dim3 grid((unsigned)((long long)a.items * wg_rows));
-    if (f16) hipLaunchKernelGGL((attn_join_kernel<true, D>), grid, dim3(64), 0, s, a, wg_rows);
-    else hipLaunchKernelGGL((attn_join_kernel<false, D>), grid, dim3(64), 0, s, a, wg_rows);
+    const dim3 grid((unsigned)(items * a.slot_rows)), block(kJoinWaves * 64);
+    if (p.rows_by_wave) {
+        if (f16) hipLaunchKernelGGL((join_rows_kernel<true, D>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((join_rows_kernel<false, D>), grid, block, 0, s, a);
+    } else {
+        if (f16) hipLaunchKernelGGL((join_tokens_kernel<true, D>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((join_tokens_kernel<false, D>), grid, block, 0, s, a);
+    }
 }
 
 }  // namespace
@@ -81,11 +164,11 @@ void go_join(const KvAttnArgs &a, int wg_rows, bool f16, hipStream_t s)
 hipError_t launch_kv4_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s)
 {
     const hipError_t e = a.g.head_dim == 64 ? launch_attn_d64(a, p, f16, s) : a.g.head_dim == 128 ? launch_attn_d128(a, p, f16, s) : launch_attn_d256(a, p, f16, s);
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int wg_rows = attn_rows(p.rt, p.rows_by_wave);
-    if (a.g.head_dim == 64) go_join<64>(a, wg_rows, f16, s);
-    else if (a.g.head_dim == 128) go_join<128>(a, wg_rows, f16, s);
-    else go_join<256>(a, wg_rows, f16, s);
+    if (e != hipSuccess || p.slots == 0) return e;
+    const long long items = p.row_tiles * a.b.n_seq * a.g.n_kv_heads;
+    if (a.g.head_dim == 64) go_join<64>(a, p, f16, items, s);
+    else if (a.g.head_dim == 128) go_join<128>(a, p, f16, items, s);
+    else go_join<256>(a, p, f16, items, s);
     return hipGetLastError();
 }
 

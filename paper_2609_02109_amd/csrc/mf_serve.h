@@ -12,11 +12,8 @@ namespace mfs {
 
 // ---------------------------------------------------------------- codes
 // Eight codes of a row, k = 8 q + j, share a dword: code j sits at bits
-// 16 (j % 2) + 4 (j / 2).  So (w << 3 | w >> 1, 5, 9) & 0x00780078 puts one pair
-// (2 s, 2 s + 1) of codes where or-ing 0x4180 into each half makes two
-// bfloat16 values 16 + c, exactly (bits 6.. and 0x4c00 for binary16): one
-// shift and one and-or for two matrix operands.  The 16 is taken out of the
-// fp32 sums.
+// 16 (j % 2) + 4 (j / 2), so that a mask takes a pair (2 s, 2 s + 1) to the same
+// place in both halves: the two make one register of a matrix operand.
 
 // ------------------------------------------------------- packed 4-bit weights
 // [N / 16][K / 128] records: 1024 bytes of codes, then 128 / G x 16 dwords of
@@ -49,10 +46,10 @@ hipError_t launch_w4(const W4Args &a, int group, bool f16, hipStream_t s);
 //   keys    8 D bytes: lane l's D / 8 bytes at l D / 8; dword i is the codes
 //           d = 32 i + 8 (l / 16) .. + 7 of token l % 16 (an A operand)
 //   values  8 D bytes: lane l's D / 8 bytes at l D / 8; dword i is dims
-//           d = 32 i + l % 16 (pairs s = 0, 1) and 32 i + 16 + l % 16 (s = 2, 3)
-//           of tokens 4 (l / 16) .. + 3, pair s % 2 = tokens (2 s', 2 s' + 1)
-//   tables of 16 D / G binary16 each: key scales [group][token], key offsets
-//   [token][group], value scales [group][token], value offsets [group][token]
+//           d = 32 i + l % 16 (pairs s = 0, 2) and 32 i + 16 + l % 16 (s = 1, 3)
+//           of tokens 4 (l / 16) .. + 3, pair s / 2 = tokens (2 (s / 2), 2 (s / 2) + 1)
+//   binary16 tables: scales [token / 4][keys, values][group][token % 4], key
+//   offsets [token][group], value offsets [group][token]
 // The values' order makes the matrix product's own result rows (tokens
 // 4 (l / 16) + r) the next product's contraction index, so the softmax weights
 // never cross lanes.
@@ -105,6 +102,7 @@ struct KvReadArgs {
 };
 constexpr int kAttnWaves = 4;
 constexpr int kAttnStep = 32;   // tokens a wave takes at a time
+constexpr int kAttnUnit = kAttnStep * kAttnWaves;
 
 // Rows a workgroup covers.
 __host__ __device__ constexpr int attn_rows(int rt, bool rows_by_wave) { return rt * 16 * (rows_by_wave ? kAttnWaves : 1); }
@@ -117,17 +115,21 @@ struct KvAttnArgs {
     long long q_stride, q_head, out_stride, out_head;
     float scale_log2;        // softmax scale times log2 e
     int window, n_heads, per_kv;   // per_kv = n_heads / n_kv_heads
-    // plan (kv4_plan)
-    int items, row_tiles;    // work items; tiles of rows a sequence and head can have
-    int splits, chunk;       // parts of the tokens, tokens of a part
-    float *part;             // [item][split][row][D] sums, then [item][split][row] (base, sum of weights)
+    // from the plan (kv4_plan)
+    int row_tiles;           // by rows: tiles of rows that a sequence and head can have
+    int splits, chunk;       // by rows: parts of the tokens, tokens of a part
+    int workgroups, whole;   // by tokens
+    int slots, slot_rows;    // room for parts that the join adds up
+    float *part;             // [slot][row][D] sums, then [slot][row] (base, sum of weights)
 };
 // How the work is laid over the card: a function of the sizes alone.
 struct KvPlan {
     int rt;                  // 16-row tiles a wave holds
     bool rows_by_wave;       // the waves of a workgroup take different rows (else: different tokens)
-    long long row_tiles, items;
-    int splits, chunk;
+    bool whole;              // by tokens: a workgroup per sequence and head
+    int waves;               // by tokens: waves of a workgroup
+    long long row_tiles, workgroups, slots;
+    int splits, chunk, slot_rows;
     size_t ws_bytes;
 };
 KvPlan kv4_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window);

@@ -110,12 +110,18 @@ mf_status check_attn(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const
     a.window = args->window;
     a.scale_log2 = (float)((double)args->scale * 1.4426950408889634);
     p = kv4_plan(a.g, a.b, a.n_heads, a.window);
-    // work items times parts are one grid, and so are their rows in the join
-    if (p.items * p.splits > INT32_MAX || (p.splits > 1 && p.items * attn_rows(p.rt, p.rows_by_wave) > INT32_MAX)) return MF_EUNSUPPORTED;
-    a.items = (int)p.items;
+    // all sequences' units of one head are an int
+    if ((((int64_t)batch->max_kv + kAttnUnit - 1) / kAttnUnit + 1) * batch->n_seq > INT32_MAX) return MF_EUNSUPPORTED;
+    // one grid each: the workgroups, and the join's rows
+    const int64_t items = p.row_tiles * batch->n_seq * cache->n_kv_heads;
+    if (p.workgroups > INT32_MAX || (p.slots > 0 && (items * p.slot_rows > INT32_MAX || p.slots > INT32_MAX))) return MF_EUNSUPPORTED;
     a.row_tiles = (int)p.row_tiles;
     a.splits = p.splits;
     a.chunk = p.chunk;
+    a.workgroups = (int)p.workgroups;
+    a.whole = p.whole;
+    a.slots = (int)p.slots;
+    a.slot_rows = p.slot_rows;
     return MF_OK;
 }
 

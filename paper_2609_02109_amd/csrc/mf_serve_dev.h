@@ -58,17 +58,30 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return bits<uint32_t>(v);
 }
 
-// Codes 2 s, 2 s + 1 of a dword as two values 16 + c of the 16-bit type.
-template <bool F16, int S>
-__device__ __forceinline__ uint32_t codes2(uint32_t w)
+// Codes 2 s, 2 s + 1 of a dword as two values 16 + c of the 16-bit type.  The two
+// constants are kept in registers (one scalar, one vector): as literals they
+// would make an and and an or of one v_and_or_b32.
+struct CodeBits {
+    uint32_t mask, sixteen;
+};
+template <bool F16>
+__device__ __forceinline__ CodeBits code_bits()
 {
-    if (F16) return ((S < 2 ? w << (6 - 4 * S) : w >> (4 * S - 6)) & 0x03c003c0u) | 0x4c004c00u;
-    return ((S < 1 ? w << 3 : w >> (4 * S - 3)) & 0x00780078u) | 0x41804180u;
+    CodeBits b = {F16 ? 0x03c003c0u : 0x00780078u, F16 ? 0x4c004c00u : 0x41804180u};
+    asm("" : "+s"(b.mask));
+    asm("" : "+v"(b.sixteen));
+    return b;
+}
+template <bool F16, int S>
+__device__ __forceinline__ uint32_t codes2(uint32_t w, const CodeBits &b)
+{
+    if (F16) return ((S < 2 ? w << (6 - 4 * S) : w >> (4 * S - 6)) & b.mask) | b.sixteen;
+    return ((S < 1 ? w << 3 : w >> (4 * S - 3)) & b.mask) | b.sixteen;
 }
 template <bool F16>
-__device__ __forceinline__ u32x4 codes8(uint32_t w)
+__device__ __forceinline__ u32x4 codes8(uint32_t w, const CodeBits &b)
 {
-    return (u32x4){codes2<F16, 0>(w), codes2<F16, 1>(w), codes2<F16, 2>(w), codes2<F16, 3>(w)};
+    return (u32x4){codes2<F16, 0>(w, b), codes2<F16, 1>(w, b), codes2<F16, 2>(w, b), codes2<F16, 3>(w, b)};
 }
 
 // D += A B, 16 x 16 x 32: lane l holds A[l % 16][8 (l / 16) ..+8], B[8 (l / 16) ..+8][l % 16], D[4 (l / 16) + r][l % 16].

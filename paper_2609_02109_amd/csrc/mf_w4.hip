@@ -61,6 +61,7 @@ __global__ __launch_bounds__(NW * 64) void w4_kernel(W4Args a)
         const int m = m0 + t * 16 + col;
         xp[t] = (const uint16_t *)a.x + (long long)(m < a.rows ? m : a.rows - 1) * a.x_stride + qt * 8;
     }
+    const CodeBits cb = code_bits<F16>();
     f32x4 acc[MT][NT] = {};
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     for (int c = wave; c < chunks; c += NW) {
@@ -94,7 +95,7 @@ __global__ __launch_bounds__(NW * 64) void w4_kernel(W4Args a)
                 f32x4 P[MT];
 #pragma unroll
                 for (int i = 0; i < IPG; i++) {
-                    const u32x4 A = codes8<F16>(w[t][g * IPG + i]);
+                    const u32x4 A = codes8<F16>(w[t][g * IPG + i], cb);
 #pragma unroll
                     for (int m = 0; m < MT; m++) P[m] = mfma<F16>(A, x[m][g * IPG + i], i ? P[m] : zero);
                 }
