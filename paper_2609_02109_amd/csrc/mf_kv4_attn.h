@@ -17,10 +17,13 @@
 // O^T = V^T P^T takes its right operand: softmax weights stay in their lane.
 //   o = sum_t w c + sum_t p off_g,   w = p scale_g,
 // p and w rounded to binary16 (11 bits; everything else is fp32).  Weights are
-// kept relative to 2^base, base = the largest s so far (in powers of two) less 14,
-// more where a step has scales of 2 and above, so that p, w < 2^15: binary16 then
-// holds weights down to 2^-38 of the largest, and the small weights of long
-// contexts are not lost.
+// kept relative to 2^base.  The largest score is looked for only where a weight
+// shows that it is needed: a step's weights are computed with the base at hand,
+// and when one reaches 2^14, so that w could leave binary16's range, the base goes
+// to the largest score so far (in powers of two) less 10 and the step's weights
+// are computed again.  Binary16 then holds weights down to 2^-34 of the largest,
+// and the small weights of long contexts are not lost.  Steps with scales of 2
+// and above, which are rare, bound w by its own size.
 #pragma once
 
 #include "mf_serve_dev.h"
@@ -30,6 +33,11 @@
 #endif
 namespace mfs {
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x)
+{
+    return (long long)((unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
+}
 // What a row sees: tokens lo .. hi.
 struct Sight {
     int lo, hi;
@@ -68,6 +76,7 @@ __device__ __forceinline__ Words<N> load_words(const uint8_t *p)
 }
 
 // What a wave keeps for its rows: lane l's is row l % 16 of each tile.
+constexpr float kNoBase = -1e30f;   // before the first token; finite, so that differences of bases are
 template <int D, int G, int RT>
 struct AttnState {
     static constexpr int DT = D / 16, NG = D / G;
@@ -81,27 +90,33 @@ template <int D, int G>
 struct AttnTokens {
     static constexpr int NS = D / 32, NG = D / G;
     Words<NS> kc[2], vc[2];      // codes
-    Words<4 * NG> sc[2];         // scales of tokens 4 (l / 16) .. + 3: of the keys' groups, then of the values'
+    Words<2 * NG> ks[2], vs[2];  // scales of tokens 4 (l / 16) .. + 3, two words a group
     u32x2 ko[2];                 // key offsets of token l % 16: a left operand's pairs of groups
     u32x2 vo[2];                 // value offsets of group l % NG, tokens 4 (l / 16) .. + 3
-    __device__ __forceinline__ uint32_t key_scales(int u, int g, int pair) const { return sc[u].w[2 * g + pair]; }
-    __device__ __forceinline__ uint32_t value_scales(int u, int g, int pair) const { return sc[u].w[2 * NG + 2 * g + pair]; }
 };
 
 template <int D, int G>
-__device__ __forceinline__ void load_tokens(AttnTokens<D, G> &x, int u, const uint8_t *rec, int lane)
+__device__ __forceinline__ void load_keys(AttnTokens<D, G> &x, int u, const uint8_t *rec, int lane)
 {
     constexpr int NS = D / 32, NG = D / G;
     const int col = lane & 15, qt = lane >> 4;
-    x.kc[u] = load_words<NS>(rec + lane * (D / 8));
-    x.vc[u] = load_words<NS>(rec + 8 * D + lane * (D / 8));
     const uint8_t *t = rec + 16 * D;
-    x.sc[u] = load_words<4 * NG>(t + qt * 16 * NG);
+    x.kc[u] = load_words<NS>(rec + lane * (D / 8));
+    x.ks[u] = load_words<2 * NG>(t + qt * 16 * NG);
     const uint8_t *ko = t + 64 * NG + col * 2 * NG;
     if constexpr (NG == 1) x.ko[u] = (u32x2){*(const uint16_t *)ko, 0};
     if constexpr (NG == 2) x.ko[u] = (u32x2){*(const uint32_t *)ko, 0};
     if constexpr (NG == 4) x.ko[u] = *(const u32x2 *)ko;
     if constexpr (NG == 8) x.ko[u] = *(const u32x2 *)(ko + (qt & 1) * 8);
+}
+template <int D, int G>
+__device__ __forceinline__ void load_values(AttnTokens<D, G> &x, int u, const uint8_t *rec, int lane)
+{
+    constexpr int NS = D / 32, NG = D / G;
+    const int col = lane & 15, qt = lane >> 4;
+    const uint8_t *t = rec + 16 * D;
+    x.vc[u] = load_words<NS>(rec + 8 * D + lane * (D / 8));
+    x.vs[u] = load_words<2 * NG>(t + qt * 16 * NG + 8 * NG);
     x.vo[u] = *(const u32x2 *)(t + 96 * NG + (col & (NG - 1)) * 32 + qt * 8);
 }
 
@@ -124,11 +139,13 @@ __device__ __forceinline__ bool sees(const Sight &v, int ok, int t0, int qt, int
     return (ok >> (e >> 2) & 1) && tok >= v.lo && tok <= v.hi;
 }
 
-// full: every row sees every token; limit: tokens from it on were never written; c: softmax scale times log2 e (and the row's power of two).
-template <bool F16, int D, int G, int RT>
+// keys_done, values_done: called where the step has no more use for its keys and its values, to
+// fetch the next step's into their place.  full: every row sees every token; limit: tokens from it on were never written; c: softmax scale times log2 e (and the row's power of two).
+template <bool F16, int D, int G, int RT, class FK, class FV>
 __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (&q)[RT][D / 32], const u32x2 (&qsum)[RT],
                                           const AttnTokens<D, G> &x, const Sight (&see)[RT],
-                                          bool full, int ok, int limit, int t0, const float (&c)[RT])
+                                          bool full, int ok, int limit, int t0, const float (&c)[RT],
+                                          const FK &keys_done, const FV &values_done)
 {
     constexpr int NG = D / G, IPG = G / 32;
     const int qt = (threadIdx.x & 63) >> 4;
@@ -154,13 +171,14 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
 #pragma unroll
             for (int t = 0; t < RT; t++)
 #pragma unroll
-                for (int r = 0; r < 4; r++) sc[t][r] = fmaf(half_of(x.key_scales(u, g, r >> 1), r & 1), P[t][r], sc[t][r]);
+                for (int r = 0; r < 4; r++) sc[t][r] = fmaf(half_of(x.ks[u].w[2 * g + (r >> 1)], r & 1), P[t][r], sc[t][r]);
         }
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
             for (int r = 0; r < 4; r++) p[t][u][r] = sc[t][r];
     }
+    keys_done();
     if (!full) {
 #pragma unroll
         for (int t = 0; t < RT; t++)
@@ -168,47 +186,58 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
             for (int e = 0; e < 8; e++)
                 if (!sees(see[t], ok, t0, qt, e)) p[t][e >> 2][e & 3] = -INFINITY;
     }
-    // scales of 2 and above (bit 14) are rare, and cost a lower start of the weights
+    // weights are to stay below 2^top: 2^14, less where scales are 2 (bit 14) and above
     uint32_t any = 0;
 #pragma unroll
-    for (int g = 0; g < NG; g++) any |= x.value_scales(0, g, 0) | x.value_scales(0, g, 1) | x.value_scales(1, g, 0) | x.value_scales(1, g, 1);
-    float room = 14.f;
+    for (int g = 0; g < NG; g++) any |= x.vs[0].w[2 * g] | x.vs[0].w[2 * g + 1] | x.vs[1].w[2 * g] | x.vs[1].w[2 * g + 1];
+    int top = 14;
     if (__any(any & 0x40004000u)) {
         float v = 1.f;
 #pragma unroll
         for (int g = 0; g < NG; g++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) v = fmaxf(v, half_of(x.value_scales(e >> 2, g, (e >> 1) & 1), e & 1));
+            for (int e = 0; e < 8; e++) v = fmaxf(v, half_of(x.vs[e >> 2].w[2 * g + ((e >> 1) & 1)], e & 1));
         v = fminf(quarters_max(v), 65504.f);
-        room = 14.f - (float)((__float_as_uint(v) >> 23) - 127u);
+        top = uniform(14 - (int)((__float_as_uint(v) >> 23) - 127u));
     }
     u32x4 w[RT];
+    float e[RT][8];
+    for (bool raised = false;; raised = true) {   // twice at most
+        int highest[RT], over = 0;
+        const int most = (15 + top) << 10;   // 2^top in binary16
 #pragma unroll
-    for (int t = 0; t < RT; t++) {
-        float mx = p[t][0][0];
+        for (int t = 0; t < RT; t++) {
 #pragma unroll
-        for (int e = 1; e < 8; e++) mx = fmaxf(mx, p[t][e >> 2][e & 3]);
-        mx = fmaf(quarters_max(mx), c[t], -room);
-        if (__any(mx > st.base[t])) {
-            const float base = fmaxf(mx, st.base[t]), a = base == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.base[t] - base);
+            for (int i = 0; i < 8; i++) e[t][i] = __builtin_amdgcn_exp2f(fmaf(p[t][i >> 2][i & 3], c[t], -st.base[t]));
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[t][i] = pack2<true>(e[t][2 * i], e[t][2 * i + 1]);
+            // none is negative: as whole numbers they are in the same order
+            const u16x2 high = __builtin_elementwise_max(__builtin_elementwise_max(bits<u16x2>(w[t][0]), bits<u16x2>(w[t][1])),
+                                                         __builtin_elementwise_max(bits<u16x2>(w[t][2]), bits<u16x2>(w[t][3])));
+            highest[t] = max(high[0], high[1]);
+            over = max(over, highest[t]);
+        }
+        if (raised || !__any(over >= most)) break;
+#pragma unroll
+        for (int t = 0; t < RT; t++) {
+            // only the rows that need it, so that no row's result depends on another's
+            const bool hit = quarters_max((float)highest[t]) >= (float)most;
+            float mx = p[t][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; i++) mx = fmaxf(mx, p[t][i >> 2][i & 3]);
+            mx = fmaf(quarters_max(mx), c[t], 4.f - (float)top);
+            const float base = hit ? fmaxf(mx, st.base[t]) : st.base[t], a = __builtin_amdgcn_exp2f(st.base[t] - base);
             st.base[t] = base;
             st.l[t] *= a;
             st.om[t] *= a;
 #pragma unroll
             for (int d = 0; d < D / 16; d++) st.o[t][d] *= a;
         }
-        const float base = st.base[t] == -INFINITY ? 0.f : st.base[t];
-#pragma unroll
-        for (int u = 0; u < 2; u++) {
-#pragma unroll
-            for (int r = 0; r < 4; r++) {
-                p[t][u][r] = __builtin_amdgcn_exp2f(fmaf(p[t][u][r], c[t], -base));
-                st.l[t] += p[t][u][r];
-            }
-            w[t][2 * u] = pack2<true>(p[t][u][0], p[t][u][1]);
-            w[t][2 * u + 1] = pack2<true>(p[t][u][2], p[t][u][3]);
-        }
     }
+#pragma unroll
+    for (int t = 0; t < RT; t++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) st.l[t] += e[t][i];
     u32x4 vo = {x.vo[0][0], x.vo[0][1], x.vo[1][0], x.vo[1][1]};
     if (!full) {
         // what was never written may be anything; a zero weight does not make it zero
@@ -227,7 +256,7 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
-            for (int e = 0; e < 4; e++) wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(x.value_scales(e >> 1, g, e & 1)));
+            for (int e = 0; e < 4; e++) wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(x.vs[e >> 1].w[2 * g + (e & 1)]));
         if (!full) {   // nor do scales of tokens that the row does not see
 #pragma unroll
             for (int t = 0; t < RT; t++)
@@ -246,6 +275,7 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
             }
         }
     }
+    values_done();
 }
 
 // A sequence of the batch as far as it lies in the step's rows and the cache,
@@ -255,11 +285,6 @@ struct SeqRows {
     int limit;            // tokens of the cache that may be read
     long long first_p;    // position of the first row
 };
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long long uniform(long long x)
-{
-    return (long long)((unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32 | (unsigned)uniform((int)x));
-}
 // The batch's numbers of a sequence, and what they come to.
 struct SeqRaw {
     int q0, q1, kv;
@@ -324,7 +349,9 @@ __device__ __forceinline__ Lanes lanes_at(const KvAttnArgs &a, int s0, int lane)
 // Rows row0 .. of one sequence and key head over its tokens [begin, end):
 // into the output (slot < 0) or a slot of the parts.
 // NW: waves that share the rows and take different tokens; 0: the wave has rows of its own.
-template <bool F16, int D, int G, int RT, int NW>
+// AHEAD: a step's keys and values are fetched where the step before has no more use for its
+// own, which takes some 20 registers.
+template <bool F16, int D, int G, int RT, int NW, bool AHEAD>
 __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, const SeqRows &sr, int row0, int row_end, int begin, int end,
                                           long long slot)
 {
@@ -369,23 +396,33 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
         return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(starts >> 32), l) << 32 |
                            (unsigned)__builtin_amdgcn_readlane((int)starts, l));
     };
-    const auto load = [&](AttnTokens<D, G> &x, int i) {
-        // where there is none the first record is read, and masked
-        int ok = 0;
+    // a step's records, and which of them there are; where there is none the first one is read, and masked
+    struct Step {
+        const uint8_t *rec[2];
+        int ok;
+    };
+    const auto step_at = [&](int i) {
+        Step r;
+        r.ok = 0;
 #pragma unroll
         for (int u = 0; u < 2; u++) {
             const long long at = start_of(2 * i + u);
-            ok |= (at >= 0) << u;
-            load_tokens(x, u, a.g.pages + (at < 0 ? 0 : at), lane);
+            r.ok |= (at >= 0) << u;
+            r.rec[u] = a.g.pages + (at < 0 ? 0 : at);
         }
-        return ok;
+        return r;
     };
     // the first step's records are on their way while the queries are made ready
-    int t0 = begin + (ROWS ? 0 : wave * kAttnStep), i = 0, ok = 0;
+    int t0 = begin + (ROWS ? 0 : wave * kAttnStep), i = 0;
     AttnTokens<D, G> x;
+    Step now = {{a.g.pages, a.g.pages}, 0};
     if (t0 < end) {
         find(t0);
-        ok = load(x, 0);
+        now = step_at(0);
+#pragma unroll
+        for (int u = 0; u < 2; u++) load_keys(x, u, now.rec[u], lane);
+#pragma unroll
+        for (int u = 0; u < 2; u++) load_values(x, u, now.rec[u], lane);
     }
 
     u32x2 qsum[RT];        // sum q as the right operand of the offsets' product: its pieces
@@ -430,25 +467,43 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
         }
         qsum[t] = bits<u32x2>(piece);
         st.om[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        st.base[t] = -INFINITY;
+        st.base[t] = kNoBase;
         st.l[t] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; d++) st.o[t][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
 
-    const auto step = [&](int ok, const AttnTokens<D, G> &x, int t0) {
-        const bool full = ok == 3 && t0 >= see1.lo && t0 + kAttnStep - 1 <= see0.hi;
-        attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, ok, limit, t0, c);
+    const auto keys_of = [&](const Step &r) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) load_keys(x, u, r.rec[u], lane);
+    };
+    const auto values_of = [&](const Step &r) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) load_values(x, u, r.rec[u], lane);
     };
     while (t0 < end) {
-        step(ok, x, t0);
-        t0 += STRIDE;
-        if (t0 >= end) break;
-        if (++i == 32) {
-            find(t0);
+        const bool full = now.ok == 3 && t0 >= see1.lo && t0 + kAttnStep - 1 <= see0.hi;
+        if (++i == 32 && AHEAD) {
+            find(t0 + STRIDE);
             i = 0;
         }
-        ok = load(x, i);
+        if constexpr (AHEAD) {
+            const Step next = step_at(i);   // past the end: records that are none
+            attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, now.ok, limit, t0, c, [&] { keys_of(next); }, [&] { values_of(next); });
+            now = next;
+        } else {
+            attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, now.ok, limit, t0, c, [] {}, [] {});
+            if (t0 + STRIDE < end) {
+                if (i == 32) {
+                    find(t0 + STRIDE);
+                    i = 0;
+                }
+                now = step_at(i);
+                keys_of(now);
+                values_of(now);
+            }
+        }
+        t0 += STRIDE;
     }
 
     // the lanes' own sums together; o: the values' weighted sum
@@ -488,8 +543,7 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
                 for (int t = 0; t < RT; t++) {
                     const f32x2 other = sm[wave][t][lane];
                     const float base = fmaxf(st.base[t], other[0]);
-                    const float x = base == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.base[t] - base);
-                    const float y = base == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(other[0] - base);
+                    const float x = __builtin_amdgcn_exp2f(st.base[t] - base), y = __builtin_amdgcn_exp2f(other[0] - base);
                     st.base[t] = base;
                     st.l[t] = st.l[t] * x + other[1] * y;
 #pragma unroll
@@ -546,7 +600,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, D < 256 ? 2 : 1) void attn_rows_ke
     const Range t = range_of(sr, row0 / a.per_kv, (min(row_end, row0 + RT * 16) - 1) / a.per_kv, a.window);
     const long long part = t.from + (long long)split * a.chunk;
     const int begin = (int)min(part, (long long)t.to), end = split + 1 == a.splits ? t.to : (int)min(part + a.chunk, (long long)t.to);
-    attn_item<F16, D, G, RT, 0>(a, s, h, sr, row0, row_end, begin, end, a.splits == 1 ? -1 : (long long)item * a.splits + split);
+    attn_item<F16, D, G, RT, 0, true>(a, s, h, sr, row0, row_end, begin, end, a.splits == 1 ? -1 : (long long)item * a.splits + split);
 }
 
 // By tokens (few rows: 16 RT at most of a sequence and key head): the waves of a
@@ -563,7 +617,7 @@ __global__ __launch_bounds__(NW * 64, WPE_) void attn_tokens_kernel(KvAttnArgs a
         const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
         if (sr.n == 0) return;
         const Range t = range_of(sr, 0, sr.n - 1, a.window);
-        attn_item<F16, D, G, RT, NW>(a, s, h, sr, 0, sr.n * a.per_kv, t.from, t.to, -1);
+        attn_item<F16, D, G, RT, NW, RT == 1>(a, s, h, sr, 0, sr.n * a.per_kv, t.from, t.to, -1);
         return;
     }
     const int lane = threadIdx.x & 63, heads = a.g.n_kv_heads;
@@ -591,7 +645,7 @@ __global__ __launch_bounds__(NW * 64, WPE_) void attn_tokens_kernel(KvAttnArgs a
         const int take = (int)min((long long)(units - off), todo);
         const bool begun = off > 0, ends = off + take == units;
         const int begin = t.from + off * kAttnUnit, end = min(t.to, begin + take * kAttnUnit);
-        attn_item<F16, D, G, RT, NW>(a, s0 + i, h, sr, 0, sr.n * a.per_kv, begin, end, !begun && ends ? -1ll : 2ll * blockIdx.x + (begun ? 0 : 1));
+        attn_item<F16, D, G, RT, NW, false>(a, s0 + i, h, sr, 0, sr.n * a.per_kv, begin, end, !begun && ends ? -1ll : 2ll * blockIdx.x + (begun ? 0 : 1));
         todo -= take;
         off = 0;
         if (todo > 0 && ++h == heads) {

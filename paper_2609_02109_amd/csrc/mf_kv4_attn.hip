@@ -76,14 +76,13 @@ __device__ __forceinline__ void join_row(const KvAttnArgs &a, long long first, l
     __shared__ f32x2 sm[PG];
     const int t = threadIdx.x % T, g = threadIdx.x / T;
     const f32x2 *ml = (const f32x2 *)(a.part + (long long)a.slots * a.slot_rows * D);
-    float base = -INFINITY, l = 0.f;
+    float base = kNoBase, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i = g; i < parts; i += PG) {
         const long long at = (i ? rest + i * step : first) * a.slot_rows + srow;
         const f32x2 m = ml[at];
         const f32x4 v = *(const f32x4 *)(a.part + at * D + 4 * t);
-        const float to = fmaxf(base, m[0]), x = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(base - to),
-                    y = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[0] - to);
+        const float to = fmaxf(base, m[0]), x = __builtin_amdgcn_exp2f(base - to), y = __builtin_amdgcn_exp2f(m[0] - to);
         base = to;
         l = l * x + m[1] * y;
 #pragma unroll
@@ -98,7 +97,7 @@ __device__ __forceinline__ void join_row(const KvAttnArgs &a, long long first, l
     l = 0.f;
     o = (f32x4){0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < n; i++) {
-        const float x = base == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[i][0] - base);
+        const float x = __builtin_amdgcn_exp2f(sm[i][0] - base);
         l += sm[i][1] * x;
         o += so[i][t] * x;
     }

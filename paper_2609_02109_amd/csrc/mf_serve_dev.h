@@ -11,6 +11,7 @@ namespace mfs {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -51,7 +52,7 @@ template <bool F16>
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
     if (F16) {
-        const f16x2 v = {(_Float16)a, (_Float16)b};
+        const f16x2 v = __builtin_convertvector((f32x2){a, b}, f16x2);
         return bits<uint32_t>(v);
     }
     const bf16x2 v = __builtin_convertvector((f32x2){a, b}, bf16x2);
