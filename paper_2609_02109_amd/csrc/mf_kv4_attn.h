@@ -28,9 +28,6 @@
 
 #include "mf_serve_dev.h"
 
-#ifndef WPE_
-#define WPE_ 2
-#endif
 namespace mfs {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -588,7 +585,7 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
 // By rows (many query tokens): a workgroup takes a tile of attn_rows rows, its
 // waves 16 RT of them each, over a part of their tokens.
 template <bool F16, int D, int G, int RT>
-__global__ __launch_bounds__(kAttnWaves * 64, D < 256 ? 2 : 1) void attn_rows_kernel(KvAttnArgs a)
+__global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_rows_kernel(KvAttnArgs a)
 {
     constexpr int WG_ROWS = attn_rows(RT, true);
     const int split = (int)(blockIdx.x % a.splits), item = (int)(blockIdx.x / a.splits);
@@ -610,7 +607,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, D < 256 ? 2 : 1) void attn_rows_ke
 // the join adds up; slot 2 w is for a head that workgroup w found begun, 2 w + 1
 // for one that it leaves unfinished.
 template <bool F16, int D, int G, int RT, int NW, bool WHOLE>
-__global__ __launch_bounds__(NW * 64, WPE_) void attn_tokens_kernel(KvAttnArgs a)
+__global__ __launch_bounds__(NW * 64, 2) void attn_tokens_kernel(KvAttnArgs a)
 {
     if constexpr (WHOLE) {
         const int h = (int)(blockIdx.x % a.g.n_kv_heads), s = (int)(blockIdx.x / a.g.n_kv_heads);
@@ -667,7 +664,7 @@ template <bool F16, int D, int G>
 hipError_t pick_attn(const KvAttnArgs &a, const KvPlan &p, hipStream_t s)
 {
     const dim3 grid((unsigned)p.workgroups);
-    if (p.rows_by_wave) hipLaunchKernelGGL((attn_rows_kernel<F16, D, G, 2>), grid, dim3(kAttnWaves * 64), 0, s, a);
+    if (p.rows_by_wave) hipLaunchKernelGGL((attn_rows_kernel<F16, D, G, D < 256 ? 2 : 1>), grid, dim3(kAttnWaves * 64), 0, s, a);
     else if (D < 256 && p.rt == 2) {
         constexpr int RT = D < 256 ? 2 : 1;
         if (!p.whole) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 4, false>), grid, dim3(256), 0, s, a);

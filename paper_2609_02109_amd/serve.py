@@ -20,7 +20,7 @@ import threading
 import torch
 
 from . import mf
-from .mf import _check, _keep_for, _ptr, _stream
+from .mf import _check, _keep_for, _ptr
 
 _DTYPES = {torch.float32: mf.MF_F32, torch.bfloat16: mf.MF_BF16, torch.float16: mf.MF_F16}
 _HALF = (torch.bfloat16, torch.float16)
@@ -58,6 +58,19 @@ class AttnArgs(C.Structure):
                 ("q_head_stride", _i64), ("out_stride", _i64), ("out_head_stride", _i64), ("scale", C.c_float), ("window", _i32)]
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(device, stream):
+    """hipStream_t of `stream` or of torch's current stream on `device` (whose
+    Python object costs as much to make as a kernel launch)."""
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
+
+
 def _require(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
@@ -65,9 +78,9 @@ def _require(ok: bool, what: str):
 
 def _rows(t, name, shape, dtype, device):
     """A tensor of `shape` whose last dimension is contiguous (a copy where it is not)."""
-    _require(isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device,
-             f"{name}: {tuple(shape)} {dtype} on {device} is wanted")
-    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name}: {tuple(shape)} {dtype} on {device} is wanted")
+    return t if t.stride(-1) == 1 else t.contiguous()
 
 
 def _into(t, name, shape, dtype, device):
@@ -107,29 +120,36 @@ class W4Weight:
         self.packed = torch.empty(int(nb.value), dtype=torch.uint8, device=self.device)
         _keep_for(stream, codes, scales, zeros, self.packed)
         _check(mf.lib.mf_w4_pack(C.byref(self.desc), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(self.packed),
-                                 C.c_size_t(self.packed.numel()), _stream(stream)), "mf_w4_pack")
+                                 C.c_size_t(self.packed.numel()), _stream_of(self.device, stream)), "mf_w4_pack")
+        self._packed_ptr = self.packed.data_ptr()
 
     def matmul(self, x, bias=None, out=None, stream=None):
         """x [.., K] @ W.T + bias [N] -> [.., N], in the scales' type."""
-        _require(x.dim() >= 1 and x.shape[-1] == self.n_in and x.dtype is self.dtype and x.device == self.device,
-                 f"x: [.., {self.n_in}] {self.dtype} on {self.device} is wanted")
-        _require(bias is None or (bias.dtype is self.dtype and bias.device == self.device and tuple(bias.shape) == (self.n_out,)
-                                  and bias.is_contiguous()), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
         lead = x.shape[:-1]
-        if x.dim() != 2:
+        if not lead or x.shape[-1] != self.n_in or x.dtype is not self.dtype or x.device != self.device:
+            _require(x.dim() == 1 and x.shape[0] == self.n_in and x.dtype is self.dtype and x.device == self.device,
+                     f"x: [.., {self.n_in}] {self.dtype} on {self.device} is wanted")
+        if bias is not None:
+            _require(bias.dtype is self.dtype and bias.device == self.device and tuple(bias.shape) == (self.n_out,)
+                     and bias.is_contiguous(), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
+        if len(lead) != 1:
             x = x.reshape(-1, self.n_in)
         if x.stride(1) != 1:
             x = x.contiguous()
+        m = x.shape[0]
         if out is None:
-            y = torch.empty((x.shape[0], self.n_out), dtype=self.dtype, device=self.device)
+            y = x.new_empty((m, self.n_out))
             out = y if len(lead) == 1 else y.view(*lead, self.n_out)
         else:
             _into(out, "out", (*lead, self.n_out), self.dtype, self.device)
             y = out if out.dim() == 2 else out.view(-1, self.n_out)
-        args = W4Args(self.desc, self.packed.data_ptr(), x.data_ptr(), bias.data_ptr() if bias is not None else None, y.data_ptr(),
-                      x.shape[0], x.stride(0), y.stride(0))
-        _keep_for(stream, x, bias, y, self.packed)
-        _check(mf.lib.mf_w4_matmul(C.byref(args), _stream(stream)), "mf_w4_matmul")
+        args = W4Args(self.desc, self._packed_ptr, x.data_ptr(), None if bias is None else bias.data_ptr(), y.data_ptr(), m,
+                      x.stride(0), y.stride(0))
+        if stream is not None:
+            _keep_for(stream, x, bias, y, self.packed)
+        s = mf.lib.mf_w4_matmul(C.byref(args), _stream_of(self.device, stream))
+        if s:
+            _check(s, "mf_w4_matmul")
         return out
 
 
@@ -155,6 +175,7 @@ class KV4Batch:
         _require(page_table.dim() == 2 and page_table.shape[0] == n and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
                  "page_table: [n_seq, pages] with a contiguous last dimension is wanted")
         self.tensors = (q_start, kv_len, page_table)
+        self._ws_bytes = {}   # of attention, by (query heads, window): a function of the sizes
         self.rows = int(rows)
         self.raw = Batch(n, int(max_new), int(max_kv), self.rows, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                          page_table.stride(0), int(page_table.shape[1]))
@@ -193,40 +214,48 @@ class KV4Cache:
         turned by their positions when cos / sin [n_pos, rot_dim // 2] are given;
         with q [rows, n_heads, head_dim] also returns the queries turned the
         same way (q_out: where to, e.g. q itself)."""
-        _require(isinstance(k, torch.Tensor) and k.dtype in _HALF, "k: bfloat16 or float16 is wanted")
-        shape, dt, dev = (batch.rows, self.n_kv_heads, self.head_dim), k.dtype, self.device
+        dt, dev = k.dtype, self.device
+        _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
+        shape = (batch.rows, self.n_kv_heads, self.head_dim)
         k, v = _rows(k, "k", shape, dt, dev), _rows(v, "v", shape, dt, dev)
         _require((cos is None) == (sin is None), "cos and sin: both or neither are wanted")
-        a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+        a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), *k.stride()[:2], *v.stride()[:2])
         if cos is not None:
-            _require(cos.dim() == 2 and all(t.shape == cos.shape and t.dtype is torch.float32 and t.device == dev and t.is_contiguous()
-                                            for t in (cos, sin)), f"cos, sin: contiguous float32 [n_pos, rot_dim // 2] on {dev} is wanted")
-            a.d_cos, a.d_sin, a.n_pos, a.rot_dim = cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1]
-            a.interleaved = int(bool(interleaved))
+            n_pos, half = cos.shape
+            _require(cos.shape == sin.shape and cos.dtype is sin.dtype is torch.float32 and cos.device == sin.device == dev
+                     and cos.is_contiguous() and sin.is_contiguous(), f"cos, sin: contiguous float32 [n_pos, rot_dim // 2] on {dev} is wanted")
+            a.d_cos, a.d_sin, a.n_pos, a.rot_dim = cos.data_ptr(), sin.data_ptr(), n_pos, 2 * half
+            a.interleaved = 1 if interleaved else 0
         if q is not None:
             _require(cos is not None, "q: only turned here, so cos and sin are wanted with it")
             _require(q.dim() == 3, "q: [rows, n_heads, head_dim] is wanted")
-            q = _rows(q, "q", (batch.rows, q.shape[1], self.head_dim), dt, dev)
-            q_out = _into(q_out, "q_out", q.shape, dt, dev)
-            a.n_heads, a.d_q, a.d_q_out = q.shape[1], q.data_ptr(), q_out.data_ptr()
-            a.q_stride, a.q_head_stride, a.qo_stride, a.qo_head_stride = q.stride(0), q.stride(1), q_out.stride(0), q_out.stride(1)
-        _keep_for(stream, k, v, cos, sin, q, q_out, self.pages, *batch.tensors)
-        _check(mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream(stream)), "mf_kv4_append")
+            heads = q.shape[1]
+            q = _rows(q, "q", (batch.rows, heads, self.head_dim), dt, dev)
+            q_out = q.new_empty(q.shape) if q_out is None else _into(q_out, "q_out", q.shape, dt, dev)
+            a.n_heads, a.d_q, a.d_q_out = heads, q.data_ptr(), q_out.data_ptr()
+            a.q_stride, a.q_head_stride, _ = q.stride()
+            a.qo_stride, a.qo_head_stride, _ = q_out.stride()
+        if stream is not None:
+            _keep_for(stream, k, v, cos, sin, q, q_out, self.pages, *batch.tensors)
+        s = mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream_of(dev, stream))
+        if s:
+            _check(s, "mf_kv4_append")
         return q_out
 
     def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
         """(keys, values) [rows, n_kv_heads, head_dim] that the cache holds for the batch's rows."""
         _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
-        shape = (batch.rows, self.n_kv_heads, self.head_dim)
-        k, v = torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device)
-        _keep_for(stream, k, v, self.pages, *batch.tensors)
-        _check(mf.lib.mf_kv4_read(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(), _stream(stream)),
-               "mf_kv4_read")
+        k, v = torch.empty((2, batch.rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device).unbind(0)
+        if stream is not None:
+            _keep_for(stream, k, v, self.pages, *batch.tensors)
+        s = mf.lib.mf_kv4_read(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(),
+                               _stream_of(self.device, stream))
+        if s:
+            _check(s, "mf_kv4_read")
         return k, v
 
     def _workspace(self, nbytes: int, stream):
-        s = stream if stream is not None else torch.cuda.current_stream(self.device)
-        key = (threading.get_ident(), s.cuda_stream)
+        key = (threading.get_ident(), _stream_of(self.device, stream))
         with self._ws_lock:
             ws = self._ws.get(key)
             if ws is None or ws.numel() < nbytes:
@@ -240,17 +269,22 @@ class KV4Cache:
         tokens: [rows, n_heads, head_dim], with lse=True also the log of the
         softmax sums [rows, n_heads] float32.  scale: 1 / sqrt(head_dim) by
         default; window > 0: only the newest `window` tokens up to each row's."""
-        _require(isinstance(q, torch.Tensor) and q.dtype in _HALF and q.dim() == 3, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
-        q = _rows(q, "q", (batch.rows, q.shape[1], self.head_dim), q.dtype, self.device)
-        out = _into(out, "out", q.shape, q.dtype, self.device)
-        ls = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device) if lse else None
-        a = AttnArgs(_DTYPES[q.dtype], q.shape[1], q.data_ptr(), out.data_ptr(), ls.data_ptr() if lse else None, q.stride(0),
-                     q.stride(1), out.stride(0), out.stride(1), 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale),
-                     int(window))
-        nb = C.c_size_t()
-        _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
-        ws = self._workspace(nb.value, stream) if nb.value else None
-        _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
-        _check(mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _ptr(ws), nb, _stream(stream)),
-               "mf_kv4_attention")
-        return (out, ls) if lse else out
+        _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
+        heads = q.shape[1]
+        q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
+        out = q.new_empty(q.shape) if out is None else _into(out, "out", q.shape, q.dtype, self.device)
+        ls = torch.empty((batch.rows, heads), dtype=torch.float32, device=self.device) if lse else None
+        a = AttnArgs(_DTYPES[q.dtype], heads, q.data_ptr(), out.data_ptr(), None if ls is None else ls.data_ptr(), *q.stride()[:2],
+                     *out.stride()[:2], 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(window))
+        need = batch._ws_bytes.get((heads, a.window))
+        if need is None:
+            nb = C.c_size_t()
+            _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
+            need = batch._ws_bytes[(heads, a.window)] = nb.value
+        ws = self._workspace(need, stream).data_ptr() if need else None
+        if stream is not None:
+            _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
+        s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws, need, _stream_of(self.device, stream))
+        if s:
+            _check(s, "mf_kv4_attention")
+        return out if ls is None else (out, ls)
