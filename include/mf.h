@@ -430,13 +430,17 @@ typedef struct {
     const void *d_x;        /* [rows][K], row stride x_stride >= K */
     const void *d_bias;     /* [N] or NULL */
     void *d_y;              /* [rows][N], row stride y_stride >= N */
-    int64_t rows;           /* 0 (nothing is done) .. 2^24 */
+    int64_t rows;           /* 0 (nothing is done) .. 2^20 */
     int64_t x_stride, y_stride;
 } mf_w4_args;
 
+/* Bytes of workspace (possibly 0), a function of the sizes, not of pointers. */
+mf_status mf_w4_workspace_size(const mf_w4_args *args, size_t *bytes);
+
 /* Any number of rows; made for the few (up to 64) of a decode step, which read
- * the weights once.  Deterministic. */
-mf_status mf_w4_matmul(const mf_w4_args *args, void *stream);
+ * the weights once.  Deterministic.  d_ws: mf_w4_workspace_size bytes, 256-byte
+ * aligned; need not be initialised. */
+mf_status mf_w4_matmul(const mf_w4_args *args, void *d_ws, size_t ws_bytes, void *stream);
 
 /* --- the paged cache in 4 bits
  *

@@ -39,7 +39,19 @@ struct W4PackArgs {
     bool f16;
 };
 hipError_t launch_w4_pack(const W4PackArgs &a, hipStream_t s);
-hipError_t launch_w4(const W4Args &a, int group, bool f16, hipStream_t s);
+enum W4Form {
+    kW4One16, kW4One8, kW4Four4,        // up to 16 rows: tiles of outputs, waves of a workgroup
+    kW4Two8,                            // up to 32 rows, one tile of outputs, 8 waves
+    kW4Rows32, kW4Rows64, kW4Rows64x2   // by rows: 32 or 64 of them, one or two tiles of outputs a wave
+};
+// How the work is laid over the card: a function of the sizes alone.
+struct W4Plan {
+    W4Form form;
+    int splits;       // by rows: parts of the inputs that different workgroups take
+    size_t ws_bytes;  // their sums
+};
+W4Plan w4_plan(int rows, int n_out, int n_in);
+hipError_t launch_w4(const W4Args &a, const W4Plan &p, int group, bool f16, float *part, hipStream_t s);
 
 // ------------------------------------------------------------- 4-bit cache
 // A page holds, per head and per block of 16 tokens, one record (rec bytes):

@@ -48,6 +48,16 @@ mf_status check_w4(const mf_w4_desc *d)
     return MF_OK;
 }
 
+mf_status check_w4_rows(const mf_w4_args *a)
+{
+    const mf_status st = check_w4(&a->w);
+    if (st != MF_OK) return st;
+    if (a->rows < 0) return MF_EINVAL;
+    // blocks of 32 rows are a grid's third dimension, rows times outputs a grid's first
+    if (a->rows > (1 << 20) || a->rows * (a->w.n_out / 4 + 1) > INT32_MAX * (int64_t)256) return MF_EUNSUPPORTED;
+    return MF_OK;
+}
+
 size_t w4_bytes(const mf_w4_desc &d)
 {
     return (size_t)((d.n_out + kW4Tile - 1) / kW4Tile) * (size_t)((d.n_in + kW4Chunk - 1) / kW4Chunk) * w4_record(d.group);
@@ -156,14 +166,20 @@ mf_status mf_w4_pack(const mf_w4_desc *desc, const uint8_t *d_codes, const void 
     return of(launch_w4_pack(a, (hipStream_t)stream));
 }
 
-mf_status mf_w4_matmul(const mf_w4_args *args, void *stream)
+mf_status mf_w4_workspace_size(const mf_w4_args *args, size_t *bytes)
+{
+    if (!args || !bytes) return MF_EINVAL;
+    const mf_status st = check_w4_rows(args);
+    if (st == MF_OK) *bytes = args->rows > 0 ? w4_plan((int)args->rows, (int)args->w.n_out, (int)args->w.n_in).ws_bytes : 0;
+    return st;
+}
+
+mf_status mf_w4_matmul(const mf_w4_args *args, void *d_ws, size_t ws_bytes, void *stream)
 {
     if (!args) return MF_EINVAL;
-    const mf_status st = check_w4(&args->w);
+    const mf_status st = check_w4_rows(args);
     if (st != MF_OK) return st;
     const mf_w4_desc &w = args->w;
-    if (args->rows < 0) return MF_EINVAL;
-    if (args->rows > (1 << 24)) return MF_EUNSUPPORTED;
     if (args->rows == 0) return MF_OK;
     if (!args->d_packed || !aligned(args->d_packed, 256) || !args->d_x || !args->d_y || !aligned(args->d_x, 2) ||
         !aligned(args->d_y, 2) || !aligned(args->d_bias, 2))
@@ -181,7 +197,10 @@ mf_status mf_w4_matmul(const mf_w4_args *args, void *stream)
     a.rows = (int)args->rows;
     a.n_out = (int)w.n_out;
     a.n_in = (int)w.n_in;
-    return of(launch_w4(a, w.group, as_int(w.dtype) == MF_F16, (hipStream_t)stream));
+    const W4Plan p = w4_plan(a.rows, a.n_out, a.n_in);
+    if (p.ws_bytes > 0 && (ws_bytes < p.ws_bytes || !d_ws)) return MF_ENOMEM;
+    if (p.ws_bytes > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
+    return of(launch_w4(a, p, w.group, as_int(w.dtype) == MF_F16, (float *)d_ws, (hipStream_t)stream));
 }
 
 mf_status mf_kv4_cache_bytes(const mf_kv4_cache *cache, size_t *bytes)

@@ -76,8 +76,9 @@ __device__ __forceinline__ CodeBits code_bits()
 template <bool F16, int S>
 __device__ __forceinline__ uint32_t codes2(uint32_t w, const CodeBits &b)
 {
-    if (F16) return ((S < 2 ? w << (6 - 4 * S) : w >> (4 * S - 6)) & b.mask) | b.sixteen;
-    return ((S < 1 ? w << 3 : w >> (4 * S - 3)) & b.mask) | b.sixteen;
+    constexpr int left = (F16 ? 6 : 3) - 4 * S;   // to bits 6.. or 3.. of each half
+    const uint32_t v = left >= 0 ? w << (left & 31) : w >> (-left & 31);
+    return (v & b.mask) | b.sixteen;
 }
 template <bool F16>
 __device__ __forceinline__ u32x4 codes8(uint32_t w, const CodeBits &b)
@@ -101,6 +102,10 @@ __device__ __forceinline__ u32x4 ones8()
 }
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+// A barrier for what went through LDS.  __syncthreads() also waits for every load
+// from memory that is on its way, which is the end of fetching ahead.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Over the four lanes l, l ^ 16, l ^ 32, l ^ 48 (the contraction index of an operand).
 __device__ __forceinline__ float quarters_max(float x)

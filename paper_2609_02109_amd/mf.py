@@ -33,7 +33,7 @@ EXPORTS = ["mf_problem_bytes", "mf_problem_create", "mf_problem_destroy", "mf_sp
            "mf_workspace_size", "mf_search", "mf_search_noalloc", "mf_eval_fast", "mf_eval_canonical",
            "mf_static_workspace_size", "mf_search_static", "mf_eval_static",
            "mf_ga_workspace_size", "mf_ga_run",
-           "mf_w4_pack_bytes", "mf_w4_pack", "mf_w4_matmul", "mf_kv4_cache_bytes", "mf_kv4_append", "mf_kv4_read",
+           "mf_w4_pack_bytes", "mf_w4_pack", "mf_w4_workspace_size", "mf_w4_matmul", "mf_kv4_cache_bytes", "mf_kv4_append", "mf_kv4_read",
            "mf_kv4_workspace_size", "mf_kv4_attention", "mf_status_string"]
 
 
@@ -136,7 +136,8 @@ def _load():
         "mf_ga_run": (S, [P, P, P, C.c_size_t, P, P, P, P]),
         "mf_w4_pack_bytes": (S, [P, P]),
         "mf_w4_pack": (S, [P, P, P, P, P, C.c_size_t, P]),
-        "mf_w4_matmul": (S, [P, P]),
+        "mf_w4_workspace_size": (S, [P, P]),
+        "mf_w4_matmul": (S, [P, P, C.c_size_t, P]),
         "mf_kv4_cache_bytes": (S, [P, P]),
         "mf_kv4_append": (S, [P, P, P, P]),
         "mf_kv4_read": (S, [P, P, S, P, P, P]),

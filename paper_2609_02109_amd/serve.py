@@ -71,6 +71,26 @@ def _stream_of(device, stream):
     return torch.cuda.current_stream(device).cuda_stream
 
 
+class _Workspaces:
+    """Device workspaces, one per (thread, stream) and device: calls that overlap must not share one."""
+
+    def __init__(self):
+        self._held, self._lock = {}, threading.Lock()
+
+    def pointer(self, nbytes: int, device, stream):
+        key = (threading.get_ident(), device, _stream_of(device, stream))
+        with self._lock:
+            ws = self._held.get(key)
+            if ws is None or ws.numel() < nbytes:
+                ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+                _keep_for(stream, ws)
+                self._held[key] = ws
+        return ws.data_ptr()
+
+
+_workspaces = _Workspaces()
+
+
 def _require(ok: bool, what: str):
     if not ok:
         raise ValueError(what)
@@ -122,6 +142,7 @@ class W4Weight:
         _check(mf.lib.mf_w4_pack(C.byref(self.desc), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(self.packed),
                                  C.c_size_t(self.packed.numel()), _stream_of(self.device, stream)), "mf_w4_pack")
         self._packed_ptr = self.packed.data_ptr()
+        self._ws_bytes = {}   # by rows
 
     def matmul(self, x, bias=None, out=None, stream=None):
         """x [.., K] @ W.T + bias [N] -> [.., N], in the scales' type."""
@@ -147,7 +168,13 @@ class W4Weight:
                       x.stride(0), y.stride(0))
         if stream is not None:
             _keep_for(stream, x, bias, y, self.packed)
-        s = mf.lib.mf_w4_matmul(C.byref(args), _stream_of(self.device, stream))
+        need = self._ws_bytes.get(m)
+        if need is None:
+            nb = C.c_size_t()
+            _check(mf.lib.mf_w4_workspace_size(C.byref(args), C.byref(nb)), "mf_w4_workspace_size")
+            need = self._ws_bytes[m] = nb.value
+        ws = _workspaces.pointer(need, self.device, stream) if need else None
+        s = mf.lib.mf_w4_matmul(C.byref(args), ws, need, _stream_of(self.device, stream))
         if s:
             _check(s, "mf_w4_matmul")
         return out
@@ -196,9 +223,6 @@ class KV4Cache:
         self.raw.d_pages = self.pages.data_ptr()
         self.n_kv_heads, self.head_dim, self.page_size = int(n_kv_heads), int(head_dim), int(page_size)
         self.bytes_per_token = int(nb.value) // (int(n_pages) * self.page_size)
-        # one workspace per (thread, stream), as a problem's
-        self._ws = {}
-        self._ws_lock = threading.Lock()
 
     def batch(self, q_start, kv_len, page_table, rows, max_new, max_kv) -> KV4Batch:
         """q_start int32 [n_seq + 1], kv_len int32 [n_seq] (tokens of each
@@ -254,16 +278,6 @@ class KV4Cache:
             _check(s, "mf_kv4_read")
         return k, v
 
-    def _workspace(self, nbytes: int, stream):
-        key = (threading.get_ident(), _stream_of(self.device, stream))
-        with self._ws_lock:
-            ws = self._ws.get(key)
-            if ws is None or ws.numel() < nbytes:
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-                _keep_for(stream, ws)
-                self._ws[key] = ws
-        return ws
-
     def attention(self, batch: KV4Batch, q, scale=None, window=0, lse=False, out=None, stream=None):
         """Causal attention of q [rows, n_heads, head_dim] over the cached
         tokens: [rows, n_heads, head_dim], with lse=True also the log of the
@@ -281,7 +295,7 @@ class KV4Cache:
             nb = C.c_size_t()
             _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
             need = batch._ws_bytes[(heads, a.window)] = nb.value
-        ws = self._workspace(need, stream).data_ptr() if need else None
+        ws = _workspaces.pointer(need, self.device, stream) if need else None
         if stream is not None:
             _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
         s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws, need, _stream_of(self.device, stream))
