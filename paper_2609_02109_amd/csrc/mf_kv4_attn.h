@@ -48,30 +48,6 @@ __device__ __forceinline__ Sight sight_of(long long p, int window, int limit)
     return v;
 }
 
-template <int N>
-struct Words {
-    uint32_t w[N];
-};
-template <int N>
-__device__ __forceinline__ Words<N> load_words(const uint8_t *p)
-{
-    Words<N> r;
-    if constexpr (N % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < N / 4; i++) {
-            const u32x4 v = ((const u32x4 *)p)[i];
-#pragma unroll
-            for (int j = 0; j < 4; j++) r.w[4 * i + j] = v[j];
-        }
-    } else {
-        static_assert(N == 2, "8 bytes");
-        const u32x2 v = *(const u32x2 *)p;
-        r.w[0] = v[0];
-        r.w[1] = v[1];
-    }
-    return r;
-}
-
 // What a wave keeps for its rows: lane l's is row l % 16 of each tile.
 constexpr float kNoBase = -1e30f;   // before the first token; finite, so that differences of bases are
 template <int D, int G, int RT>

@@ -36,6 +36,31 @@ __device__ __forceinline__ u32x4 load16(const void *p)
     return v;
 }
 
+// N dwords from an address aligned to 8, to 16 from four on.
+template <int N>
+struct Words {
+    uint32_t w[N];
+};
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const uint8_t *p)
+{
+    Words<N> r;
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; i++) {
+            const u32x4 v = ((const u32x4 *)p)[i];
+#pragma unroll
+            for (int j = 0; j < 4; j++) r.w[4 * i + j] = v[j];
+        }
+    } else {
+        static_assert(N == 2, "8 bytes");
+        const u32x2 v = *(const u32x2 *)p;
+        r.w[0] = v[0];
+        r.w[1] = v[1];
+    }
+    return r;
+}
+
 template <bool F16>
 __device__ __forceinline__ float to_float(uint16_t h)
 {
