@@ -103,10 +103,13 @@ def _rows(t, name, shape, dtype, device):
     return t if t.stride(-1) == 1 else t.contiguous()
 
 
+def _like(t):
+    """A new contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _into(t, name, shape, dtype, device):
-    """An output: a new tensor, or the caller's."""
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+    """An output of the caller's."""
     _require(isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device
              and (t.stride(-1) == 1 or t.shape[-1] <= 1), f"{name}: {tuple(shape)} {dtype} on {device} with a contiguous last dimension is wanted")
     return t
@@ -242,23 +245,27 @@ class KV4Cache:
         _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
         shape = (batch.rows, self.n_kv_heads, self.head_dim)
         k, v = _rows(k, "k", shape, dt, dev), _rows(v, "v", shape, dt, dev)
-        _require((cos is None) == (sin is None), "cos and sin: both or neither are wanted")
-        a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), *k.stride()[:2], *v.stride()[:2])
-        if cos is not None:
+        ks, vs = k.stride(), v.stride()
+        if cos is None:
+            _require(sin is None, "cos and sin: both or neither are wanted")
+            _require(q is None, "q: only turned here, so cos and sin are wanted with it")
+            a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1])
+        else:
+            _require(sin is not None, "cos and sin: both or neither are wanted")
             n_pos, half = cos.shape
             _require(cos.shape == sin.shape and cos.dtype is sin.dtype is torch.float32 and cos.device == sin.device == dev
                      and cos.is_contiguous() and sin.is_contiguous(), f"cos, sin: contiguous float32 [n_pos, rot_dim // 2] on {dev} is wanted")
-            a.d_cos, a.d_sin, a.n_pos, a.rot_dim = cos.data_ptr(), sin.data_ptr(), n_pos, 2 * half
-            a.interleaved = 1 if interleaved else 0
-        if q is not None:
-            _require(cos is not None, "q: only turned here, so cos and sin are wanted with it")
-            _require(q.dim() == 3, "q: [rows, n_heads, head_dim] is wanted")
-            heads = q.shape[1]
-            q = _rows(q, "q", (batch.rows, heads, self.head_dim), dt, dev)
-            q_out = q.new_empty(q.shape) if q_out is None else _into(q_out, "q_out", q.shape, dt, dev)
-            a.n_heads, a.d_q, a.d_q_out = heads, q.data_ptr(), q_out.data_ptr()
-            a.q_stride, a.q_head_stride, _ = q.stride()
-            a.qo_stride, a.qo_head_stride, _ = q_out.stride()
+            turn = (cos.data_ptr(), sin.data_ptr(), n_pos, 2 * half, 1 if interleaved else 0)
+            if q is None:
+                a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], *turn)
+            else:
+                _require(q.dim() == 3, "q: [rows, n_heads, head_dim] is wanted")
+                heads = q.shape[1]
+                q = _rows(q, "q", (batch.rows, heads, self.head_dim), dt, dev)
+                q_out = _like(q) if q_out is None else _into(q_out, "q_out", q.shape, dt, dev)
+                qs, os = q.stride(), q_out.stride()
+                a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], *turn, heads, q.data_ptr(),
+                               q_out.data_ptr(), qs[0], qs[1], os[0], os[1])
         if stream is not None:
             _keep_for(stream, k, v, cos, sin, q, q_out, self.pages, *batch.tensors)
         s = mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream_of(dev, stream))
@@ -269,7 +276,8 @@ class KV4Cache:
     def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
         """(keys, values) [rows, n_kv_heads, head_dim] that the cache holds for the batch's rows."""
         _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
-        k, v = torch.empty((2, batch.rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device).unbind(0)
+        k = torch.empty((batch.rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
         if stream is not None:
             _keep_for(stream, k, v, self.pages, *batch.tensors)
         s = mf.lib.mf_kv4_read(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(),
@@ -286,7 +294,7 @@ class KV4Cache:
         _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
         heads = q.shape[1]
         q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
-        out = q.new_empty(q.shape) if out is None else _into(out, "out", q.shape, q.dtype, self.device)
+        out = _like(q) if out is None else _into(out, "out", q.shape, q.dtype, self.device)
         ls = torch.empty((batch.rows, heads), dtype=torch.float32, device=self.device) if lse else None
         a = AttnArgs(_DTYPES[q.dtype], heads, q.data_ptr(), out.data_ptr(), None if ls is None else ls.data_ptr(), *q.stride()[:2],
                      *out.stride()[:2], 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(window))
