@@ -471,8 +471,10 @@ mf_status mf_kv4_cache_bytes(const mf_kv4_cache *cache, size_t *bytes);
  * A page that is written must belong to one sequence.
  * The kernels read and write nothing outside the buffers whatever the device
  * arrays hold: rows past `rows`, tokens at negative positions or at positions
- * from max_kv on, and tokens whose page number is not in 0..n_pages are left
- * out (not written; read as zeros; invisible to attention). */
+ * from max_kv on, and tokens whose page number is not in 0..n_pages - 1 are left
+ * out (not written; read as zeros; invisible to attention).  Attention does not
+ * write a sequence's rows past its first max_new, and no call writes outputs of
+ * rows that belong to no sequence. */
 typedef struct {
     int32_t n_seq;          /* 0 .. 2^20 */
     int32_t max_new;        /* the largest n_s, >= 0: sizes the launch */

@@ -269,7 +269,8 @@ __device__ __forceinline__ SeqRows seq_rows(const KvBatch &b, const SeqRaw &w)
     r.q0 = w.q0;
     r.limit = max(0, min(w.kv, b.max_kv));
     r.first_p = (long long)w.kv - ((long long)w.q1 - w.q0);
-    r.n = w.q0 < 0 || w.q0 >= b.rows || w.q1 <= w.q0 ? 0 : min(w.q1, b.rows) - w.q0;
+    // max_new: a workgroup's rows and the parts' room are made for it
+    r.n = w.q0 < 0 || w.q0 >= b.rows || w.q1 <= w.q0 ? 0 : min(min(w.q1, b.rows) - w.q0, b.max_new);
     return r;
 }
 

@@ -579,3 +579,20 @@ def test_random_steps(serve):
         print(i, kv, new, heads, per, D, G, c.page, c.dt, flush=True)
         c.fill(rng.randint(1, 4))
         check_attention(c, per, window=rng.choice([0, 0, rng.randint(1, 80)]))
+
+
+@pytest.mark.parametrize("kv", [200, 3000])
+def test_attention_of_more_rows_than_the_batch_says(serve, kv):
+    """A device array that gives a sequence more new tokens than max_new: its rows up to there, nothing past them."""
+    c = Case(serve, [kv, 40], [3, 1], heads=1, D=64, G=32, page=16, dt="bf16", seed=17)
+    c.fill(2)
+    q = torch.randn(4, 1, 64, generator=c.gen).bfloat16()
+    want = c.cache.attention(c.batch(), q.cuda())
+    b = c.batch()
+    b.raw.max_new = 1
+    out = torch.full((4, 1, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    c.cache.attention(b, q.cuda(), out=out)
+    assert (out[1:3] == 7).all()
+    tol = 2 * UNIT["bf16"] * want.float().abs() + 2.0 ** -8 * float(want.float().abs().max())
+    for i in (0, 3):   # other shares of the tokens: rounded elsewhere
+        assert ((out[i].float() - want[i].float()).abs() <= tol[i]).all()
