@@ -72,12 +72,18 @@ def _stream_of(device, stream):
 
 
 class _Workspaces:
-    """Device workspaces, one per (thread, stream) and device: calls that overlap must not share one."""
+    """Device workspaces, one per (thread, stream) and device: calls that overlap must not share one.
+    A call that is captured gets one of its own from the graph's pool: the graph holds its address for good,
+    and a larger one may take the held one's place."""
 
     def __init__(self):
         self._held, self._lock = {}, threading.Lock()
 
-    def pointer(self, nbytes: int, device, stream):
+    def get(self, nbytes: int, device, stream):
+        if torch.cuda.is_current_stream_capturing():
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            _keep_for(stream, ws)
+            return ws
         key = (threading.get_ident(), device, _stream_of(device, stream))
         with self._lock:
             ws = self._held.get(key)
@@ -85,7 +91,7 @@ class _Workspaces:
                 ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
                 _keep_for(stream, ws)
                 self._held[key] = ws
-        return ws.data_ptr()
+        return ws
 
 
 _workspaces = _Workspaces()
@@ -176,8 +182,8 @@ class W4Weight:
             nb = C.c_size_t()
             _check(mf.lib.mf_w4_workspace_size(C.byref(args), C.byref(nb)), "mf_w4_workspace_size")
             need = self._ws_bytes[m] = nb.value
-        ws = _workspaces.pointer(need, self.device, stream) if need else None
-        s = mf.lib.mf_w4_matmul(C.byref(args), ws, need, _stream_of(self.device, stream))
+        ws = _workspaces.get(need, self.device, stream) if need else None
+        s = mf.lib.mf_w4_matmul(C.byref(args), ws.data_ptr() if need else None, need, _stream_of(self.device, stream))
         if s:
             _check(s, "mf_w4_matmul")
         return out
@@ -303,10 +309,10 @@ class KV4Cache:
             nb = C.c_size_t()
             _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
             need = batch._ws_bytes[(heads, a.window)] = nb.value
-        ws = _workspaces.pointer(need, self.device, stream) if need else None
+        ws = _workspaces.get(need, self.device, stream) if need else None
         if stream is not None:
             _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
-        s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws, need, _stream_of(self.device, stream))
+        s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws.data_ptr() if need else None, need, _stream_of(self.device, stream))
         if s:
             _check(s, "mf_kv4_attention")
         return out if ls is None else (out, ls)

@@ -596,3 +596,28 @@ def test_attention_of_more_rows_than_the_batch_says(serve, kv):
     tol = 2 * UNIT["bf16"] * want.float().abs() + 2.0 ** -8 * float(want.float().abs().max())
     for i in (0, 3):   # other shares of the tokens: rounded elsewhere
         assert ((out[i].float() - want[i].float()).abs() <= tol[i]).all()
+
+
+def test_a_graph_keeps_its_workspace(serve):
+    """Attention in parts, captured, replayed after larger calls have taken other workspaces."""
+    c = Case(serve, [3000, 2500], [1, 1], heads=2, D=64, G=32, page=16, dt="bf16", seed=18)
+    c.fill(1)
+    q = torch.randn(2, 4, 64, generator=c.gen).bfloat16().cuda()
+    b = c.batch()
+    want = c.cache.attention(b, q)
+    assert b._ws_bytes[(4, 0)] > 0
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = c.cache.attention(b, q)
+    big = Case(serve, [6000] * 6, [4] * 6, heads=4, D=128, G=64, page=16, dt="bf16", seed=19)
+    big.fill(1)
+    bq = torch.randn(24, 8, 128, generator=c.gen).bfloat16().cuda()
+    bb = big.batch()
+    for i in range(3):
+        big.cache.attention(bb, bq)
+        junk = torch.full((1 << 22,), float("nan"), device="cuda")   # over what was handed back
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+        del junk
