@@ -7,7 +7,7 @@ on hosts without the built library.
 """
 import importlib
 
-__all__ = ["synth", "mf", "serve"]
+__all__ = ["synth", "mf", "serve", "step"]
 
 
 def __getattr__(name):
