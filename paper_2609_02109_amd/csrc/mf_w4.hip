@@ -219,7 +219,8 @@ __global__ __launch_bounds__(NW * 64) void w4_rows_kernel(W4Args a, int splits, 
     const int lane = threadIdx.x & 63, wave = wave_id(), col = lane & 15, qt = lane >> 4;
     const int n_tiles = (a.n_out + kW4Tile - 1) / kW4Tile, chunks = (a.n_in + kW4Chunk - 1) / kW4Chunk;
     const int tile0 = ((int)blockIdx.x * NW + wave) * NT, m0 = (int)blockIdx.z * ROWS;
-    const int c0 = (int)((long long)chunks * blockIdx.y / splits), c1 = (int)((long long)chunks * (blockIdx.y + 1) / splits);
+    const int rounds = (chunks + DEEP - 1) / DEEP;
+    const int c0 = (int)((long long)rounds * blockIdx.y / splits) * DEEP, c1 = min((int)((long long)rounds * (blockIdx.y + 1) / splits) * DEEP, chunks);
     const uint8_t *wp[NT];
 #pragma unroll
     for (int t = 0; t < NT; t++) {
@@ -260,45 +261,51 @@ __global__ __launch_bounds__(NW * 64) void w4_rows_kernel(W4Args a, int splits, 
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     f32x4 acc[MT][NT] = {};
     W4Chunk<G, NT> w[DEEP];
+    // in the order of the loop, so that at its head the compiler counts the same loads from both sides
+    fetch(raw[0], c0);
 #pragma unroll
     for (int d = 0; d < DEEP; d++) {
-        fetch(raw[d], c0 + d);
+        if (d == DEEP - 1) put(raw[0], 0);
+        fetch(raw[(d + 1) % DEEP], c0 + d + 1);
         w[d].load(wp, (long long)min(c0 + d, chunks - 1) * REC, lane);
     }
-    put(raw[0], 0);
-    fetch(raw[0], c0 + DEEP);
     lds_barrier();
     for (int cc = c0; cc < c1; cc += DEEP) {
 #pragma unroll
         for (int d = 0; d < DEEP; d++) {
             const int c = cc + d, buf = d & 1;   // DEEP is even
-            if (c >= c1) break;
+            // A round's chunks past the end are fetched and not computed: a way out of the loop from
+            // here has every load awaited at its head (64 x 32768 x 8192, groups of 64: 83 us, so 66).
+            // Groups of 32 do leave it: without, they need more registers than there are.
+            if (G == 32 && c >= c1) break;
             put(raw[(d + 1) % DEEP], buf ^ 1);   // chunk c + 1
             fetch(raw[(d + 1) % DEEP], c + 1 + DEEP);
+            if (G == 32 || c < c1) {
 #pragma unroll
-            for (int g = 0; g < GPC; g++) {
-                u32x4 x[MT][IPG];
-                float X[MT];
+                for (int g = 0; g < GPC; g++) {
+                    u32x4 x[MT][IPG];
+                    float X[MT];
 #pragma unroll
-                for (int m = 0; m < MT; m++) {
-                    X[m] = sums[buf][g][m * 16 + col];
+                    for (int m = 0; m < MT; m++) {
+                        X[m] = sums[buf][g][m * 16 + col];
 #pragma unroll
-                    for (int i = 0; i < IPG; i++) x[m][i] = stage[buf][(m * 16 + col) * 16 + ((4 * (g * IPG + i) + qt) ^ col)];
-                }
-#pragma unroll
-                for (int t = 0; t < NT; t++) {
-                    f32x4 P[MT];
-#pragma unroll
-                    for (int i = 0; i < IPG; i++) {
-                        const u32x4 A = codes8<F16>(w[d].w[t][g * IPG + i], cb);
-#pragma unroll
-                        for (int m = 0; m < MT; m++) P[m] = mfma<F16>(A, x[m][i], i ? P[m] : zero);
+                        for (int i = 0; i < IPG; i++) x[m][i] = stage[buf][(m * 16 + col) * 16 + ((4 * (g * IPG + i) + qt) ^ col)];
                     }
 #pragma unroll
-                    for (int r = 0; r < 4; r++) {
-                        const float s = to_float<F16>((uint16_t)w[d].meta[t][g][r]), z = to_float<F16>((uint16_t)(w[d].meta[t][g][r] >> 16));
+                    for (int t = 0; t < NT; t++) {
+                        f32x4 P[MT];
 #pragma unroll
-                        for (int m = 0; m < MT; m++) acc[m][t][r] = fmaf(s, fmaf(-z, X[m], P[m][r]), acc[m][t][r]);
+                        for (int i = 0; i < IPG; i++) {
+                            const u32x4 A = codes8<F16>(w[d].w[t][g * IPG + i], cb);
+#pragma unroll
+                            for (int m = 0; m < MT; m++) P[m] = mfma<F16>(A, x[m][i], i ? P[m] : zero);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            const float s = to_float<F16>((uint16_t)w[d].meta[t][g][r]), z = to_float<F16>((uint16_t)(w[d].meta[t][g][r] >> 16));
+#pragma unroll
+                            for (int m = 0; m < MT; m++) acc[m][t][r] = fmaf(s, fmaf(-z, X[m], P[m][r]), acc[m][t][r]);
+                        }
                     }
                 }
             }
@@ -358,8 +365,8 @@ hipError_t go_rows(const W4Args &a, const W4Plan &p, float *part, hipStream_t s)
 template <bool F16, int G>
 hipError_t pick(const W4Args &a, const W4Plan &p, float *part, hipStream_t s)
 {
-    // registers of two waves a SIMD
-    constexpr int DEEP = 4, DEEP2 = G == 32 ? 2 : 4;
+    // what the registers of two waves a SIMD hold
+    constexpr int DEEP = 4, DEEP2 = G == 128 ? 4 : 2;
     switch (p.form) {
         case kW4One16: return go_few<F16, G, 1, 1, 16>(a, s);
         case kW4One8: return go_few<F16, G, 1, 1, 8>(a, s);
@@ -390,7 +397,7 @@ hipError_t launch_w4_pack(const W4PackArgs &a, hipStream_t s)
 // * up to 32 rows of small layers the same with two tiles of rows (32 x 1024 x 4096: 5.9,
 //   by rows 9.2; 32 x 8192 x 8192: 22 and 18).
 // * otherwise by rows, two tiles of outputs a wave where that leaves workgroups enough (64 x
-//   32768 x 8192: 58, one 66; 512 x 8192 x 8192: 84, one 108; 64 x 4096 x 4096: 16, two 20), the inputs in as many parts as give every
+//   32768 x 8192: 57, one 66; 512 x 8192 x 8192: 84, one 108; 64 x 4096 x 4096: 16, two 20), the inputs in as many parts as give every
 //   compute unit a workgroup (32 x 8192 x 8192 in 4: 18, whole 40).
 W4Plan w4_plan(int rows, int n_out, int n_in)
 {
