@@ -102,7 +102,10 @@ __device__ __forceinline__ void quantise(float v[D / 32][8], uint32_t code[D / 3
         lo = quarters_min(lo);
         hi = quarters_max(hi);
         bad = quarters_max(bad);
-        _Float16 scale = (_Float16)((hi - lo) * (float)(1.0 / 15.0)), off = (_Float16)lo;
+        // two roundings, as the definition has it: left to itself the compiler makes one of them (v_fma_mixlo_f16)
+        float step = (hi - lo) * (float)(1.0 / 15.0);
+        asm("" : "+v"(step));
+        const _Float16 scale = (_Float16)step, off = (_Float16)lo;
         const float s = (float)scale, o = (float)off, inv = s > 0.f ? 1.f / s : 0.f;
 #pragma unroll
         for (int i = g * IPG; i < (g + 1) * IPG; i++)

@@ -621,3 +621,22 @@ def test_a_graph_keeps_its_workspace(serve):
         torch.cuda.synchronize()
         assert torch.equal(out, want), i
         del junk
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+def test_append_rounds_a_scale_twice(serve, dt):
+    """Groups whose (hi - lo) / 15 rounded to fp32 and then to binary16 is not what one rounding gives."""
+    x = 3 * torch.randn(2, 1 << 22, generator=_gen(20)).to(DT[dt]).float()
+    lo, hi = torch.minimum(x[0], x[1]).numpy(), torch.maximum(x[0], x[1]).numpy()
+    c = np.float32(1 / 15.0)
+    twice, once = ((hi - lo) * c).astype(np.float16), ((hi - lo).astype(np.float64) * np.float64(c)).astype(np.float16)
+    at = np.flatnonzero(twice != once)
+    assert at.size >= 64
+    lo, hi = (torch.from_numpy(v[at[:64]])[:, None, None] for v in (lo, hi))
+    rows = (lo + (hi - lo) * torch.rand(64, 1, 64, generator=_gen(21))).to(DT[dt])
+    rows = torch.minimum(torch.maximum(rows, lo.to(DT[dt])), hi.to(DT[dt]))
+    rows[..., 0::32], rows[..., 5::32] = lo.to(DT[dt]), hi.to(DT[dt])
+    c = Case(serve, [64], [64], heads=1, D=64, G=32, page=16, dt=dt, seed=22)
+    c.cache.append(c.batch(), rows.cuda(), rows.flip(0).contiguous().cuda())
+    k, v = c.cache.read(c.batch())
+    assert torch.equal(k.cpu(), c.held(rows)) and torch.equal(v.cpu(), c.held(rows.flip(0)))
