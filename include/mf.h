@@ -407,7 +407,10 @@ mf_status mf_ga_run(mf_problem *p, const mf_ga_args *args, void *d_ws, size_t ws
 /* --- products with 4-bit weights
  *
  * y[m][n] = sum_k x[m][k] s[n][k / G] (c[n][k] - z[n][k / G]) + bias[n],
- * c and z in 0..15, summed in fp32 and rounded once. */
+ * c and z in 0..15, summed in fp32 and rounded once.  The zero point is taken out
+ * of a group's sum, not of each code (sum (16 + c) x - (16 + z) sum x): a row of x
+ * with an infinity or a NaN gives NaN wherever it is multiplied, and sums of 31 |x|
+ * over a group have to stay within fp32. */
 typedef struct {
     int64_t n_out, n_in;    /* 1 <= N <= 2^31 - 16, 1 <= K <= 2^24, K a multiple of G */
     int32_t group;          /* G: weights that share a scale, 32, 64 or 128 */
@@ -519,8 +522,9 @@ mf_status mf_kv4_read(const mf_kv4_cache *cache, const mf_kv4_batch *batch, mf_d
  * reads key head h / (n_heads / n_kv_heads).  Row i of a sequence sees the
  * tokens j <= p_i = kv_len - n_s + i, with window > 0 only those > p_i - window;
  * out = sum_j softmax(scale q.k_j) v_j, lse = log sum_j exp(scale q.k_j).  A row
- * that sees no token gives 0 and -inf.  Sums and softmax in fp32; the weights of
- * the values are rounded to bfloat16.  Deterministic. */
+ * that sees no token gives 0 and -inf; a NaN in a token that a row sees makes the
+ * row NaN.  Sums and softmax in fp32; the weights of the values, alone and times
+ * their scales, are rounded to binary16.  Deterministic. */
 typedef struct {
     mf_dtype dtype;         /* MF_BF16 or MF_F16: of q and out */
     int32_t n_heads;        /* a multiple of n_kv_heads, at most 4096 */

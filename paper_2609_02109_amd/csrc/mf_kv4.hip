@@ -277,7 +277,10 @@ __device__ __forceinline__ void turn_queries(const KvAppendArgs &a, const Span &
 }
 
 // Work item: (sequence, 16 positions, head), the numbers past the heads standing for
-// slices of the queries' heads.
+// slices of the queries' heads: few tokens or many, there is a wave for each 16 of a head.
+// Bound by the bytes of rows and queries from some thousand rows on (32768 rows of 32 + 2 x
+// 8 heads of 128: 178 us for 747 MB, 4.2 TB/s, a copy 5.2), below that by one trip to
+// memory after another (a row each of 8 requests: 5.8 us).
 template <bool F16, int D, int G>
 __global__ __launch_bounds__(64) void append_kernel(KvAppendArgs a, int blocks, int slices, int few)
 {
@@ -310,6 +313,9 @@ __device__ __forceinline__ void put8(void *dst, long long at, const float *v)
     }
 }
 
+// Rows back, a wave per 16 positions of a head as in the append; bound by the bytes written
+// (32768 rows of 2 x 8 heads of 128: 49 us for 210 MB, 4.3 TB/s) or by the trip to
+// memory (8 rows: 4.3 us).
 template <int TY, int D, int G>   // TY: mf_dtype of the outputs
 __global__ __launch_bounds__(64) void read_kernel(KvReadArgs a, int blocks)
 {

@@ -8,35 +8,44 @@
 namespace mfs {
 namespace {
 
-// One thread per dword of a record: code dwords first, then scales.
-__global__ void w4_pack_kernel(W4PackArgs a)
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t v)
 {
-    const int chunks = (a.n_in + kW4Chunk - 1) / kW4Chunk, rec = w4_record(a.group), gpc = kW4Chunk / a.group;
-    const uint8_t *codes = a.codes;
+    v &= 0x0f0f0f0fu;
+    v = (v | v >> 4) & 0x00ff00ffu;
+    return (v | v >> 8) & 0xffffu;
+}
+
+// A wave per record: 16 rows of 64 bytes of codes in, 1 KB in a row out, then the scales.
+// Once a weight (134 MB of codes: 87 us; a workgroup a record, by single bytes, 106).
+__global__ __launch_bounds__(256) void w4_pack_kernel(W4PackArgs a)
+{
+    const int tiles = (a.n_out + kW4Tile - 1) / kW4Tile, chunks = (a.n_in + kW4Chunk - 1) / kW4Chunk, rec = w4_record(a.group), gpc = kW4Chunk / a.group;
     const long long row_bytes = a.n_in / 2, groups = a.n_in / a.group;
-    for (long long t = blockIdx.x; t < (long long)((a.n_out + kW4Tile - 1) / kW4Tile) * chunks; t += gridDim.x) {
-        const int tile = (int)(t / chunks), chunk = (int)(t % chunks);
-        uint32_t *out = (uint32_t *)(a.packed + t * rec);
-        for (int e = (int)threadIdx.x; e < rec / 4; e += (int)blockDim.x) {
-            uint32_t w = 0;
-            if (e < kW4Codes / 4) {
-                const int lane = e >> 2, i = e & 3;
-                const int n = tile * kW4Tile + (lane & 15), k = chunk * kW4Chunk + i * 32 + (lane >> 4) * 8;
-                if (n < a.n_out && k < a.n_in) {
-                    const uint8_t *src = codes + (long long)n * row_bytes + k / 2;
-                    for (int j = 0; j < 4; j++) w |= (uint32_t)(src[j] & 15) << (4 * j) | (uint32_t)(src[j] >> 4) << (16 + 4 * j);
-                }
-            } else {
-                const int m = e - kW4Codes / 4;
-                const int n = tile * kW4Tile + (m & 15), g = chunk * gpc + (m >> 4);
-                if (n < a.n_out && g < groups) {
-                    const long long at = (long long)n * groups + g;
-                    const float z = 16.f + (float)(a.zeros ? a.zeros[at] & 15 : 8);
-                    w = a.scales[at] | (uint32_t)(a.f16 ? from_float<true>(z) : from_float<false>(z)) << 16;
-                }
+    const int lane = threadIdx.x & 63, chunk = (int)blockIdx.x * 4 + wave_id();
+    if (chunk >= chunks) return;
+    for (int tile = (int)blockIdx.y; tile < tiles; tile += (int)gridDim.y) {
+        uint8_t *out = a.packed + ((long long)tile * chunks + chunk) * rec;
+        const int n = tile * kW4Tile + (lane & 15);
+        u32x4 w = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int k = chunk * kW4Chunk + i * 32 + (lane >> 4) * 8;
+            if (n < a.n_out && k < a.n_in) {
+                uint32_t v;
+                __builtin_memcpy(&v, a.codes + n * row_bytes + k / 2, 4);
+                w[i] = low_nibbles(v) | low_nibbles(v >> 4) << 16;
             }
-            out[e] = w;
         }
+        ((u32x4 *)out)[lane] = w;
+        if (lane >= 16 * gpc) continue;
+        const int g = chunk * gpc + (lane >> 4);
+        uint32_t m = 0;
+        if (n < a.n_out && g < groups) {
+            const long long at = n * groups + g;
+            const float z = 16.f + (float)(a.zeros ? a.zeros[at] & 15 : 8);
+            m = a.scales[at] | (uint32_t)(a.f16 ? from_float<true>(z) : from_float<false>(z)) << 16;
+        }
+        ((uint32_t *)(out + kW4Codes))[lane] = m;
     }
 }
 
@@ -72,6 +81,9 @@ struct W4Chunk {
     }
 };
 
+// Few rows (bound by the weights' bytes: 8 rows of 32768 x 8192 in groups of 128 take 30 us
+// for 140 MB, 4.7 TB/s; small layers by the trip to memory and the sum through LDS: 1 x 4096
+// x 4096 4.5 us).
 // A workgroup takes NT tiles of 16 outputs and MT tiles of 16 rows; its NW waves
 // take every NW-th chunk of 128 inputs, the next chunk on its way while one is
 // computed, and add up through LDS at the end, in wave order.  The operand of the
@@ -203,7 +215,11 @@ __device__ __forceinline__ float dpp(float x)
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
-// Many rows: all NW waves of a workgroup take the same chunk, for NT tiles of 16
+// Many rows (bound by the issue of two waves a SIMD: at 64 x 32768 x 8192, 48 us, vector
+// instructions take 46 % of the cycles, matrix ones 30 %, and little of the two runs at
+// once; the codes' conversion and scale and zero point are most of the first.  Four chunks
+// in LDS for one barrier took as long: 57 us, at 512 rows 87 for 82).
+// All NW waves of a workgroup take the same chunk, for NT tiles of 16
 // outputs each, so that the rows come from memory once for 16 NW NT outputs.  A
 // chunk of MT x 16 rows goes into LDS (pieces as above) with its groups' sums
 // while the one before is computed; rows and weights are DEEP chunks ahead in
@@ -327,7 +343,7 @@ __global__ __launch_bounds__(NW * 64) void w4_rows_kernel(W4Args a, int splits, 
     }
 }
 
-// Adds the parts up, in order.
+// Adds the parts up, in order (bytes: 17 MB for 64 x 32768 in 2 parts, 4.5 us).
 template <bool F16>
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Args a, int splits, const float *part)
 {
@@ -383,9 +399,8 @@ hipError_t pick(const W4Args &a, const W4Plan &p, float *part, hipStream_t s)
 
 hipError_t launch_w4_pack(const W4PackArgs &a, hipStream_t s)
 {
-    const long long recs = (long long)((a.n_out + kW4Tile - 1) / kW4Tile) * ((a.n_in + kW4Chunk - 1) / kW4Chunk);
-    const unsigned grid = (unsigned)(recs < 65536 ? recs : 65536);
-    hipLaunchKernelGGL(w4_pack_kernel, dim3(grid), dim3(256), 0, s, a);
+    const unsigned tiles = (unsigned)((a.n_out + kW4Tile - 1) / kW4Tile), chunks = (unsigned)((a.n_in + kW4Chunk - 1) / kW4Chunk);
+    hipLaunchKernelGGL(w4_pack_kernel, dim3((chunks + 3) / 4, tiles < 16384 ? tiles : 16384), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -11,10 +11,11 @@ result's type (2^-8 bfloat16, 2^-11 binary16):
 * append: codes are equal to the definition's in fp32, step for step, so the
   values read back are equal bit for bit; turned queries are two products and a
   sum in fp32, rounded once: u |y| plus 3 2^-24 (|a| + |b|).
-* attention: the weights times the scales are rounded to bfloat16 (2^-9 of
-  each, against code distances of at most 7.5 scales), so an element is within
-  u |o| plus 2^-9 sum_t p_t 7.5 scale_t, plus 2^-9-free fp32 terms that 1e-4 of
-  the largest value covers; lse: 1e-4 (fp32 products over D <= 256).
+* attention: the weights, alone and times the scales, are rounded to 16 bits
+  (2^-11 of each in binary16; 2^-9, bfloat16's, against code distances of at most
+  7.5 scales is asked for), so an element is within u |o| plus 2^-9 sum_t p_t 7.5
+  scale_t, plus fp32 terms that 1e-4 of the largest value covers; lse: 1e-4 (fp32
+  products over D <= 256).
 """
 import math
 import random
