@@ -432,7 +432,7 @@ typedef struct {
     const void *d_packed;   /* as mf_w4_pack wrote it */
     const void *d_x;        /* [rows][K], row stride x_stride >= K */
     const void *d_bias;     /* [N] or NULL */
-    void *d_y;              /* [rows][N], row stride y_stride >= N */
+    void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x */
     int64_t rows;           /* 0 (nothing is done) .. 2^20 */
     int64_t x_stride, y_stride;
 } mf_w4_args;

@@ -164,9 +164,9 @@ class W4Weight:
                      and bias.is_contiguous(), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
         if len(lead) != 1:
             x = x.reshape(-1, self.n_in)
-        if x.stride(1) != 1:
-            x = x.contiguous()
         m = x.shape[0]
+        if x.stride(1) != 1 or (m > 1 and x.stride(0) < self.n_in):
+            x = x.contiguous()
         if out is None:
             y = x.new_empty((m, self.n_out))
             out = y if len(lead) == 1 else y.view(*lead, self.n_out)
@@ -211,7 +211,7 @@ class KV4Batch:
         _require(page_table.dim() == 2 and page_table.shape[0] == n and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
                  "page_table: [n_seq, pages] with a contiguous last dimension is wanted")
         self.tensors = (q_start, kv_len, page_table)
-        self._ws_bytes = {}   # of attention, by (query heads, window): a function of the sizes
+        self._ws_bytes = {}   # of attention, by query heads, window and the cache's shape: a function of the sizes
         self.rows = int(rows)
         self.raw = Batch(n, int(max_new), int(max_kv), self.rows, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                          page_table.stride(0), int(page_table.shape[1]))
@@ -231,6 +231,7 @@ class KV4Cache:
         self.device = self.pages.device
         self.raw.d_pages = self.pages.data_ptr()
         self.n_kv_heads, self.head_dim, self.page_size = int(n_kv_heads), int(head_dim), int(page_size)
+        self._shape = (self.n_kv_heads, self.head_dim, int(group), self.page_size)
         self.bytes_per_token = int(nb.value) // (int(n_pages) * self.page_size)
 
     def batch(self, q_start, kv_len, page_table, rows, max_new, max_kv) -> KV4Batch:
@@ -304,11 +305,12 @@ class KV4Cache:
         ls = torch.empty((batch.rows, heads), dtype=torch.float32, device=self.device) if lse else None
         a = AttnArgs(_DTYPES[q.dtype], heads, q.data_ptr(), out.data_ptr(), None if ls is None else ls.data_ptr(), *q.stride()[:2],
                      *out.stride()[:2], 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(window))
-        need = batch._ws_bytes.get((heads, a.window))
+        key = (heads, a.window, self._shape)
+        need = batch._ws_bytes.get(key)
         if need is None:
             nb = C.c_size_t()
             _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
-            need = batch._ws_bytes[(heads, a.window)] = nb.value
+            need = batch._ws_bytes[key] = nb.value
         ws = _workspaces.get(need, self.device, stream) if need else None
         if stream is not None:
             _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
