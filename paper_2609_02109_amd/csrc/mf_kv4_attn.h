@@ -559,8 +559,8 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
     }
 }
 
-// By rows (many query tokens; bound by vector instructions, 73 % of the SIMDs' cycles
-// beside 33 % of matrix ones: 2 x 1024 query tokens of 32 heads over 12345 tokens take 567 us,
+// By rows (many query tokens; bound by vector instructions, 70 % of the SIMDs' cycles
+// beside 32 % of matrix ones: 2 x 1024 query tokens of 32 heads over 12345 tokens take 567 us,
 // 693 TFLOP/s; a third tile of rows a wave would share the codes' work further and has no
 // registers): a workgroup takes a tile of attn_rows rows, its
 // waves 16 RT of them each, over a part of their tokens.

@@ -216,7 +216,7 @@ __device__ __forceinline__ float dpp(float x)
 }
 
 // Many rows (bound by the issue of two waves a SIMD: at 64 x 32768 x 8192, 48 us, vector
-// instructions take 46 % of the cycles, matrix ones 30 %, and little of the two runs at
+// instructions take 43 % of the cycles, matrix ones 27 %, and little of the two runs at
 // once; the codes' conversion and scale and zero point are most of the first.  Four chunks
 // in LDS for one barrier took as long: 57 us, at 512 rows 87 for 82).
 // All NW waves of a workgroup take the same chunk, for NT tiles of 16

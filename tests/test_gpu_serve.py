@@ -660,3 +660,16 @@ def test_w4_rows_that_repeat(serve):
     W = serve.W4Weight(codes.cuda(), scales.cuda(), z.cuda())
     x = torch.randn(1, 128, generator=_gen(25)).half().cuda()
     assert torch.equal(W.matmul(x.expand(5, 128)), W.matmul(x.repeat(5, 1)))
+
+
+@pytest.mark.parametrize("m,n,k,g", [
+    (33, 300, 2688, 32), (40, 200, 2880, 64), (64, 500, 4736, 128), (24, 8200, 2944, 128), (20, 8200, 2080, 32),   # parts, rounds that end early
+    (130, 5500, 1184, 32), (130, 5500, 1216, 64), (130, 5500, 1408, 128), (70, 8250, 544, 32), (70, 8250, 640, 64)])   # two tiles a wave
+def test_w4_by_rows(serve, m, n, k, g):
+    dt = "f16" if k % 3 else "bf16"
+    codes, scales, z, w = _weights(n, k, g, DT[dt], True, m + n + k)
+    x = torch.randn(m, k, generator=_gen(26)).to(DT[dt])
+    W = serve.W4Weight(codes.cuda(), scales.cuda(), z.cuda())
+    y = W.matmul(x.cuda())
+    _check_w4(y, x, w, scales, g, None, dt)
+    assert torch.equal(y, W.matmul(x.cuda()))
