@@ -22,8 +22,7 @@
 // and when one reaches 2^14, so that w could leave binary16's range, the base goes
 // to the largest score so far (in powers of two) less 10 and the step's weights
 // are computed again.  Binary16 then holds weights down to 2^-34 of the largest,
-// and the small weights of long contexts are not lost.  Steps with scales of 2
-// and above, which are rare, bound w by its own size.
+// and the small weights of long contexts are not lost.
 #pragma once
 
 #include "mf_serve_dev.h"
@@ -112,6 +111,33 @@ __device__ __forceinline__ bool sees(const Sight &v, int ok, int t0, int qt, int
     return (ok >> (e >> 2) & 1) && tok >= v.lo && tok <= v.hi;
 }
 
+// Of tokens 2 e, 2 e + 1 of the lane's, the halves that a row sees.
+__device__ __forceinline__ uint32_t seen_pair(const Sight &v, int ok, int t0, int qt, int e)
+{
+    return (sees(v, ok, t0, qt, 2 * e) ? 0xffffu : 0u) | (sees(v, ok, t0, qt, 2 * e + 1) ? 0xffff0000u : 0u);
+}
+
+// The largest of a row's eight numbers a lane, as whole numbers of 16 bits.
+__device__ __forceinline__ uint32_t largest(u32x4 v)
+{
+    const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(bits<u16x2>(v[0]), bits<u16x2>(v[1])),
+                                              __builtin_elementwise_max(bits<u16x2>(v[2]), bits<u16x2>(v[3])));
+    return (uint32_t)quarters_max((float)max(m[0], m[1]));
+}
+
+// The power of two that a row's scales of a group (scales: of the tokens that it sees, others 0) are taken times, so that
+// they and their products with the weights w stay below 2^15; 0 unless it sees a scale of 2 and above.
+__device__ __forceinline__ int unit_of(u32x4 scales, u32x4 w)
+{
+    u32x4 products;
+#pragma unroll
+    for (int e = 0; e < 4; e++) products[e] = bits<uint32_t>(bits<f16x2>(w[e]) * bits<f16x2>(scales[e]));
+    const int scale = (int)(largest(scales) >> 10) - 15, weight = (int)(largest(w) >> 10) - 15, product = (int)(largest(products) >> 10) - 15;
+    if (scale < 1) return 0;
+    // past binary16's range a product is at most its largest factors'
+    return min(14 - scale, 14 - (product < 16 ? product : scale + weight + 1));
+}
+
 // keys_done, values_done: called where the step has no more use for its keys and its values, to
 // fetch the next step's into their place.  full: every row sees every token; limit: tokens from it on were never written; c: softmax scale times log2 e (and the row's power of two).
 template <bool F16, int D, int G, int RT, class FK, class FV>
@@ -159,25 +185,11 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
             for (int e = 0; e < 8; e++)
                 if (!sees(see[t], ok, t0, qt, e)) p[t][e >> 2][e & 3] = -INFINITY;
     }
-    // weights are to stay below 2^top: 2^14, less where scales are 2 (bit 14) and above
-    uint32_t any = 0;
-#pragma unroll
-    for (int g = 0; g < NG; g++) any |= x.vs[0].w[2 * g] | x.vs[0].w[2 * g + 1] | x.vs[1].w[2 * g] | x.vs[1].w[2 * g + 1];
-    int top = 14;
-    if (__any(any & 0x40004000u)) {
-        float v = 1.f;
-#pragma unroll
-        for (int g = 0; g < NG; g++)
-#pragma unroll
-            for (int e = 0; e < 8; e++) v = fmaxf(v, half_of(x.vs[e >> 2].w[2 * g + ((e >> 1) & 1)], e & 1));
-        v = fminf(quarters_max(v), 65504.f);
-        top = uniform(14 - (int)((__float_as_uint(v) >> 23) - 127u));
-    }
     u32x4 w[RT];
     float e[RT][8];
     for (bool raised = false;; raised = true) {   // twice at most
         int highest[RT], over = 0;
-        const int most = (15 + top) << 10;   // 2^top in binary16
+        constexpr int most = (15 + 14) << 10;   // 2^14 in binary16
 #pragma unroll
         for (int t = 0; t < RT; t++) {
 #pragma unroll
@@ -198,7 +210,7 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
             float mx = p[t][0][0];
 #pragma unroll
             for (int i = 1; i < 8; i++) mx = fmaxf(mx, p[t][i >> 2][i & 3]);
-            mx = fmaf(quarters_max(mx), c[t], 4.f - (float)top);
+            mx = fmaf(quarters_max(mx), c[t], -10.f);
             const float base = hit ? fmaxf(mx, st.base[t]) : st.base[t], a = __builtin_amdgcn_exp2f(st.base[t] - base);
             st.base[t] = base;
             st.l[t] *= a;
@@ -223,19 +235,43 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
     }
 #pragma unroll
     for (int t = 0; t < RT; t++) st.om[t] = mfma<true>(vo, w[t], st.om[t]);
+    // Scales of 2 (bit 14) and above, which are rare, may take w out of binary16's range.  Where a row sees one, the
+    // group's scales of this step and the sums that the products go into are taken 2^up times, and the sums back: per
+    // row, and of the scales that the row sees, so that no row's result depends on anything else.
+    uint32_t any = 0;
+#pragma unroll
+    for (int g = 0; g < NG; g++) any |= x.vs[0].w[2 * g] | x.vs[0].w[2 * g + 1] | x.vs[1].w[2 * g] | x.vs[1].w[2 * g + 1];
+    const bool odd = __any(any & 0x40004000u);
 #pragma unroll
     for (int g = 0; g < NG; g++) {
         u32x4 wg[RT];
+        int up[RT];
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
             for (int e = 0; e < 4; e++) wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(x.vs[e >> 1].w[2 * g + (e & 1)]));
+        if (odd) {
+#pragma unroll
+            for (int t = 0; t < RT; t++) {
+                u32x4 scales;
+#pragma unroll
+                for (int e = 0; e < 4; e++) scales[e] = x.vs[e >> 1].w[2 * g + (e & 1)] & (full ? ~0u : seen_pair(see[t], ok, t0, qt, e));
+                up[t] = unit_of(scales, w[t]);
+                const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.f, up[t]);
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * (bits<f16x2>(scales[e]) * (f16x2){f, f}));
+#pragma unroll
+                for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], up[t]);
+            }
+        }
         if (!full) {   // nor do scales of tokens that the row does not see
 #pragma unroll
             for (int t = 0; t < RT; t++)
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    wg[t][e] &= (sees(see[t], ok, t0, qt, 2 * e) ? 0xffffu : 0u) | (sees(see[t], ok, t0, qt, 2 * e + 1) ? 0xffff0000u : 0u);
+                for (int e = 0; e < 4; e++) wg[t][e] &= seen_pair(see[t], ok, t0, qt, e);
         }
 #pragma unroll
         for (int i = g * IPG; i < (g + 1) * IPG; i++) {
@@ -246,6 +282,14 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
                 st.o[t][2 * i] = mfma<true>(lo, wg[t], st.o[t][2 * i]);
                 st.o[t][2 * i + 1] = mfma<true>(hi, wg[t], st.o[t][2 * i + 1]);
             }
+        }
+        if (odd) {
+#pragma unroll
+            for (int t = 0; t < RT; t++)
+#pragma unroll
+                for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
+#pragma unroll
+                    for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], -up[t]);
         }
     }
     values_done();

@@ -1,0 +1,101 @@
+"""The served steps' operators where what they hold is unusual: pages with
+leftovers of other requests, values of all sizes, batches of many sequences, and
+calls on other streams.
+
+Tolerances, derived before the first run, with u the rounding unit of the result's
+type (2^-8 bfloat16, 2^-11 binary16):
+* attention: a softmax weight and its product with a token's scale are each rounded
+  to binary16, 2^-11 of them, so an element is within
+    u |o| + 2^-11 sum_t p_t (|v_t| + scale_t code_t) <= u |o| + 2^-10 sum_t p_t (|v_t| + |off_t|),
+  plus 2^-13 sum_t p_t |v_t| for fp32 scores (2^-22 of products that sum to some
+  hundred), and half of binary16's smallest step, 2^-25, where it is the result's type.
+* products: with the codes 16 + c and the zero points 16 + z (at most 31) a group is two
+  sums of at most 128 products, by matrix instructions of 32: five levels of sums and one
+  onto the last, four times, and the group's own two operations, so at most 32 roundings of
+  2^-24 (2^-23 where an instruction cuts off) each stand above any product:
+  u |y| + 2^-18 31 sum |x| s, and 64 more of the sum so far, 2^-18 of max |sum| <= sum |x s (c - z)|.
+"""
+import math
+
+import pytest
+import torch
+
+from test_gpu_serve import DT, SHAPES, UNIT, Case, _gen, _weights, plain_attention, serve  # noqa: F401  (the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def _parts(x, G):
+    """What a row stands for in the cache and the size of its offset, [.., D] each, in fp32 step by step."""
+    y = x.float().clamp(-65504, 65504).unflatten(-1, (-1, G))
+    lo, hi = y.amin(-1, keepdim=True), y.amax(-1, keepdim=True)
+    s = ((hi - lo) * torch.tensor(1 / 15.0, dtype=torch.float32)).half().float()
+    o = lo.half().float()
+    c = ((y - o) * torch.where(s > 0, 1.0 / s, torch.zeros_like(s))).round().clamp(0, 15)
+    return (o + s * c).flatten(-2).double(), o.abs().expand(*y.shape).flatten(-2).double()
+
+
+def check(c, per, q, got, lse=None, window=0, scale=None, kv=None, new=None):
+    """got [rows, heads, D] against 64 bits, at the tolerance above."""
+    kv, new = c.kv if kv is None else kv, c.new if new is None else new
+    scale, at = 1 / math.sqrt(c.D) if scale is None else scale, 0
+    for i, n in enumerate(new):
+        if n and kv[i]:
+            k, _ = _parts(c.k[i][: kv[i]], c.G)
+            v, off = _parts(c.v[i][: kv[i]], c.G)
+            o, l, p = plain_attention(q[at:at + n], k, v, per, n, window, scale)
+            for h in range(q.shape[1]):
+                mass, offs = p[:, h] @ v[:, h // per].abs(), p[:, h] @ off[:, h // per]
+                tol = UNIT[c.dt] * o[:, h].abs() + 2.0 ** -10 * (mass + offs) + 2.0 ** -13 * mass + (2.0 ** -25 if c.dt == "f16" else 0) + 1e-30
+                err = (got[at:at + n, h].cpu().double() - o[:, h]).abs()
+                assert (err <= tol).all(), (i, h, float((err / tol).max()))
+            if lse is not None:
+                seen = torch.isfinite(l)
+                assert torch.equal(torch.isfinite(lse[at:at + n].cpu()), seen) and ((lse[at:at + n].cpu().double() - l)[seen].abs() <= 1e-4).all()
+        at += n
+
+
+# ------------------------------------------------------- leftovers in the pages
+
+# what pages hold before anything is written, as binary16: scales from the smallest to the largest, infinities, NaN
+LEFTOVERS = [6e-8, 1e-3, 2.0, 100.0, 65504.0, float("inf"), float("nan")]
+
+
+def _leave(cache, value):
+    cache.pages.view(torch.float16).fill_(value)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("D,G", SHAPES)
+@pytest.mark.parametrize("kv,new,per", [([90, 37, 20, 0], [1, 1, 1, 1], 4), ([90, 37, 21], [20, 7, 3], 2), ([2500, 37], [1, 1], 2), ([150], [60], 3)])
+def test_attention_does_not_depend_on_leftovers(serve, D, G, dt, kv, new, per):
+    """The rest of a sequence's last page, and pages that are none of the cache's: the same bits whatever the memory holds."""
+    c = Case(serve, kv, new, heads=1, D=D, G=G, page=16 if kv[0] < 1000 else 64, dt=dt, seed=31)
+    q = torch.randn(sum(new), per, D, generator=c.gen).to(DT[dt])
+    bad = c.table.clone()
+    bad[0, 1], bad[-1, 0] = -1, c.n_pages
+    want = None
+    for value in [0.0] + LEFTOVERS:
+        _leave(c.cache, value)
+        c.fill(1)
+        got = [*c.cache.attention(c.batch(), q.cuda(), lse=True), *c.cache.attention(c.batch(table=bad), q.cuda(), lse=True)]
+        if want is None:
+            want = got
+            check(c, per, q, *got[:2])
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), value
+
+
+@pytest.mark.parametrize("big", [1e-6, 3e-3, 40.0, 3000.0])
+def test_a_row_does_not_depend_on_later_tokens(serve, big):
+    """Rows of a chunk before a token whose values are of another size: the same bits as without it."""
+    for window in (0, 30):
+        c = Case(serve, [100], [40], heads=1, D=128, G=64, page=32, dt="f16", seed=33)
+        q = torch.randn(40, 2, 128, generator=c.gen).half()
+        c.fill(1)
+        want = c.cache.attention(c.batch(), q.cuda(), window=window)
+        for pos in (71, 75, 90):
+            c.v[0][pos] = (c.v[0][pos].float() * big).half()
+        c.fill(1)
+        got = c.cache.attention(c.batch(), q.cuda(), window=window)
+        check(c, 2, q, got, window=window)
+        assert torch.equal(got[:11], want[:11]) and not torch.equal(got[11:], want[11:])
