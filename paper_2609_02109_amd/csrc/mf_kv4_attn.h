@@ -139,11 +139,12 @@ __device__ __forceinline__ int unit_of(u32x4 scales, u32x4 w)
 }
 
 // keys_done, values_done: called where the step has no more use for its keys and its values, to
-// fetch the next step's into their place.  full: every row sees every token; limit: tokens from it on were never written; c: softmax scale times log2 e (and the row's power of two).
+// fetch the next step's into their place.  full: every row sees every token; all: what any row sees, for the memory
+// of the others may hold anything; c: softmax scale times log2 e (and the row's power of two).
 template <bool F16, int D, int G, int RT, class FK, class FV>
 __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (&q)[RT][D / 32], const u32x2 (&qsum)[RT],
                                           const AttnTokens<D, G> &x, const Sight (&see)[RT],
-                                          bool full, int ok, int limit, int t0, const float (&c)[RT],
+                                          bool full, int ok, const Sight &all, int t0, const float (&c)[RT],
                                           const FK &keys_done, const FV &values_done)
 {
     constexpr int NG = D / G, IPG = G / 32;
@@ -225,12 +226,12 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
         for (int i = 0; i < 8; i++) st.l[t] += e[t][i];
     u32x4 vo = {x.vo[0][0], x.vo[0][1], x.vo[1][0], x.vo[1][1]};
     if (!full) {
-        // what was never written may be anything; a zero weight does not make it zero
+        // what no row sees may be anything, not a number too; a zero weight does not make it zero
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int tok = t0 + 16 * (e >> 1) + 4 * qt + 2 * (e & 1);
             const bool page = ok >> (e >> 1) & 1;
-            vo[e] &= (page && tok < limit ? 0xffffu : 0u) | (page && tok + 1 < limit ? 0xffff0000u : 0u);
+            vo[e] &= (page && tok >= all.lo && tok <= all.hi ? 0xffffu : 0u) | (page && tok + 1 >= all.lo && tok + 1 <= all.hi ? 0xffff0000u : 0u);
         }
     }
 #pragma unroll
@@ -393,6 +394,7 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
         for (int d = 0; d < NS; d++) q[t][d] = load16(x + 32 * d);
     }
     const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
+    const Sight all = {see0.lo, see1.hi};
 
     const int *table = a.b.table + (long long)s * a.b.table_stride;
     constexpr bool ROWS = NW == 0;
@@ -507,10 +509,10 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
         }
         if constexpr (AHEAD) {
             const Step next = step_at(i);   // past the end: records that are none
-            attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, now.ok, limit, t0, c, [&] { keys_of(next); }, [&] { values_of(next); });
+            attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, now.ok, all, t0, c, [&] { keys_of(next); }, [&] { values_of(next); });
             now = next;
         } else {
-            attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, now.ok, limit, t0, c, [] {}, [] {});
+            attn_step<F16, D, G, RT>(st, q, qsum, x, see, full, now.ok, all, t0, c, [] {}, [] {});
             if (t0 + STRIDE < end) {
                 if (i == 32) {
                     find(t0 + STRIDE);

@@ -85,6 +85,23 @@ def test_attention_does_not_depend_on_leftovers(serve, D, G, dt, kv, new, per):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), value
 
 
+@pytest.mark.parametrize("new,per", [(1, 4), (5, 4), (20, 4)])
+def test_attention_in_a_window_over_pages_that_were_given_back(serve, new, per):
+    """Tokens before every row's window need not be there: their pages may be another's by now, or partly written."""
+    c = Case(serve, [300], [new], heads=2, D=64, G=32, page=16, dt="bf16", seed=32)
+    q = torch.randn(new, 2 * per, 64, generator=c.gen).bfloat16()
+    tail = 24 + new - 1   # what the rows see
+    want = None
+    for value in [0.0] + LEFTOVERS:
+        _leave(c.cache, value)
+        c.cache.append(c.batch(new=[tail]), c.k[0][-tail:].cuda(), c.v[0][-tail:].cuda())
+        got = c.cache.attention(c.batch(), q.cuda(), window=24)
+        if want is None:
+            want = got
+            check(c, per, q, got, window=24)
+        assert torch.equal(got, want), value
+
+
 @pytest.mark.parametrize("big", [1e-6, 3e-3, 40.0, 3000.0])
 def test_a_row_does_not_depend_on_later_tokens(serve, big):
     """Rows of a chunk before a token whose values are of another size: the same bits as without it."""
