@@ -22,7 +22,8 @@
 // and when one reaches 2^14, so that w could leave binary16's range, the base goes
 // to the largest score so far (in powers of two) less 10 and the step's weights
 // are computed again.  Binary16 then holds weights down to 2^-34 of the largest,
-// and the small weights of long contexts are not lost.
+// and the small weights of long contexts are not lost; a step's w are brought to
+// the same range by a power of two where scales are not of ordinary size.
 #pragma once
 
 #include "mf_serve_dev.h"
@@ -125,17 +126,25 @@ __device__ __forceinline__ uint32_t largest(u32x4 v)
     return (uint32_t)quarters_max((float)max(m[0], m[1]));
 }
 
-// The power of two that a row's scales of a group (scales: of the tokens that it sees, others 0) are taken times, so that
-// they and their products with the weights w stay below 2^15; 0 unless it sees a scale of 2 and above.
+// Scales of 2^-7 (bit 13) up to 2 (bit 14), and 0, leave the products with the weights well inside binary16's range.
+// Of eight scales a lane, turned by kPlain: above kPlain where one is of another size.
+constexpr uint32_t kPlain = 0x2000;
+__device__ __forceinline__ u16x2 plainness(uint32_t scales) { return bits<u16x2>(scales ^ (kPlain | kPlain << 16)); }
+
+// The power of two that a row's scales of a group (scales: of the tokens that it sees, others 0) are taken times: their
+// products with the weights w, and they, come to the top of binary16's range, below 2^15.  0 where all are plain.
 __device__ __forceinline__ int unit_of(u32x4 scales, u32x4 w)
 {
-    u32x4 products;
+    u32x4 products, turned;
 #pragma unroll
-    for (int e = 0; e < 4; e++) products[e] = bits<uint32_t>(bits<f16x2>(w[e]) * bits<f16x2>(scales[e]));
+    for (int e = 0; e < 4; e++) {
+        products[e] = bits<uint32_t>(bits<f16x2>(w[e]) * bits<f16x2>(scales[e]));
+        turned[e] = bits<uint32_t>(plainness(scales[e]));
+    }
+    const bool plain = largest(turned) <= kPlain;
     const int scale = (int)(largest(scales) >> 10) - 15, weight = (int)(largest(w) >> 10) - 15, product = (int)(largest(products) >> 10) - 15;
-    if (scale < 1) return 0;
-    // past binary16's range a product is at most its largest factors'
-    return min(14 - scale, 14 - (product < 16 ? product : scale + weight + 1));
+    // past binary16's range a product is at most its largest factors'; 2^15 is the largest that the scales are taken times
+    return plain ? 0 : min(min(14 - scale, 15), 14 - (product < 16 ? product : scale + weight + 1));
 }
 
 // keys_done, values_done: called where the step has no more use for its keys and its values, to
@@ -236,17 +245,20 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
     }
 #pragma unroll
     for (int t = 0; t < RT; t++) st.om[t] = mfma<true>(vo, w[t], st.om[t]);
-    // Scales of 2 (bit 14) and above, which are rare, may take w out of binary16's range.  Where a row sees one, the
-    // group's scales of this step and the sums that the products go into are taken 2^up times, and the sums back: per
-    // row, and of the scales that the row sees, so that no row's result depends on anything else.
-    uint32_t any = 0;
+    // Scales of 2 and above may take w out of binary16's range, scales below 2^-7 to its end, where it has few bits or
+    // none; both are rare.  Where a row sees one, the group's scales of this step and the sums that the products go
+    // into are taken 2^up times, and the sums back: per row, and of the scales that the row sees, so that no row's
+    // result depends on anything else.
+    u16x2 turned = {0, 0};
 #pragma unroll
-    for (int g = 0; g < NG; g++) any |= x.vs[0].w[2 * g] | x.vs[0].w[2 * g + 1] | x.vs[1].w[2 * g] | x.vs[1].w[2 * g + 1];
-    const bool odd = __any(any & 0x40004000u);
+    for (int g = 0; g < NG; g++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) turned = __builtin_elementwise_max(turned, plainness(x.vs[e >> 1].w[2 * g + (e & 1)]));
+    const bool odd = __any(max(turned[0], turned[1]) > kPlain);
+    int up[RT][NG];
 #pragma unroll
     for (int g = 0; g < NG; g++) {
         u32x4 wg[RT];
-        int up[RT];
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
@@ -257,15 +269,15 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
                 u32x4 scales;
 #pragma unroll
                 for (int e = 0; e < 4; e++) scales[e] = x.vs[e >> 1].w[2 * g + (e & 1)] & (full ? ~0u : seen_pair(see[t], ok, t0, qt, e));
-                up[t] = unit_of(scales, w[t]);
-                const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.f, up[t]);
+                up[t][g] = unit_of(scales, w[t]);
+                const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.f, up[t][g]);
 #pragma unroll
                 for (int e = 0; e < 4; e++)
                     wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * (bits<f16x2>(scales[e]) * (f16x2){f, f}));
 #pragma unroll
                 for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], up[t]);
+                    for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], up[t][g]);
             }
         }
         if (!full) {   // nor do scales of tokens that the row does not see
@@ -284,14 +296,14 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
                 st.o[t][2 * i + 1] = mfma<true>(hi, wg[t], st.o[t][2 * i + 1]);
             }
         }
-        if (odd) {
+    }
+    if (odd) {
 #pragma unroll
-            for (int t = 0; t < RT; t++)
+        for (int t = 0; t < RT; t++)
 #pragma unroll
-                for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
+            for (int d = 0; d < D / 16; d++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], -up[t]);
-        }
+                for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], -up[t][d * 16 / G]);
     }
     values_done();
 }

@@ -116,3 +116,33 @@ def test_a_row_does_not_depend_on_later_tokens(serve, big):
         got = c.cache.attention(c.batch(), q.cuda(), window=window)
         check(c, 2, q, got, window=window)
         assert torch.equal(got[:11], want[:11]) and not torch.equal(got[11:], want[11:])
+
+
+# --------------------------------------------------------- values of all sizes
+
+def _sink(c, at, powers, per):
+    """Keys and queries for which token `at` weighs 2^powers times the others, which weigh about the same."""
+    D = c.D
+    q = torch.zeros(sum(c.new), per * c.heads, D)
+    q[..., 0] = 1.0
+    for k in c.k:
+        k.copy_((k.float() * 0.01).to(k.dtype))
+        k[:, :, 0] = 0.0
+        if k.shape[0] > at:
+            k[at, :, 0] = powers * math.log(2) * math.sqrt(D)
+    return q.to(DT[c.dt])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("size", [1.0, 0.05, 1e-2, 1e-3, 1e-4, 1e-5])
+@pytest.mark.parametrize("kv,new,per", [([700], [1], 4), ([9000], [1], 2), ([1500], [40], 2)])
+@pytest.mark.parametrize("powers", [11, 14])
+def test_attention_of_small_values_beside_a_heavy_token(serve, size, dt, kv, new, per, powers):
+    c = Case(serve, kv, new, heads=1, D=64, G=32, page=64, dt=dt, seed=34)
+    q = _sink(c, 3, powers, per)
+    for v in c.v:
+        v.copy_((v.float() * size).to(v.dtype))
+        v[3] = 0
+    c.fill(1)
+    out, lse = c.cache.attention(c.batch(), q.cuda(), lse=True)
+    check(c, per, q, out, lse)
