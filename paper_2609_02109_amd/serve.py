@@ -9,7 +9,8 @@ their positions on the way, and its attention.
 
 As in `mf`, this is marshalling only: torch supplies device memory and the
 stream, the kernels of libmf.so do the work.  Calls enqueue on `stream` (None:
-torch's current one) and do not synchronise; include/mf.h has the definitions.
+torch's current one), copies of what is not contiguous too, and do not
+synchronise; include/mf.h has the definitions.
 """
 from __future__ import annotations
 
@@ -20,7 +21,7 @@ import threading
 import torch
 
 from . import mf
-from .mf import _check, _keep_for, _ptr
+from .mf import _check, _ptr
 
 _DTYPES = {torch.float32: mf.MF_F32, torch.bfloat16: mf.MF_BF16, torch.float16: mf.MF_F16}
 _HALF = (torch.bfloat16, torch.float16)
@@ -61,14 +62,34 @@ class AttnArgs(C.Structure):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_of(device, stream):
-    """hipStream_t of `stream` or of torch's current stream on `device` (whose
-    Python object costs as much to make as a kernel launch)."""
-    if stream is not None:
-        return stream.cuda_stream
+def _stream_of(device):
+    """hipStream_t of torch's current stream on `device` (whose Python object
+    costs as much to make as a kernel launch)."""
     if _raw_stream is not None:
         return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
+
+
+def _tensors(x):
+    if isinstance(x, (tuple, list)):
+        return [t for y in x for t in _tensors(y)]
+    return [x] if isinstance(x, torch.Tensor) and x.is_cuda else []
+
+
+def _on(stream, tensors, call):
+    """`call` with `stream` as torch's current one, so that whatever it copies, allocates and launches
+    is in one order.  What it reads is kept until that has run, what it returns until the caller's own
+    stream has."""
+    before = torch.cuda.current_stream(stream.device)
+    if stream == before:
+        return call()
+    with torch.cuda.stream(stream):
+        got = call()
+    for t in _tensors(tensors):
+        t.record_stream(stream)
+    for t in _tensors(got):
+        t.record_stream(before)
+    return got
 
 
 class _Workspaces:
@@ -79,18 +100,14 @@ class _Workspaces:
     def __init__(self):
         self._held, self._lock = {}, threading.Lock()
 
-    def get(self, nbytes: int, device, stream):
+    def get(self, nbytes: int, device):
         if torch.cuda.is_current_stream_capturing():
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-            _keep_for(stream, ws)
-            return ws
-        key = (threading.get_ident(), device, _stream_of(device, stream))
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        key = (threading.get_ident(), device, _stream_of(device))
         with self._lock:
             ws = self._held.get(key)
             if ws is None or ws.numel() < nbytes:
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-                _keep_for(stream, ws)
-                self._held[key] = ws
+                ws = self._held[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return ws
 
 
@@ -144,17 +161,23 @@ class W4Weight:
         self.desc = W4Desc(self.n_out, self.n_in, self.group, _DTYPES[self.dtype])
         nb = C.c_size_t()
         _check(mf.lib.mf_w4_pack_bytes(C.byref(self.desc), C.byref(nb)), "mf_w4_pack_bytes")
-        codes, scales = codes.contiguous(), scales.contiguous()
-        zeros = zeros if zeros is None else zeros.contiguous()
-        self.packed = torch.empty(int(nb.value), dtype=torch.uint8, device=self.device)
-        _keep_for(stream, codes, scales, zeros, self.packed)
-        _check(mf.lib.mf_w4_pack(C.byref(self.desc), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(self.packed),
-                                 C.c_size_t(self.packed.numel()), _stream_of(self.device, stream)), "mf_w4_pack")
+        lay_out = lambda: self._pack(codes, scales, zeros, int(nb.value))
+        self.packed = lay_out() if stream is None else _on(stream, (codes, scales, zeros), lay_out)
         self._packed_ptr = self.packed.data_ptr()
         self._ws_bytes = {}   # by rows
 
+    def _pack(self, codes, scales, zeros, nbytes):
+        codes, scales = codes.contiguous(), scales.contiguous()
+        zeros = zeros if zeros is None else zeros.contiguous()
+        packed = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        _check(mf.lib.mf_w4_pack(C.byref(self.desc), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(packed),
+                                 C.c_size_t(nbytes), _stream_of(self.device)), "mf_w4_pack")
+        return packed
+
     def matmul(self, x, bias=None, out=None, stream=None):
         """x [.., K] @ W.T + bias [N] -> [.., N], in the scales' type."""
+        if stream is not None:
+            return _on(stream, (x, bias, out, self.packed), lambda: self.matmul(x, bias, out))
         lead = x.shape[:-1]
         if not lead or x.shape[-1] != self.n_in or x.dtype is not self.dtype or x.device != self.device:
             _require(x.dim() == 1 and x.shape[0] == self.n_in and x.dtype is self.dtype and x.device == self.device,
@@ -175,15 +198,13 @@ class W4Weight:
             y = out if out.dim() == 2 else out.view(-1, self.n_out)
         args = W4Args(self.desc, self._packed_ptr, x.data_ptr(), None if bias is None else bias.data_ptr(), y.data_ptr(), m,
                       x.stride(0), y.stride(0))
-        if stream is not None:
-            _keep_for(stream, x, bias, y, self.packed)
         need = self._ws_bytes.get(m)
         if need is None:
             nb = C.c_size_t()
             _check(mf.lib.mf_w4_workspace_size(C.byref(args), C.byref(nb)), "mf_w4_workspace_size")
             need = self._ws_bytes[m] = nb.value
-        ws = _workspaces.get(need, self.device, stream) if need else None
-        s = mf.lib.mf_w4_matmul(C.byref(args), ws.data_ptr() if need else None, need, _stream_of(self.device, stream))
+        ws = _workspaces.get(need, self.device) if need else None
+        s = mf.lib.mf_w4_matmul(C.byref(args), ws.data_ptr() if need else None, need, _stream_of(self.device))
         if s:
             _check(s, "mf_w4_matmul")
         return out
@@ -248,6 +269,9 @@ class KV4Cache:
         turned by their positions when cos / sin [n_pos, rot_dim // 2] are given;
         with q [rows, n_heads, head_dim] also returns the queries turned the
         same way (q_out: where to, e.g. q itself)."""
+        if stream is not None:
+            return _on(stream, (k, v, cos, sin, q, q_out, self.pages, batch.tensors),
+                       lambda: self.append(batch, k, v, cos, sin, q, interleaved, q_out))
         dt, dev = k.dtype, self.device
         _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
         shape = (batch.rows, self.n_kv_heads, self.head_dim)
@@ -273,22 +297,20 @@ class KV4Cache:
                 qs, os = q.stride(), q_out.stride()
                 a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], *turn, heads, q.data_ptr(),
                                q_out.data_ptr(), qs[0], qs[1], os[0], os[1])
-        if stream is not None:
-            _keep_for(stream, k, v, cos, sin, q, q_out, self.pages, *batch.tensors)
-        s = mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream_of(dev, stream))
+        s = mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream_of(dev))
         if s:
             _check(s, "mf_kv4_append")
         return q_out
 
     def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
         """(keys, values) [rows, n_kv_heads, head_dim] that the cache holds for the batch's rows."""
+        if stream is not None:
+            return _on(stream, (self.pages, batch.tensors), lambda: self.read(batch, dtype))
         _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
         k = torch.empty((batch.rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
-        if stream is not None:
-            _keep_for(stream, k, v, self.pages, *batch.tensors)
         s = mf.lib.mf_kv4_read(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(),
-                               _stream_of(self.device, stream))
+                               _stream_of(self.device))
         if s:
             _check(s, "mf_kv4_read")
         return k, v
@@ -298,6 +320,8 @@ class KV4Cache:
         tokens: [rows, n_heads, head_dim], with lse=True also the log of the
         softmax sums [rows, n_heads] float32.  scale: 1 / sqrt(head_dim) by
         default; window > 0: only the newest `window` tokens up to each row's."""
+        if stream is not None:
+            return _on(stream, (q, out, self.pages, batch.tensors), lambda: self.attention(batch, q, scale, window, lse, out))
         _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
         heads = q.shape[1]
         q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
@@ -311,10 +335,8 @@ class KV4Cache:
             nb = C.c_size_t()
             _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
             need = batch._ws_bytes[key] = nb.value
-        ws = _workspaces.get(need, self.device, stream) if need else None
-        if stream is not None:
-            _keep_for(stream, q, out, ls, self.pages, *batch.tensors)
-        s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws.data_ptr() if need else None, need, _stream_of(self.device, stream))
+        ws = _workspaces.get(need, self.device) if need else None
+        s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws.data_ptr() if need else None, need, _stream_of(self.device))
         if s:
             _check(s, "mf_kv4_attention")
         return out if ls is None else (out, ls)

@@ -146,3 +146,75 @@ def test_attention_of_small_values_beside_a_heavy_token(serve, size, dt, kv, new
     c.fill(1)
     out, lse = c.cache.attention(c.batch(), q.cuda(), lse=True)
     check(c, per, q, out, lse)
+
+
+# -------------------------------------------------------------------- streams
+
+def _busy():
+    """Some tenths of a second of work on the current stream."""
+    a = torch.ones(8192, 8192, device="cuda")
+    for _ in range(40):
+        a = (a @ a).clamp_(0, 1)
+    return a
+
+
+def test_copies_run_on_the_stream_of_the_call(serve):
+    """What is not contiguous is copied within a call: on its stream, not on the current one, which is busy."""
+    n, k, g = 80, 256, 64
+    codes, scales, z, _ = _weights(n, k, g, torch.bfloat16, True, 39)
+    codes, scales, z = codes.cuda(), scales.cuda(), z.cuda()
+    turned = [t.t().contiguous().t() for t in (codes, scales, z)]
+    xt = torch.randn(k, 40, generator=_gen(40)).bfloat16().cuda()
+    x3 = torch.randn(3, k, 5, generator=_gen(41)).bfloat16().cuda().transpose(1, 2)
+    c = Case(serve, [3000, 40], [2, 1], heads=2, D=64, G=32, page=16, dt="bf16", seed=42)
+    c.fill(1)
+    b, cos, sin = c.batch(), *serve.rope_table(3008, 64)
+    rows = [torch.randn(3, h, 64, 2, generator=c.gen).bfloat16().cuda()[..., 0] for h in (2, 2, 8)]
+
+    def calls(stream):
+        w = serve.W4Weight(*turned, stream=stream)
+        y = w.matmul(xt.t(), stream=stream)
+        y3 = w.matmul(x3, stream=stream)
+        q = c.cache.append(b, rows[0], rows[1], cos=cos, sin=sin, q=rows[2], stream=stream)
+        o, ls = c.cache.attention(b, rows[2], lse=True, stream=stream)
+        return [w.packed, y, y3, q, o, ls, *c.cache.read(b, stream=stream)]
+
+    W = serve.W4Weight(codes, scales, z)
+    want = calls(None)
+    assert torch.equal(want[0], W.packed) and torch.equal(want[1], W.matmul(xt.t().contiguous()))
+    main, side = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(main):
+        for _ in range(3):
+            # what the caching allocator hands out next on `main` is still being written there
+            freed = [torch.full_like(t, 3) for t in want for _ in range(2)]
+            busy = _busy()
+            for t in freed:
+                t.fill_(7)
+            del freed, t
+            got = calls(side)
+            side.synchronize()
+            copies = [t.cpu() for t in got]   # on `main`, after what is under way there
+            main.synchronize()
+            assert all(torch.equal(a, b.cpu()) for a, b in zip(copies, want))
+            del busy
+
+
+def test_results_of_another_stream_outlive_it(serve):
+    """A result is not handed out again while the caller's stream still reads it."""
+    codes, scales, z, _ = _weights(4096, 256, 64, torch.bfloat16, True, 43)
+    W = serve.W4Weight(codes.cuda(), scales.cuda(), z.cuda())
+    x = torch.randn(64, 256, generator=_gen(44)).bfloat16().cuda()
+    want, side = W.matmul(x), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        y = W.matmul(x, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        busy = _busy()
+        kept = y.clone()   # after the work above
+        del y
+        for _ in range(4):
+            W.matmul(-x, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(kept, want)
+        del busy
