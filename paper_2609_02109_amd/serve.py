@@ -60,6 +60,7 @@ class AttnArgs(C.Structure):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream_of(device):
@@ -76,15 +77,19 @@ def _tensors(x):
     return [x] if isinstance(x, torch.Tensor) and x.is_cuda else []
 
 
-def _on(stream, tensors, call):
-    """`call` with `stream` as torch's current one, so that whatever it copies, allocates and launches
-    is in one order.  What it reads is kept until that has run, what it returns until the caller's own
+def _on(device, stream, tensors, call):
+    """`call` with `device` as the current one and `stream` (None: the device's own) as torch's current
+    one, so that whatever it copies, allocates and launches is in one order: HIP runs stream 0 on the
+    current device.  What it reads is kept until that has run, what it returns until the caller's own
     stream has."""
-    before = torch.cuda.current_stream(stream.device)
-    if stream == before:
-        return call()
-    with torch.cuda.stream(stream):
-        got = call()
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream: one of {device} is wanted")
+    with torch.cuda.device(device):
+        before = torch.cuda.current_stream(device)
+        if stream is None or stream == before:
+            return call()
+        with torch.cuda.stream(stream):
+            got = call()
     for t in _tensors(tensors):
         t.record_stream(stream)
     for t in _tensors(got):
@@ -162,7 +167,7 @@ class W4Weight:
         nb = C.c_size_t()
         _check(mf.lib.mf_w4_pack_bytes(C.byref(self.desc), C.byref(nb)), "mf_w4_pack_bytes")
         lay_out = lambda: self._pack(codes, scales, zeros, int(nb.value))
-        self.packed = lay_out() if stream is None else _on(stream, (codes, scales, zeros), lay_out)
+        self.packed = _on(self.device, stream, (codes, scales, zeros), lay_out)
         self._packed_ptr = self.packed.data_ptr()
         self._ws_bytes = {}   # by rows
 
@@ -176,8 +181,8 @@ class W4Weight:
 
     def matmul(self, x, bias=None, out=None, stream=None):
         """x [.., K] @ W.T + bias [N] -> [.., N], in the scales' type."""
-        if stream is not None:
-            return _on(stream, (x, bias, out, self.packed), lambda: self.matmul(x, bias, out))
+        if stream is not None or self.device.index != _current_device():
+            return _on(self.device, stream, (x, bias, out, self.packed), lambda: self.matmul(x, bias, out))
         lead = x.shape[:-1]
         if not lead or x.shape[-1] != self.n_in or x.dtype is not self.dtype or x.device != self.device:
             _require(x.dim() == 1 and x.shape[0] == self.n_in and x.dtype is self.dtype and x.device == self.device,
@@ -231,7 +236,7 @@ class KV4Batch:
         _require(tuple(q_start.shape) == (n + 1,) and q_start.is_contiguous(), "q_start: contiguous [n_seq + 1] is wanted")
         _require(page_table.dim() == 2 and page_table.shape[0] == n and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
                  "page_table: [n_seq, pages] with a contiguous last dimension is wanted")
-        self.tensors = (q_start, kv_len, page_table)
+        self.tensors, self.device = (q_start, kv_len, page_table), kv_len.device
         self._ws_bytes = {}   # of attention, by query heads, window and the cache's shape: a function of the sizes
         self.rows = int(rows)
         self.raw = Batch(n, int(max_new), int(max_kv), self.rows, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
@@ -264,13 +269,18 @@ class KV4Cache:
         _require(all(t.device == self.device for t in b.tensors), f"the batch's tensors: on {self.device} is wanted")
         return b
 
+    def _beside(self, batch):
+        if batch.device != self.device:
+            raise ValueError(f"batch: on {self.device} is wanted")
+
     def append(self, batch: KV4Batch, k, v, cos=None, sin=None, q=None, interleaved=False, q_out=None, stream=None):
         """Writes k and v [rows, n_kv_heads, head_dim] into the cache, the keys
         turned by their positions when cos / sin [n_pos, rot_dim // 2] are given;
         with q [rows, n_heads, head_dim] also returns the queries turned the
         same way (q_out: where to, e.g. q itself)."""
-        if stream is not None:
-            return _on(stream, (k, v, cos, sin, q, q_out, self.pages, batch.tensors),
+        self._beside(batch)
+        if stream is not None or self.device.index != _current_device():
+            return _on(self.device, stream, (k, v, cos, sin, q, q_out, self.pages, batch.tensors),
                        lambda: self.append(batch, k, v, cos, sin, q, interleaved, q_out))
         dt, dev = k.dtype, self.device
         _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
@@ -304,8 +314,9 @@ class KV4Cache:
 
     def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
         """(keys, values) [rows, n_kv_heads, head_dim] that the cache holds for the batch's rows."""
-        if stream is not None:
-            return _on(stream, (self.pages, batch.tensors), lambda: self.read(batch, dtype))
+        self._beside(batch)
+        if stream is not None or self.device.index != _current_device():
+            return _on(self.device, stream, (self.pages, batch.tensors), lambda: self.read(batch, dtype))
         _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
         k = torch.empty((batch.rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
@@ -320,8 +331,9 @@ class KV4Cache:
         tokens: [rows, n_heads, head_dim], with lse=True also the log of the
         softmax sums [rows, n_heads] float32.  scale: 1 / sqrt(head_dim) by
         default; window > 0: only the newest `window` tokens up to each row's."""
-        if stream is not None:
-            return _on(stream, (q, out, self.pages, batch.tensors), lambda: self.attention(batch, q, scale, window, lse, out))
+        self._beside(batch)
+        if stream is not None or self.device.index != _current_device():
+            return _on(self.device, stream, (q, out, self.pages, batch.tensors), lambda: self.attention(batch, q, scale, window, lse, out))
         _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
         heads = q.shape[1]
         q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
