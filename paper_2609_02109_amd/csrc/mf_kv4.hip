@@ -286,7 +286,7 @@ __global__ __launch_bounds__(64) void append_kernel(KvAppendArgs a, int blocks, 
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[kKvBlock * D];
     const int items = a.g.n_kv_heads + slices;
-    const int h = (int)(blockIdx.x % items), rest = (int)(blockIdx.x / items), s = rest / blocks;
+    const int h = (int)(blockIdx.x % items), rest = (int)(blockIdx.x / items), s = a.first_seq + rest / blocks;
     const Span p = span_of(a.b, s);
     if (p.lo >= p.hi) return;
     if (h >= a.g.n_kv_heads) {
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(64) void read_kernel(KvReadArgs a, int blocks)
 {
     constexpr int NS = D / 32, NG = D / G;
     __shared__ __attribute__((aligned(16))) uint8_t lds[kKvBlock * D];
-    const int h = (int)(blockIdx.x % a.g.n_kv_heads), rest = (int)(blockIdx.x / a.g.n_kv_heads), s = rest / blocks;
+    const int h = (int)(blockIdx.x % a.g.n_kv_heads), rest = (int)(blockIdx.x / a.g.n_kv_heads), s = a.first_seq + rest / blocks;
     const Span p = span_of(a.b, s);
     const int lane = threadIdx.x & 63, tok = lane & 15, qt = lane >> 4;
     for (int blk = (p.lo >> 4) + rest % blocks; blk * kKvBlock < p.hi; blk += blocks) {
@@ -394,12 +394,20 @@ void go_read(const KvReadArgs &a, unsigned grid, int blocks, hipStream_t s)
     hipLaunchKernelGGL((read_kernel<TY, D, G>), dim3(grid), dim3(64), 0, s, a, blocks);
 }
 
-// Workgroups a sequence gets for its blocks of 16, so that the grid stays within 2^30; a kernel takes further blocks in turn.
-int blocks_for(long long span, long long others)
+// Launches of workgroups of 64 for n_seq sequences of `items` items and up to `span` tokens each: as many sequences to a
+// launch as have room, and as many workgroups to an item as it has blocks of 16 or the launch has room; a kernel takes further blocks in turn.
+template <class F>
+hipError_t each_launch(int n_seq, int items, int span, const F &launch)
 {
-    long long b = (span + 14) / 16 + 1;   // 16-blocks that span tokens can touch
-    const long long most = (1ll << 30) / (others > 0 ? others : 1);
-    return (int)(b < most ? b : most > 1 ? most : 1);
+    const long long room = most_workgroups(64) / items, touched = (span + 14ll) / 16 + 1;
+    for (int first = 0; first < n_seq;) {
+        const int n = (int)(n_seq - first < room ? n_seq - first : room), blocks = (int)(touched < room / n ? touched : room / n);
+        launch(first, (unsigned)((long long)n * items * blocks), blocks);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        first += n;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -410,27 +418,29 @@ int blocks_for(long long span, long long others)
         if ((g).group == 32) { CALL(128, 32); } else if ((g).group == 64) { CALL(128, 64); } else { CALL(128, 128); } } \
     else { if ((g).group == 32) { CALL(256, 32); } else if ((g).group == 64) { CALL(256, 64); } else { CALL(256, 128); } }
 
-hipError_t launch_kv4_append(const KvAppendArgs &a, bool f16, hipStream_t s)
+hipError_t launch_kv4_append(const KvAppendArgs &args, bool f16, hipStream_t s)
 {
     // eight heads of queries to a workgroup
-    const int slices = a.q ? (a.n_heads + 7) / 8 : 0, few = a.b.max_new < 8, items = a.g.n_kv_heads + slices;
-    const int blocks = blocks_for(a.b.max_new, (long long)a.b.n_seq * items);
-    const unsigned grid = (unsigned)((long long)a.b.n_seq * items * blocks);
+    const int slices = args.q ? (args.n_heads + 7) / 8 : 0, few = args.b.max_new < 8;
+    return each_launch(args.b.n_seq, args.g.n_kv_heads + slices, args.b.max_new, [&](int first, unsigned grid, int blocks) {
+        KvAppendArgs a = args;
+        a.first_seq = first;
 #define CALL(D, G) f16 ? go_append<true, D, G>(a, grid, blocks, slices, few, s) : go_append<false, D, G>(a, grid, blocks, slices, few, s)
-    MFS_FOR_SHAPE(a.g, CALL)
+        MFS_FOR_SHAPE(a.g, CALL)
 #undef CALL
-    return hipGetLastError();
+    });
 }
 
-hipError_t launch_kv4_read(const KvReadArgs &a, int dtype, hipStream_t s)
+hipError_t launch_kv4_read(const KvReadArgs &args, int dtype, hipStream_t s)
 {
-    const int blocks = blocks_for(a.b.max_new, (long long)a.b.n_seq * a.g.n_kv_heads);
-    const unsigned grid = (unsigned)((long long)a.b.n_seq * a.g.n_kv_heads * blocks);
+    return each_launch(args.b.n_seq, args.g.n_kv_heads, args.b.max_new, [&](int first, unsigned grid, int blocks) {
+        KvReadArgs a = args;
+        a.first_seq = first;
 #define CALL(D, G) dtype == MF_F32 ? go_read<MF_F32, D, G>(a, grid, blocks, s) \
                                    : dtype == MF_BF16 ? go_read<MF_BF16, D, G>(a, grid, blocks, s) : go_read<MF_F16, D, G>(a, grid, blocks, s)
-    MFS_FOR_SHAPE(a.g, CALL)
+        MFS_FOR_SHAPE(a.g, CALL)
 #undef CALL
-    return hipGetLastError();
+    });
 }
 
 }  // namespace mfs

@@ -10,6 +10,10 @@
 
 namespace mfs {
 
+// A launch has fewer than 2^32 threads in a dimension of its grid: the most
+// workgroups.  Larger grids are launched in parts.
+constexpr long long most_workgroups(int threads) { return ((1ll << 32) - 1) / threads; }
+
 // ---------------------------------------------------------------- codes
 // Eight codes of a row, k = 8 q + j, share a dword: code j sits at bits
 // 16 (j % 2) + 4 (j / 2), so that a mask takes a pair (2 s, 2 s + 1) to the same
@@ -106,11 +110,13 @@ struct KvAppendArgs {
     const float *cos, *sin;
     long long k_stride, k_head, v_stride, v_head, q_stride, q_head, qo_stride, qo_head;
     int rot, interleaved, n_heads;
+    int first_seq;           // of this launch
 };
 struct KvReadArgs {
     KvGeom g;
     KvBatch b;
     void *k, *v;
+    int first_seq;
 };
 constexpr int kAttnWaves = 4;
 constexpr int kAttnStep = 32;   // tokens a wave takes at a time
