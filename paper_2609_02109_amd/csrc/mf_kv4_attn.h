@@ -626,7 +626,7 @@ template <bool F16, int D, int G, int RT>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_rows_kernel(KvAttnArgs a)
 {
     constexpr int WG_ROWS = attn_rows(RT, true);
-    const int split = (int)(blockIdx.x % a.splits), item = (int)(blockIdx.x / a.splits);
+    const int wg = a.first + (int)blockIdx.x, split = wg % a.splits, item = wg / a.splits;
     const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
     const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
     const int row_end = (int)min((long long)sr.n * a.per_kv, (long long)(tile + 1) * WG_ROWS);
@@ -652,7 +652,7 @@ template <bool F16, int D, int G, int RT, int NW, bool WHOLE>
 __global__ __launch_bounds__(NW * 64, 2) void attn_tokens_kernel(KvAttnArgs a)
 {
     if constexpr (WHOLE) {
-        const int h = (int)(blockIdx.x % a.g.n_kv_heads), s = (int)(blockIdx.x / a.g.n_kv_heads);
+        const int wg = a.first + (int)blockIdx.x, h = wg % a.g.n_kv_heads, s = wg / a.g.n_kv_heads;
         const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
         if (sr.n == 0) return;
         const Range t = range_of(sr, 0, sr.n - 1, a.window);
@@ -701,23 +701,32 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_tokens_kernel(KvAttnArgs a)
     }
 }
 
+// A kernel over `workgroups` of them, in as many launches as they take.
+inline hipError_t each_launch(void (*kernel)(KvAttnArgs), KvAttnArgs a, long long workgroups, int threads, hipStream_t s)
+{
+    const long long most = most_workgroups(threads);
+    for (long long first = 0; first < workgroups; first += most) {
+        a.first = (int)first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(workgroups - first < most ? workgroups - first : most)), dim3(threads), 0, s, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // One head size's kernels (mf_kv4_attn_d*.hip).
 template <bool F16, int D, int G>
 hipError_t pick_attn(const KvAttnArgs &a, const KvPlan &p, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.workgroups);
-    if (p.rows_by_wave) hipLaunchKernelGGL((attn_rows_kernel<F16, D, G, D < 256 ? 2 : 1>), grid, dim3(kAttnWaves * 64), 0, s, a);
-    else if (D < 256 && p.rt == 2) {
+    const auto go = [&](void (*kernel)(KvAttnArgs), int waves) { return each_launch(kernel, a, p.workgroups, waves * 64, s); };
+    if (p.rows_by_wave) return go(attn_rows_kernel<F16, D, G, D < 256 ? 2 : 1>, kAttnWaves);
+    if (D < 256 && p.rt == 2) {
         constexpr int RT = D < 256 ? 2 : 1;
-        if (!p.whole) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 4, false>), grid, dim3(256), 0, s, a);
-        else if (p.waves == 8) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 8, true>), grid, dim3(512), 0, s, a);
-        else hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, RT, 4, true>), grid, dim3(256), 0, s, a);
-    } else {
-        if (!p.whole) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, 1, 4, false>), grid, dim3(256), 0, s, a);
-        else if (p.waves == 8) hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, 1, 8, true>), grid, dim3(512), 0, s, a);
-        else hipLaunchKernelGGL((attn_tokens_kernel<F16, D, G, 1, 4, true>), grid, dim3(256), 0, s, a);
+        if (!p.whole) return go(attn_tokens_kernel<F16, D, G, RT, 4, false>, 4);
+        return p.waves == 8 ? go(attn_tokens_kernel<F16, D, G, RT, 8, true>, 8) : go(attn_tokens_kernel<F16, D, G, RT, 4, true>, 4);
     }
-    return hipGetLastError();
+    if (!p.whole) return go(attn_tokens_kernel<F16, D, G, 1, 4, false>, 4);
+    return p.waves == 8 ? go(attn_tokens_kernel<F16, D, G, 1, 8, true>, 8) : go(attn_tokens_kernel<F16, D, G, 1, 4, true>, 4);
 }
 
 }  // namespace mfs

@@ -132,7 +132,7 @@ __device__ __forceinline__ void join_row(const KvAttnArgs &a, long long first, l
 template <bool F16, int D>
 __global__ __launch_bounds__(kJoinWaves * 64) void join_rows_kernel(KvAttnArgs a)
 {
-    const int item = (int)(blockIdx.x / a.slot_rows), rr = (int)(blockIdx.x % a.slot_rows);
+    const int wg = a.first + (int)blockIdx.x, item = wg / a.slot_rows, rr = wg % a.slot_rows;
     const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
     const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
     const long long row = (long long)tile * a.slot_rows + rr;
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_rows_kernel(KvAttnArgs a
 template <bool F16, int D>
 __global__ __launch_bounds__(kJoinWaves * 64) void join_tokens_kernel(KvAttnArgs a)
 {
-    const int item = (int)(blockIdx.x / a.slot_rows), rr = (int)(blockIdx.x % a.slot_rows);
+    const int wg = a.first + (int)blockIdx.x, item = wg / a.slot_rows, rr = wg % a.slot_rows;
     const int h = item % a.g.n_kv_heads, s = item / a.g.n_kv_heads, lane = threadIdx.x & 63;
     const SeqRaw raw = seq_raw(a.b, s);
     const SeqRows sr = seq_rows(a.b, raw);
@@ -166,16 +166,11 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_tokens_kernel(KvAttnArgs
 }
 
 template <int D>
-void go_join(const KvAttnArgs &a, const KvPlan &p, bool f16, long long items, hipStream_t s)
+hipError_t go_join(const KvAttnArgs &a, const KvPlan &p, bool f16, long long items, hipStream_t s)
 {
-    const dim3 grid((unsigned)(items * a.slot_rows)), block(kJoinWaves * 64);
-    if (p.rows_by_wave) {
-        if (f16) hipLaunchKernelGGL((join_rows_kernel<true, D>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((join_rows_kernel<false, D>), grid, block, 0, s, a);
-    } else {
-        if (f16) hipLaunchKernelGGL((join_tokens_kernel<true, D>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((join_tokens_kernel<false, D>), grid, block, 0, s, a);
-    }
+    const auto go = [&](void (*kernel)(KvAttnArgs)) { return each_launch(kernel, a, items * a.slot_rows, kJoinWaves * 64, s); };
+    if (p.rows_by_wave) return f16 ? go(join_rows_kernel<true, D>) : go(join_rows_kernel<false, D>);
+    return f16 ? go(join_tokens_kernel<true, D>) : go(join_tokens_kernel<false, D>);
 }
 
 }  // namespace
@@ -185,10 +180,7 @@ hipError_t launch_kv4_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipSt
     const hipError_t e = a.g.head_dim == 64 ? launch_attn_d64(a, p, f16, s) : a.g.head_dim == 128 ? launch_attn_d128(a, p, f16, s) : launch_attn_d256(a, p, f16, s);
     if (e != hipSuccess || p.slots == 0) return e;
     const long long items = p.row_tiles * a.b.n_seq * a.g.n_kv_heads;
-    if (a.g.head_dim == 64) go_join<64>(a, p, f16, items, s);
-    else if (a.g.head_dim == 128) go_join<128>(a, p, f16, items, s);
-    else go_join<256>(a, p, f16, items, s);
-    return hipGetLastError();
+    return a.g.head_dim == 64 ? go_join<64>(a, p, f16, items, s) : a.g.head_dim == 128 ? go_join<128>(a, p, f16, items, s) : go_join<256>(a, p, f16, items, s);
 }
 
 }  // namespace mfs

@@ -138,6 +138,7 @@ struct KvAttnArgs {
     int splits, chunk;       // by rows: parts of the tokens, tokens of a part
     int workgroups, whole;   // by tokens
     int slots, slot_rows;    // room for parts that the join adds up
+    int first;               // workgroup of this launch, where they are more than one launch's
     float *part;             // [slot][row][D] sums, then [slot][row] (base, sum of weights)
 };
 // How the work is laid over the card: a function of the sizes alone.

@@ -122,7 +122,7 @@ mf_status check_attn(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const
     p = kv4_plan(a.g, a.b, a.n_heads, a.window);
     // all sequences' units of one head are an int
     if ((((int64_t)batch->max_kv + kAttnUnit - 1) / kAttnUnit + 1) * batch->n_seq > INT32_MAX) return MF_EUNSUPPORTED;
-    // one grid each: the workgroups, and the join's rows
+    // a workgroup's number, and a row's of the join, are an int
     const int64_t items = p.row_tiles * batch->n_seq * cache->n_kv_heads;
     if (p.workgroups > INT32_MAX || (p.slots > 0 && (items * p.slot_rows > INT32_MAX || p.slots > INT32_MAX))) return MF_EUNSUPPORTED;
     a.row_tiles = (int)p.row_tiles;
