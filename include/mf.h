@@ -412,7 +412,7 @@ mf_status mf_ga_run(mf_problem *p, const mf_ga_args *args, void *d_ws, size_t ws
  * with an infinity or a NaN gives NaN wherever it is multiplied, and sums of 31 |x|
  * over a group have to stay within fp32. */
 typedef struct {
-    int64_t n_out, n_in;    /* 1 <= N <= 2^31 - 16, 1 <= K <= 2^24, K a multiple of G */
+    int64_t n_out, n_in;    /* 1 <= N <= 2^27 - 16, 1 <= K <= 2^24, K a multiple of G */
     int32_t group;          /* G: weights that share a scale, 32, 64 or 128 */
     mf_dtype dtype;         /* MF_BF16 or MF_F16: of the scales, x, bias and y */
 } mf_w4_desc;

@@ -44,7 +44,7 @@ mf_status check_w4(const mf_w4_desc *d)
     if (!half_type(as_int(d->dtype))) return MF_EINVAL;
     if (d->group != 32 && d->group != 64 && d->group != 128) return MF_EUNSUPPORTED;
     if (d->n_out < 1 || d->n_in < 1 || d->n_in % d->group != 0) return MF_EINVAL;
-    if (d->n_out > INT32_MAX - 15 || d->n_in > (1 << 24)) return MF_EUNSUPPORTED;
+    if (d->n_out > kW4MostOut || d->n_in > (1 << 24)) return MF_EUNSUPPORTED;
     return MF_OK;
 }
 

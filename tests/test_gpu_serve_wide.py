@@ -112,3 +112,15 @@ def test_attention_of_a_million_sequences(serve):
     for lo in (0, n // 2 - 1000, n - 2000):
         few = cache.attention(cache.batch(start[:2001], kv[lo:lo + 2000], table[lo:lo + 2000], 2000, 1, 16), q[lo:lo + 2000])
         assert torch.equal(out[lo:lo + 2000], few) and few.abs().max() > 0
+
+
+def test_w4_with_the_most_outputs(serve):
+    # a workgroup for each of 2^23 - 1 tiles of outputs
+    n, k = 2 ** 27 - 16, 32
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    codes = torch.randint(0, 256, (n, k // 2), device="cuda", generator=gen, dtype=torch.uint8)
+    scales = torch.rand(n, 1, device="cuda", generator=gen).bfloat16()
+    x = torch.randn(2, k, device="cuda", generator=gen).bfloat16()
+    y = serve.W4Weight(codes, scales).matmul(x)
+    for lo in (0, n // 2, n - 4096):
+        assert torch.equal(y[:, lo:lo + 4096], serve.W4Weight(codes[lo:lo + 4096], scales[lo:lo + 4096]).matmul(x))

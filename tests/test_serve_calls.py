@@ -1,6 +1,7 @@
 """The served steps' Python calls without a GPU: what they do before the library
 is called (torch's devices and streams are stood in for)."""
 import contextlib
+import ctypes as C
 
 import pytest
 import torch
@@ -102,3 +103,15 @@ def test_a_batch_of_another_device_is_refused():
     for call in (lambda: cache.append(batch, None, None), lambda: cache.read(batch), lambda: cache.attention(batch, None)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("n,want", [(2 ** 27 - 16, mf.MF_OK), (2 ** 27 - 15, mf.MF_EUNSUPPORTED), (2 ** 31 - 16, mf.MF_EUNSUPPORTED)])
+def test_w4_outputs_that_one_launch_takes(n, want):
+    """Every call says so, the sizes' too."""
+    d, nb = serve.W4Desc(n, 32, 32, mf.MF_BF16), C.c_size_t()
+    a = serve.W4Args(d, 256, 1024, None, 4096, 0, 32, n)
+    assert mf.lib.mf_w4_pack_bytes(C.byref(d), C.byref(nb)) == want
+    assert mf.lib.mf_w4_workspace_size(C.byref(a), C.byref(nb)) == want
+    assert mf.lib.mf_w4_matmul(C.byref(a), None, 0, None) == want
+    if want:
+        assert mf.lib.mf_w4_pack(C.byref(d), 1024, 2048, None, 4096, C.c_size_t(1 << 40), None) == want
