@@ -39,15 +39,22 @@ class Decoder:
     def __init__(self, seqs, context, layers=1, heads=32, kv_heads=8, head_dim=128, inner=8192, group=128, kv_group=64, page=64,
                  dtype=torch.bfloat16, seed=0, device="cuda"):
         self.heads, self.kv_heads, self.head_dim, self.width, self.context = heads, kv_heads, head_dim, heads * head_dim, context
+        self._shapes = dict(qkv=((heads + 2 * kv_heads) * head_dim, self.width), out=(self.width, heads * head_dim),
+                            up=(2 * inner, self.width), down=(self.width, inner))
+        self._drawn = (layers, group, dtype, seed, device)
         gen = torch.Generator(device=device).manual_seed(seed)
-        shapes = dict(qkv=((heads + 2 * kv_heads) * head_dim, self.width), out=(self.width, heads * head_dim),
-                      up=(2 * inner, self.width), down=(self.width, inner))
-        self.drawn = [{n: draw_weight(*s, group, dtype, gen, device) for n, s in shapes.items()} for _ in range(layers)]
-        self.layers = [{n: serve.W4Weight(*w) for n, w in layer.items()} for layer in self.drawn]
+        self.layers = [{n: serve.W4Weight(*draw_weight(*s, group, dtype, gen, device)) for n, s in self._shapes.items()} for _ in range(layers)]
         cols = -(-context // page)
         self.caches = [serve.KV4Cache(seqs * cols, page, kv_heads, head_dim, group=kv_group, device=device) for _ in range(layers)]
         self.table = torch.randperm(seqs * cols, generator=gen, device=device).to(torch.int32).view(seqs, cols)
         self.cos, self.sin = serve.rope_table(cols * page, head_dim, device=device)
+
+    @property
+    def drawn(self):
+        """Codes, scales and zero points of every layer's weights, drawn again: they are not held beside the laid out ones."""
+        layers, group, dtype, seed, device = self._drawn
+        gen = torch.Generator(device=device).manual_seed(seed)
+        return [{n: draw_weight(*s, group, dtype, gen, device) for n, s in self._shapes.items()} for _ in range(layers)]
 
     @property
     def bytes(self):
@@ -69,35 +76,37 @@ class Decoder:
         return x
 
 
+def _option(n, context, steps, decoder):
+    model = Decoder(n, context, **decoder)
+    for c in model.caches:
+        c.pages.zero_()
+    dev = model.table.device
+    batch = model.batch(torch.arange(n + 1, dtype=torch.int32, device=dev), torch.full((n,), context, dtype=torch.int32, device=dev), n, 1)
+    x = torch.randn(n, model.width, device=dev).to(model.layers[0]["qkv"].dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        model(batch, x)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        model(batch, x)
+    for _ in range(3):
+        graph.replay()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    for _ in range(steps):
+        graph.replay()
+    end.record()
+    torch.cuda.synchronize()
+    ms = begin.elapsed_time(end) / steps
+    return dict(variant="4-bit", concurrency=n, context=context, ms_per_step=ms, tokens_per_s=1e3 * n / ms, gb=model.bytes / 1e9)
+
+
 def options(concurrency, context, steps=20, **decoder):
-    """One dict per concurrency: ms a step (captured in a graph, all sequences at full context), tokens/s, GB."""
-    out = []
-    for n in concurrency:
-        model = Decoder(n, context, **decoder)
-        for c in model.caches:
-            c.pages.zero_()
-        dev = model.table.device
-        batch = model.batch(torch.arange(n + 1, dtype=torch.int32, device=dev), torch.full((n,), context, dtype=torch.int32, device=dev), n, 1)
-        x = torch.randn(n, model.width, device=dev).to(model.layers[0]["qkv"].dtype)
-        side = torch.cuda.Stream()
-        side.wait_stream(torch.cuda.current_stream())
-        with torch.cuda.stream(side):
-            model(batch, x)
-        torch.cuda.current_stream().wait_stream(side)
-        graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(graph):
-            model(batch, x)
-        for _ in range(3):
-            graph.replay()
-        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        begin.record()
-        for _ in range(steps):
-            graph.replay()
-        end.record()
-        torch.cuda.synchronize()
-        ms = begin.elapsed_time(end) / steps
-        out.append(dict(variant="4-bit", concurrency=n, context=context, ms_per_step=ms, tokens_per_s=1e3 * n / ms, gb=model.bytes / 1e9))
-    return out
+    """One dict per concurrency: ms a step (captured in a graph, all sequences at full context), tokens/s, GB.
+    One model at a time is on the device."""
+    return [_option(n, context, steps, decoder) for n in concurrency]
 
 
 def main(argv=None):
