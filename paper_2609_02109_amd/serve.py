@@ -10,7 +10,8 @@ their positions on the way, and its attention.
 As in `mf`, this is marshalling only: torch supplies device memory and the
 stream, the kernels of libmf.so do the work.  Calls enqueue on `stream` (None:
 torch's current one), copies of what is not contiguous too, and do not
-synchronise; include/mf.h has the definitions.
+synchronise; include/mf.h has the definitions.  They are for inference: an
+operand that requires a gradient is refused while gradients are recorded.
 """
 from __future__ import annotations
 
@@ -124,6 +125,14 @@ def _require(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _no_gradient(*tensors):
+    """The operators have no backward: a result without a gradient would lose it silently."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("an operand requires a gradient, and there is none through this call: torch.no_grad() or detach() is wanted")
+
+
 def _rows(t, name, shape, dtype, device):
     """A tensor of `shape` whose last dimension is contiguous (a copy where it is not)."""
     if t.shape != shape or t.dtype is not dtype or t.device != device:
@@ -190,6 +199,7 @@ class W4Weight:
         if bias is not None:
             _require(bias.dtype is self.dtype and bias.device == self.device and tuple(bias.shape) == (self.n_out,)
                      and bias.is_contiguous(), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
+        _no_gradient(x, bias, out)
         if len(lead) != 1:
             x = x.reshape(-1, self.n_in)
         m = x.shape[0]
@@ -282,6 +292,7 @@ class KV4Cache:
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (k, v, cos, sin, q, q_out, self.pages, batch.tensors),
                        lambda: self.append(batch, k, v, cos, sin, q, interleaved, q_out))
+        _no_gradient(k, v, q, q_out)
         dt, dev = k.dtype, self.device
         _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
         shape = (batch.rows, self.n_kv_heads, self.head_dim)
@@ -335,6 +346,7 @@ class KV4Cache:
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (q, out, self.pages, batch.tensors), lambda: self.attention(batch, q, scale, window, lse, out))
         _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
+        _no_gradient(q, out)
         heads = q.shape[1]
         q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
         out = _like(q) if out is None else _into(out, "out", q.shape, q.dtype, self.device)

@@ -218,3 +218,23 @@ def test_results_of_another_stream_outlive_it(serve):
         torch.cuda.synchronize()
         assert torch.equal(kept, want)
         del busy
+
+
+def test_operands_that_require_a_gradient_are_refused(serve):
+    codes, scales, z, _ = _weights(64, 128, 64, torch.bfloat16, True, 45)
+    W = serve.W4Weight(codes.cuda(), scales.cuda(), z.cuda())
+    c = Case(serve, [20], [2], heads=2, D=64, G=32, dt="bf16", seed=46)
+    c.fill(1)
+    b, (cos, sin) = c.batch(), serve.rope_table(32, 64)
+    plain = lambda *shape: torch.randn(*shape, generator=c.gen).bfloat16().cuda()
+    x, bias, k, q = plain(3, 128), plain(64), plain(2, 2, 64), plain(2, 4, 64)
+    asked = lambda t: t.clone().requires_grad_()
+    calls = [lambda f: W.matmul(f(x)), lambda f: W.matmul(x, bias=f(bias)), lambda f: W.matmul(f(x)[0]), lambda f: c.cache.append(b, f(k), k),
+             lambda f: c.cache.append(b, k, f(k)), lambda f: c.cache.append(b, k, k, cos=cos, sin=sin, q=f(q)), lambda f: c.cache.attention(b, f(q))]
+    for call in calls:
+        with pytest.raises(ValueError):
+            call(asked)
+        want = call(lambda t: t)
+        with torch.no_grad():
+            got = call(asked)
+        assert want is got is None or torch.equal(got, want)
