@@ -125,6 +125,13 @@ def _require(ok: bool, what: str):
         raise ValueError(what)
 
 
+def _int32(x, name):
+    """x for a field of 32 bits, which would take a larger number without its upper bits."""
+    x = int(x)
+    _require(-2 ** 31 <= x < 2 ** 31, f"{name}: a number of 32 bits is wanted")
+    return x
+
+
 def _no_gradient(*tensors):
     """The operators have no backward: a result without a gradient would lose it silently."""
     if torch.is_grad_enabled():
@@ -249,7 +256,8 @@ class KV4Batch:
         self.tensors, self.device = (q_start, kv_len, page_table), kv_len.device
         self._ws_bytes = {}   # of attention, by query heads, window and the cache's shape: a function of the sizes
         self.rows = int(rows)
-        self.raw = Batch(n, int(max_new), int(max_kv), self.rows, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+        _require(-2 ** 63 <= self.rows < 2 ** 63, "rows: a number of 64 bits is wanted")
+        self.raw = Batch(n, _int32(max_new, "max_new"), _int32(max_kv, "max_kv"), self.rows, q_start.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
                          page_table.stride(0), int(page_table.shape[1]))
 
 
@@ -260,7 +268,8 @@ class KV4Cache:
 
     def __init__(self, n_pages, page_size, n_kv_heads, head_dim, group=64, device="cuda"):
         self.device = torch.device(device)
-        self.raw = Cache(int(n_pages), int(page_size), int(n_kv_heads), int(head_dim), int(group), None)
+        self.raw = Cache(_int32(n_pages, "n_pages"), _int32(page_size, "page_size"), _int32(n_kv_heads, "n_kv_heads"),
+                         _int32(head_dim, "head_dim"), _int32(group, "group"), None)
         nb = C.c_size_t()
         _check(mf.lib.mf_kv4_cache_bytes(C.byref(self.raw), C.byref(nb)), "mf_kv4_cache_bytes")
         self.pages = torch.empty(int(nb.value), dtype=torch.uint8, device=self.device)
@@ -352,7 +361,7 @@ class KV4Cache:
         out = _like(q) if out is None else _into(out, "out", q.shape, q.dtype, self.device)
         ls = torch.empty((batch.rows, heads), dtype=torch.float32, device=self.device) if lse else None
         a = AttnArgs(_DTYPES[q.dtype], heads, q.data_ptr(), out.data_ptr(), None if ls is None else ls.data_ptr(), *q.stride()[:2],
-                     *out.stride()[:2], 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), int(window))
+                     *out.stride()[:2], 1.0 / math.sqrt(self.head_dim) if scale is None else float(scale), _int32(window, "window"))
         key = (heads, a.window, self._shape)
         need = batch._ws_bytes.get(key)
         if need is None:

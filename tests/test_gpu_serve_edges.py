@@ -238,3 +238,13 @@ def test_operands_that_require_a_gradient_are_refused(serve):
         with torch.no_grad():
             got = call(asked)
         assert want is got is None or torch.equal(got, want)
+
+
+def test_a_window_past_32_bits_is_refused(serve):
+    c = Case(serve, [40], [1], heads=1, D=64, G=32, dt="bf16", seed=47)
+    c.fill(1)
+    q = torch.randn(1, 1, 64, generator=c.gen).bfloat16().cuda()
+    for window in (2 ** 32, 2 ** 32 + 5, -2 ** 32 + 5, 2 ** 31):
+        with pytest.raises(ValueError):
+            c.cache.attention(c.batch(), q, window=window)
+    assert torch.equal(c.cache.attention(c.batch(), q, window=2 ** 31 - 1), c.cache.attention(c.batch(), q))

@@ -115,3 +115,41 @@ def test_w4_outputs_that_one_launch_takes(n, want):
     assert mf.lib.mf_w4_matmul(C.byref(a), None, 0, None) == want
     if want:
         assert mf.lib.mf_w4_pack(C.byref(d), 1024, 2048, None, 4096, C.c_size_t(1 << 40), None) == want
+
+
+@pytest.mark.parametrize("field", ["n_pages", "page_size", "n_kv_heads", "head_dim", "group"])
+@pytest.mark.parametrize("past", [2 ** 32, -2 ** 32, 2 ** 64])
+def test_sizes_past_32_bits_are_refused(field, past):
+    """Not taken without their upper bits, as which they would be sizes that there are."""
+    sizes = dict(n_pages=4, page_size=16, n_kv_heads=2, head_dim=64, group=32)
+    with pytest.raises(ValueError):
+        serve.KV4Cache(**{**sizes, field: sizes[field] + past})
+
+
+class Ints:
+    """As much of an int32 tensor as a batch asks of one."""
+    dtype, is_cuda, device = torch.int32, True, torch.device("cuda", 0)
+
+    def __init__(self, *shape):
+        self.shape = torch.Size(shape)
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self, d):
+        return self.shape[1] if d == 0 else 1
+
+    def data_ptr(self):
+        return 4096
+
+
+@pytest.mark.parametrize("sizes", [dict(max_new=2 ** 32 + 1), dict(max_kv=2 ** 32 + 20), dict(rows=2 ** 64 + 1), dict(max_new=2 ** 31)])
+def test_a_batch_past_32_bits_is_refused(monkeypatch, sizes):
+    monkeypatch.setattr(serve, "isinstance", lambda t, kind: type(t) is Ints if kind is torch.Tensor else isinstance(t, kind), raising=False)
+    good = dict(rows=1, max_new=1, max_kv=20)
+    assert serve.KV4Batch(Ints(2), Ints(1), Ints(1, 4), **good).raw.max_kv == 20
+    with pytest.raises(ValueError):
+        serve.KV4Batch(Ints(2), Ints(1), Ints(1, 4), **{**good, **sizes})
