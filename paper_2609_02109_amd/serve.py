@@ -98,22 +98,21 @@ def _on(device, stream, tensors, call):
     return got
 
 
-class _Workspaces:
-    """Device workspaces, one per (thread, stream) and device: calls that overlap must not share one.
-    A call that is captured gets one of its own from the graph's pool: the graph holds its address for good,
-    and a larger one may take the held one's place."""
+class _Workspaces(threading.local):
+    """Device workspaces, one per stream and device of a thread, which hands them back when it ends: calls that overlap
+    must not share one.  A call that is captured gets one of its own from the graph's pool: the graph holds its address
+    for good, and a larger one may take the held one's place."""
 
     def __init__(self):
-        self._held, self._lock = {}, threading.Lock()
+        self._held = {}
 
     def get(self, nbytes: int, device):
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
-        key = (threading.get_ident(), device, _stream_of(device))
-        with self._lock:
-            ws = self._held.get(key)
-            if ws is None or ws.numel() < nbytes:
-                ws = self._held[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        key = (device, _stream_of(device))
+        ws = self._held.get(key)
+        if ws is None or ws.numel() < nbytes:
+            ws = self._held[key] = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return ws
 
 

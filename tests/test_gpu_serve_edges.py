@@ -15,7 +15,9 @@ type (2^-8 bfloat16, 2^-11 binary16):
   2^-24 (2^-23 where an instruction cuts off) each stand above any product:
   u |y| + 2^-18 31 sum |x| s, and 64 more of the sum so far, 2^-18 of max |sum| <= sum |x s (c - z)|.
 """
+import gc
 import math
+import threading
 
 import pytest
 import torch
@@ -248,3 +250,20 @@ def test_a_window_past_32_bits_is_refused(serve):
         with pytest.raises(ValueError):
             c.cache.attention(c.batch(), q, window=window)
     assert torch.equal(c.cache.attention(c.batch(), q, window=2 ** 31 - 1), c.cache.attention(c.batch(), q))
+
+
+def test_a_thread_hands_its_workspaces_back(serve):
+    """Calls of threads that end leave nothing behind; the thread that goes on keeps its own."""
+    c = Case(serve, [3000, 2500], [1, 1], heads=2, D=64, G=32, page=16, dt="bf16", seed=48)
+    c.fill(1)
+    q, b = torch.randn(2, 4, 64, generator=c.gen).bfloat16().cuda(), c.batch()
+    want = c.cache.attention(b, q)
+    assert max(b._ws_bytes.values()) > 0
+    torch.cuda.synchronize()
+    before, got = torch.cuda.memory_allocated(), []
+    for _ in range(8):
+        t = threading.Thread(target=lambda: got.append(torch.equal(c.cache.attention(b, q), want)))
+        t.start()
+        t.join()
+    gc.collect()
+    assert got == [True] * 8 and torch.cuda.memory_allocated() == before
