@@ -150,6 +150,82 @@ def test_attention_of_small_values_beside_a_heavy_token(serve, size, dt, kv, new
     check(c, per, q, out, lse)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("kv,new,per", [([700], [1], 4), ([9000], [1], 2), ([1500], [40], 2)])
+def test_attention_of_large_values(serve, dt, kv, new, per):
+    """Values of 30 to binary16's largest, in some tokens and some groups only, the largest late; one heavy token before them."""
+    for powers in (0, 10):
+        c = Case(serve, kv, new, heads=1, D=128, G=32, page=64, dt=dt, seed=35)
+        q = _sink(c, 3, powers, per)
+        n = kv[0]
+        for pos, size, dims in ((5, 30.0, slice(0, 32)), (n // 3, 700.0, slice(0, 128)), (n // 2, 9000.0, slice(64, 96)), (n - 50, 65504.0, slice(32, 64))):
+            c.v[0][pos, :, dims] = ((c.v[0][pos, :, dims].float() * size).clamp(-65504, 65504)).to(DT[dt])
+        c.v[0][n // 2:, :, 96:] = (c.v[0][n // 2:, :, 96:].float() * 1e-4).to(DT[dt])
+        c.fill(1)
+        out, lse = c.cache.attention(c.batch(), q.cuda(), lse=True)
+        check(c, per, q, out, lse)
+
+
+# ------------------------------------------------------------- many sequences
+
+@pytest.mark.parametrize("n", [65, 128, 130])
+def test_attention_of_many_sequences(serve, n):
+    """Shares that go over more than 64 sequences, with empty ones where the lanes wrap round; heads that end inside shares."""
+    gen = _gen(n)
+    kv = [int(x) for x in torch.randint(1, 90, (n,), generator=gen)]
+    new = [1] * n
+    for i in (7, 63, 64, n - 1):
+        kv[i] = 0
+    if n > 65:
+        kv[65] = 0
+    kv[3], kv[n // 2], kv[n - 2] = 5000, 2600, 4400
+    new[9] = new[62] = 0
+    c = Case(serve, kv, new, heads=1, D=64, G=32, page=64, dt="bf16", seed=36)
+    c.fill(1)
+    q = torch.randn(sum(new), 3, 64, generator=c.gen).bfloat16()
+    out, lse = c.cache.attention(c.batch(), q.cuda(), lse=True)
+    check(c, 3, q, out, lse)
+    empty = [sum(new[:i]) for i in range(n) if new[i] and not kv[i]]
+    assert (out[empty] == 0).all() and (lse[empty] == -math.inf).all()
+    out, lse = c.cache.attention(c.batch(), q.cuda(), lse=True, window=2000)
+    check(c, 3, q, out, lse, window=2000)
+
+
+def test_attention_of_a_chunk_beside_long_decodes(serve):
+    """A batch of one prompt's chunk, single tokens over long contexts and drafts of nine."""
+    c = Case(serve, [600, 9000, 5, 3333, 0, 800], [300, 1, 1, 9, 0, 1], heads=2, D=64, G=64, page=64, dt="f16", seed=37)
+    c.fill(1)
+    q = torch.randn(312, 4, 64, generator=c.gen).half()
+    out, lse = c.cache.attention(c.batch(), q.cuda(), lse=True)
+    check(c, 2, q, out, lse)
+
+
+# ------------------------------------------------------------------- products
+
+def _check_w4(y, x, w, scales, g, dt):
+    """y against 64 bits, at the tolerance above; -> the same as a truth value, for a y that is off."""
+    x, at = x.double(), torch.arange(w.shape[1]) // g
+    want = x @ w.T
+    tol = UNIT[dt] * want.abs() + 2.0 ** -18 * (31 * (x.abs() @ scales.double().abs()[:, at].T) + x.abs() @ w.abs().T)
+    return bool(((y.cpu().double() - want).abs() <= tol).all())
+
+
+W4_LONG = [(1, 40, 16384, 128), (16, 24, 16384, 128), (1, 33, 8224, 32), (16, 17, 10272, 32), (1, 20, 9536, 64), (16, 48, 12352, 64), (5, 31, 8704, 128),
+           (3, 5003, 4128, 32), (20, 200, 8256, 64), (40, 100, 12320, 32), (64, 130, 16384, 128)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("m,n,k,g", W4_LONG)
+def test_w4_over_many_inputs(serve, m, n, k, g, dt):
+    """Every group of the inputs counts: the bound tells a product that lacks any one of them (planted in the plain form)."""
+    codes, scales, z, w = _weights(n, k, g, DT[dt], True, m + n + k)
+    x = torch.randn(m, k, generator=_gen(38)).to(DT[dt])
+    whole = x.double() @ w.T
+    for i in range(0, k, g):
+        assert not _check_w4(whole - x[:, i:i + g].double() @ w[:, i:i + g].T, x, w, scales, g, dt), i
+    assert _check_w4(serve.W4Weight(codes.cuda(), scales.cuda(), z.cuda()).matmul(x.cuda()), x, w, scales, g, dt)
+
+
 # -------------------------------------------------------------------- streams
 
 def _busy():
