@@ -263,28 +263,25 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
         for (int t = 0; t < RT; t++)
 #pragma unroll
             for (int e = 0; e < 4; e++) wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(x.vs[e >> 1].w[2 * g + (e & 1)]));
-        if (odd) {
+        if (odd || !full) {   // nor do scales of tokens that the row does not see
 #pragma unroll
             for (int t = 0; t < RT; t++) {
                 u32x4 scales;
 #pragma unroll
                 for (int e = 0; e < 4; e++) scales[e] = x.vs[e >> 1].w[2 * g + (e & 1)] & (full ? ~0u : seen_pair(see[t], ok, t0, qt, e));
-                up[t][g] = unit_of(scales, w[t]);
-                const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.f, up[t][g]);
+                if (odd) {
+                    up[t][g] = unit_of(scales, w[t]);
+                    const _Float16 f = (_Float16)__builtin_amdgcn_ldexpf(1.f, up[t][g]);
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * (bits<f16x2>(scales[e]) * (f16x2){f, f}));
+                    for (int e = 0; e < 4; e++) scales[e] = bits<uint32_t>(bits<f16x2>(scales[e]) * (f16x2){f, f});
 #pragma unroll
-                for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
+                    for (int d = g * (G / 16); d < (g + 1) * (G / 16); d++)
 #pragma unroll
-                    for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], up[t][g]);
+                        for (int r = 0; r < 4; r++) st.o[t][d][r] = __builtin_amdgcn_ldexpf(st.o[t][d][r], up[t][g]);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; e++) wg[t][e] = bits<uint32_t>(bits<f16x2>(w[t][e]) * bits<f16x2>(scales[e]));
             }
-        }
-        if (!full) {   // nor do scales of tokens that the row does not see
-#pragma unroll
-            for (int t = 0; t < RT; t++)
-#pragma unroll
-                for (int e = 0; e < 4; e++) wg[t][e] &= seen_pair(see[t], ok, t0, qt, e);
         }
 #pragma unroll
         for (int i = g * IPG; i < (g + 1) * IPG; i++) {
