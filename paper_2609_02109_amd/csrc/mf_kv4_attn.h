@@ -479,7 +479,8 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
             for (int j = 0; j < 4; j++)
                 q[t][d][j] = pack2<F16>(__builtin_amdgcn_ldexpf(to_float<F16>((uint16_t)q[t][d][j]), up - 4 * (j & 1)),
                                         __builtin_amdgcn_ldexpf(to_float<F16>((uint16_t)(q[t][d][j] >> 16)), up - 4 * (j & 1)));
-        c[t] = __builtin_amdgcn_ldexpf(a.scale_log2 / kQueryUnit<F16>, L);
+        // never 0: times the score of a token that is not seen, minus infinity, that would be a NaN
+        c[t] = fmaxf(__builtin_amdgcn_ldexpf(a.scale_log2 / kQueryUnit<F16>, L), 0x1p-126f);
         f16x4 piece = {(_Float16)0.f, (_Float16)0.f, (_Float16)0.f, (_Float16)0.f};
 #pragma unroll
         for (int g = 0; g < NG; g++) {

@@ -343,3 +343,15 @@ def test_a_thread_hands_its_workspaces_back(serve):
         t.join()
     gc.collect()
     assert got == [True] * 8 and torch.cuda.memory_allocated() == before
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("kv,new,per", [([90, 37], [1, 1], 4), ([2500, 37], [1, 1], 2), ([150], [60], 3)])
+def test_attention_of_tiny_queries_and_scales(serve, dt, kv, new, per):
+    """Scores that are all nearly the same, up to queries of zero and the smallest scales: every token weighs alike."""
+    c = Case(serve, kv, new, heads=1, D=64, G=32, page=16, dt=dt, seed=49)
+    c.fill(1)
+    q = torch.randn(sum(new), per, 64, generator=c.gen).to(DT[dt])
+    for x, scale in ((q * 0, 0.125), (q * 0, 1e-12), (q * 0, 1e-38), (q, 1e-12), (q, 1e-38), (q, 1e-45), (q * 2.0 ** -12, 1e-30)):
+        out, lse = c.cache.attention(c.batch(), x.cuda(), lse=True, scale=scale)
+        check(c, per, x, out, lse, scale=scale)
