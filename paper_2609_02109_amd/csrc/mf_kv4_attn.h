@@ -234,13 +234,20 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
 #pragma unroll
         for (int i = 0; i < 8; i++) st.l[t] += e[t][i];
     u32x4 vo = {x.vo[0][0], x.vo[0][1], x.vo[1][0], x.vo[1][1]};
+    u16x2 turned = {0, 0};   // above kPlain where some row sees a scale that is not plain
+#pragma unroll
+    for (int g = 0; g < NG; g++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) turned = __builtin_elementwise_max(turned, plainness(x.vs[e >> 1].w[2 * g + (e & 1)]));
     if (!full) {
         // what no row sees may be anything, not a number too; a zero weight does not make it zero
+        turned = (u16x2){0, 0};
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            const int tok = t0 + 16 * (e >> 1) + 4 * qt + 2 * (e & 1);
-            const bool page = ok >> (e >> 1) & 1;
-            vo[e] &= (page && tok >= all.lo && tok <= all.hi ? 0xffffu : 0u) | (page && tok + 1 >= all.lo && tok + 1 <= all.hi ? 0xffff0000u : 0u);
+            const uint32_t seen = seen_pair(all, ok, t0, qt, e);
+            vo[e] &= seen;
+#pragma unroll
+            for (int g = 0; g < NG; g++) turned = __builtin_elementwise_max(turned, plainness(x.vs[e >> 1].w[2 * g + (e & 1)] & seen));
         }
     }
 #pragma unroll
@@ -249,11 +256,6 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
     // none; both are rare.  Where a row sees one, the group's scales of this step and the sums that the products go
     // into are taken 2^up times, and the sums back: per row, and of the scales that the row sees, so that no row's
     // result depends on anything else.
-    u16x2 turned = {0, 0};
-#pragma unroll
-    for (int g = 0; g < NG; g++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) turned = __builtin_elementwise_max(turned, plainness(x.vs[e >> 1].w[2 * g + (e & 1)]));
     const bool odd = __any(max(turned[0], turned[1]) > kPlain);
     int up[RT][NG];
 #pragma unroll
