@@ -131,12 +131,10 @@ def _int32(x, name):
     return x
 
 
-def _no_gradient(*tensors):
-    """The operators have no backward: a result without a gradient would lose it silently."""
+def _no_gradient():
+    """For an operand that requires a gradient: the operators have no backward, and a result without one would lose it silently."""
     if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("an operand requires a gradient, and there is none through this call: torch.no_grad() or detach() is wanted")
+        raise ValueError("an operand requires a gradient, and there is none through this call: torch.no_grad() or detach() is wanted")
 
 
 def _rows(t, name, shape, dtype, device):
@@ -155,6 +153,8 @@ def _into(t, name, shape, dtype, device):
     """An output of the caller's."""
     _require(isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device
              and (t.stride(-1) == 1 or t.shape[-1] <= 1), f"{name}: {tuple(shape)} {dtype} on {device} with a contiguous last dimension is wanted")
+    if t.requires_grad:
+        _no_gradient()
     return t
 
 
@@ -205,7 +205,10 @@ class W4Weight:
         if bias is not None:
             _require(bias.dtype is self.dtype and bias.device == self.device and tuple(bias.shape) == (self.n_out,)
                      and bias.is_contiguous(), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
-        _no_gradient(x, bias, out)
+            if bias.requires_grad:
+                _no_gradient()
+        if x.requires_grad:
+            _no_gradient()
         if len(lead) != 1:
             x = x.reshape(-1, self.n_in)
         m = x.shape[0]
@@ -285,6 +288,7 @@ class KV4Cache:
         tokens and of tokens of a sequence, known on the host."""
         b = KV4Batch(q_start, kv_len, page_table, rows, max_new, max_kv)
         _require(all(t.device == self.device for t in b.tensors), f"the batch's tensors: on {self.device} is wanted")
+        b.device = self.device
         return b
 
     def _beside(self, batch):
@@ -296,11 +300,13 @@ class KV4Cache:
         turned by their positions when cos / sin [n_pos, rot_dim // 2] are given;
         with q [rows, n_heads, head_dim] also returns the queries turned the
         same way (q_out: where to, e.g. q itself)."""
-        self._beside(batch)
+        if batch.device is not self.device:
+            self._beside(batch)
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (k, v, cos, sin, q, q_out, self.pages, batch.tensors),
                        lambda: self.append(batch, k, v, cos, sin, q, interleaved, q_out))
-        _no_gradient(k, v, q, q_out)
+        if k.requires_grad or v.requires_grad:
+            _no_gradient()
         dt, dev = k.dtype, self.device
         _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
         shape = (batch.rows, self.n_kv_heads, self.head_dim)
@@ -321,6 +327,8 @@ class KV4Cache:
             else:
                 _require(q.dim() == 3, "q: [rows, n_heads, head_dim] is wanted")
                 heads = q.shape[1]
+                if q.requires_grad:
+                    _no_gradient()
                 q = _rows(q, "q", (batch.rows, heads, self.head_dim), dt, dev)
                 q_out = _like(q) if q_out is None else _into(q_out, "q_out", q.shape, dt, dev)
                 qs, os = q.stride(), q_out.stride()
@@ -333,7 +341,8 @@ class KV4Cache:
 
     def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
         """(keys, values) [rows, n_kv_heads, head_dim] that the cache holds for the batch's rows."""
-        self._beside(batch)
+        if batch.device is not self.device:
+            self._beside(batch)
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (self.pages, batch.tensors), lambda: self.read(batch, dtype))
         _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
@@ -350,11 +359,13 @@ class KV4Cache:
         tokens: [rows, n_heads, head_dim], with lse=True also the log of the
         softmax sums [rows, n_heads] float32.  scale: 1 / sqrt(head_dim) by
         default; window > 0: only the newest `window` tokens up to each row's."""
-        self._beside(batch)
+        if batch.device is not self.device:
+            self._beside(batch)
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (q, out, self.pages, batch.tensors), lambda: self.attention(batch, q, scale, window, lse, out))
         _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
-        _no_gradient(q, out)
+        if q.requires_grad:
+            _no_gradient()
         heads = q.shape[1]
         q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
         out = _like(q) if out is None else _into(out, "out", q.shape, q.dtype, self.device)
