@@ -524,7 +524,9 @@ mf_status mf_kv4_read(const mf_kv4_cache *cache, const mf_kv4_batch *batch, mf_d
  * out = sum_j softmax(scale q.k_j) v_j, lse = log sum_j exp(scale q.k_j).  A row
  * that sees no token gives 0 and -inf; a NaN in a token that a row sees makes the
  * row NaN.  Sums and softmax in fp32; the weights of the values, alone and times
- * their scales, are rounded to binary16.  Deterministic. */
+ * their scales, are rounded to binary16 (down to 2^-34 of a row's largest).
+ * Deterministic: no bit of a row's result depends on tokens that it does not see,
+ * nor on what the pages hold beside the tokens of its sequence. */
 typedef struct {
     mf_dtype dtype;         /* MF_BF16 or MF_F16: of q and out */
     int32_t n_heads;        /* a multiple of n_kv_heads, at most 4096 */

@@ -617,9 +617,9 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
     }
 }
 
-// By rows (many query tokens; bound by vector instructions, 70 % of the SIMDs' cycles
-// beside 32 % of matrix ones: 2 x 1024 query tokens of 32 heads over 12345 tokens take 567 us,
-// 693 TFLOP/s; a third tile of rows a wave would share the codes' work further and has no
+// By rows (many query tokens; bound by vector instructions, 68 % of the SIMDs' cycles
+// beside 34 % of matrix ones: 2 x 1024 query tokens of 32 heads over 12345 tokens take 545 us,
+// 721 TFLOP/s; a third tile of rows a wave would share the codes' work further and has no
 // registers): a workgroup takes a tile of attn_rows rows, its
 // waves 16 RT of them each, over a part of their tokens.
 template <bool F16, int D, int G, int RT>
@@ -639,10 +639,10 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn_rows_kernel(KvAttnArg
 }
 
 // By tokens (few rows: 16 RT at most of a sequence and key head; long contexts are bound by
-// the cache's bytes, 2 x 131072 tokens of 8 heads of 128 in 50 us of kernel, 5.3 TB/s; ragged
-// batches by the items' beginnings and ends too, 32 requests of up to 16384 in 85 us, 3.8 TB/s;
-// one short request by the chain of one wave's steps, 1000 tokens in 10.4 us: with a second step
-// on its way ahead 11.4, with 16 waves 19): the waves of a
+// the cache's bytes, 2 x 131072 tokens of 8 heads of 128 in 51 us of kernel, 5.4 TB/s; ragged
+// batches by the items' beginnings and ends too, 32 requests of up to 16384 in 85 us beside a join
+// of 6, 3.8 TB/s; one short request by the chain of one wave's steps, 1000 tokens in 11 us: a second
+// step on its way ahead and 16 waves were both slower): the waves of a
 // workgroup take every fourth step each.  Whole: a workgroup per sequence and
 // head.  Otherwise a.workgroups of them, as many as the card holds, take equal
 // shares of all sequences' tokens: a share may end inside a head, whose parts

@@ -40,10 +40,14 @@ KvPlan kv4_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window)
         p.slot_rows = wg_rows;
     } else {
         p.row_tiles = 1;
-        // Whole heads have neither shares to find nor parts to join, which is some 10 us,
-        // but the longest decides (own heads of 64, 16 x 16 of them, up to 4000 tokens: 22.8
-        // us, shares 21.8; one request of 8 heads and 1000 tokens: 10.5 and 11.5, of 4000:
-        // 23.5 and 11.9; 200 x 8 heads of up to 600: 27 and 59).
+        // Whole heads have neither shares to find nor parts to join, which is 3 us and more,
+        // but the longest decides.  us, whole and in shares, heads of 128 and one length:
+        //   1 x 8 of 1000: 11.0, 12.2; of 1500: 12.9, 12.6; of 4000: 22.7, 12.2
+        //   16 x 8 of 2000: 16.5, 22.3; of 3000: 20.8, 21.4; of 6000: 32.1, 31.1
+        //   16 x 16 of 4000: 27.2, 36.7; 200 x 8 of 500: 29, 56; of 2000: 94, 120
+        // (heads of 64, 16 x 16 of all lengths up to 4000: 19.8, 25.4).  Past 4096 tokens many
+        // heads of one length would still be faster whole (16 x 16 of 6000: 37.1, 46.4), of all
+        // lengths hardly (31.8, 33.7).
         const long long longest = heads * 16 < 1024 ? 1024 : heads * 16 < 4096 ? heads * 16 : 4096;
         p.whole = span <= longest;
         if (p.whole) {

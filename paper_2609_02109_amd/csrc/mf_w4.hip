@@ -409,8 +409,10 @@ hipError_t launch_w4_pack(const W4PackArgs &a, hipStream_t s)
 //   4096 x 4096: 3.9, 16 waves 4.2; but 16 where few tiles have many inputs: 16 x 4096 x
 //   16384: 15.0, 8 waves 16.6).  Past 4 rows and 1024 tiles it is the rows, read again for
 //   every tile, that count: four tiles (16 x 28672 x 4096: 15.5, one 21.9).
-// * up to 32 rows of small layers the same with two tiles of rows (32 x 1024 x 4096: 5.9,
-//   by rows 9.2; 32 x 8192 x 8192: 22 and 18).
+// * up to 32 rows of small layers the same with two tiles of rows (groups of 64, this way
+//   and by rows, up to the limit: 32 x 1024 x 4096: 6.4, 9.6; 32 x 4096 x 4096: 7.2, 11.1;
+//   past it: 32 x 4096 x 8192: 11.1, 13.7; 32 x 8192 x 4096: 12.2, 12.5; 32 x 2048 x 16384:
+//   17.4, 15.8; 32 x 8192 x 8192: 21.9, 16.6).
 // * otherwise by rows, two tiles of outputs a wave where that leaves workgroups enough (64 x
 //   32768 x 8192: 57, one 66; 512 x 8192 x 8192: 84, one 108; 64 x 4096 x 4096: 16, two 20), the inputs in as many parts as give every
 //   compute unit a workgroup (32 x 8192 x 8192 in 4: 18, whole 40).

@@ -104,8 +104,8 @@ def _option(n, context, steps, decoder):
 
 
 def options(concurrency, context, steps=20, **decoder):
-    """One dict per concurrency: ms a step (captured in a graph, all sequences at full context), tokens/s, GB.
-    One model at a time is on the device."""
+    """One dict per concurrency: ms a step (captured in a graph, all sequences at full context; torch's elementwise
+    operations between the operators are part of it), tokens/s, GB.  One model at a time is on the device."""
     return [_option(n, context, steps, decoder) for n in concurrency]
 
 
