@@ -355,3 +355,33 @@ def test_attention_of_tiny_queries_and_scales(serve, dt, kv, new, per):
     for x, scale in ((q * 0, 0.125), (q * 0, 1e-12), (q * 0, 1e-38), (q, 1e-12), (q, 1e-38), (q, 1e-45), (q * 2.0 ** -12, 1e-30)):
         out, lse = c.cache.attention(c.batch(), x.cuda(), lse=True, scale=scale)
         check(c, per, x, out, lse, scale=scale)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_attention_of_values_of_any_size(serve, seed):
+    """Every token and group of its own size, 2^-20 to 2^15, some of zeros, under sharp and flat weights: as above, and
+    half of the smallest weight that is held, 2^-35 of a row's largest."""
+    gen = _gen(1000 + seed)
+    pick = lambda *v: v[int(torch.randint(0, len(v), (1,), generator=gen))]
+    D, G = SHAPES[seed % len(SHAPES)]
+    kv, new, per = pick(([700, 33], [1, 2], 4), ([5000, 40], [1, 1], 2), ([300, 64], [40, 9], 3))
+    c = Case(serve, kv, new, heads=2, D=D, G=G, page=pick(16, 64), dt=pick("bf16", "f16"), seed=50 + seed)
+    for v in c.v:
+        size = 2.0 ** (35 * torch.rand(*v.shape[:2], D // G, generator=gen) - 20) * (torch.rand(*v.shape[:2], D // G, generator=gen) > 0.1)
+        v.copy_((v.float().clamp(-2, 2).unflatten(-1, (-1, G)) / 2 * size[..., None]).flatten(-2).to(v.dtype))
+    c.fill(pick(1, 2))
+    q = (pick(0.1, 1.0, 4.0) * torch.randn(sum(new), 2 * per, D, generator=gen)).to(DT[c.dt])
+    window = pick(0, 0, 100)
+    out = c.cache.attention(c.batch(), q.cuda(), window=window).cpu().double()
+    at = 0
+    for i, n in enumerate(new):
+        k, _ = _parts(c.k[i], G)
+        v, off = _parts(c.v[i], G)
+        o, _, p = plain_attention(q[at:at + n], k, v, per, n, window, 1 / math.sqrt(D))
+        for h in range(2 * per):
+            mass, offs, top = p[:, h] @ v[:, h // per].abs(), p[:, h] @ off[:, h // per], p[:, h].amax(-1, keepdim=True)
+            floor = 2.0 ** -35 * top * ((p[:, h] > 0).double() @ (v[:, h // per].abs() + off[:, h // per]))
+            tol = UNIT[c.dt] * o[:, h].abs() + 2.0 ** -10 * (mass + offs) + 2.0 ** -13 * mass + floor + (2.0 ** -25 if c.dt == "f16" else 0) + 1e-30
+            err = (out[at:at + n, h] - o[:, h]).abs()
+            assert (err <= tol).all(), (i, h, float((err / tol).max()))
+        at += n
