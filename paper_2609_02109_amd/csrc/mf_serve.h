@@ -26,7 +26,7 @@ constexpr long long most_workgroups(int threads) { return ((1ll << 32) - 1) / th
 // l % 16, the A operand of v_mfma_f32_16x16x32 number i.  Outputs past N and
 // inputs past K have code 0 and scale 0.
 constexpr int kW4Tile = 16, kW4Chunk = 128, kW4Codes = 1024;
-// a workgroup of 512 threads a tile at most, in one launch
+// a workgroup of 512 threads a tile at most (1024 only where there are few tiles), in one launch
 constexpr long long kW4MostOut = most_workgroups(512) * kW4Tile;
 static_assert(kW4MostOut == (1ll << 27) - 16, "as include/mf.h has it");
 __host__ __device__ constexpr int w4_record(int group) { return kW4Codes + (kW4Chunk / group) * 64; }
