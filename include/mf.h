@@ -544,6 +544,96 @@ mf_status mf_kv4_workspace_size(const mf_kv4_cache *cache, const mf_kv4_batch *b
 mf_status mf_kv4_attention(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args,
                            void *d_ws, size_t ws_bytes, void *stream);
 
+/* --- an 8-bit variant's step
+ *
+ * Between an option's 16-bit and 4-bit variants: weights, activations and cache
+ * in 8 bits.  A row in 8 bits is codes -127..127 and a scale in fp32; the value
+ * that a code stands for is scale * code. */
+
+/* --- rows in 8 bits
+ *
+ * y, computed in fp32 from a row of T (MF_BF16 or MF_F16), is held as
+ *   top = max |y|, scale = top * (float)(1 / 127.) (0 where that is below 2^-126),
+ *   code = rint(y * (1 / scale)) limited to -127..127 (0 where scale is 0),
+ * each step rounded.  A row whose y has an infinity or a NaN has a NaN as its
+ * scale and codes 0, so that whatever it is multiplied with is NaN. */
+typedef struct {
+    mf_dtype dtype;         /* of x, and what else an operator reads and writes in 16 bits */
+    int64_t rows;           /* 0 (nothing is done) .. 2^30 */
+    int64_t n;              /* values of a row, 1 .. 2^17 */
+    const void *d_x;        /* [rows][n], row stride x_stride >= n */
+    int64_t x_stride;
+    int8_t *d_codes;        /* [rows][n], row stride codes_stride >= n */
+    int64_t codes_stride;
+    float *d_scales;        /* [rows] */
+} mf_rows8_args;
+
+/* y = x. */
+mf_status mf_rows8(const mf_rows8_args *args, void *stream);
+
+/* The root-mean-square norm, of x with a residual added to it:
+ *   h = T(x + residual) (x without one), r = 1 / sqrt(sum h^2 / n + eps), y = (h r) weight.
+ * The sum is in fp32; a row whose squares leave fp32 is as one with an infinity. */
+typedef struct {
+    mf_rows8_args row;
+    const void *d_residual; /* [rows][n], row stride residual_stride >= n, or NULL */
+    int64_t residual_stride;
+    void *d_sum;            /* h, with a residual only: [rows][n], row stride sum_stride >= n; may be d_x or
+                               d_residual itself with the same stride, else over neither */
+    int64_t sum_stride;
+    const void *d_weight;   /* [n] */
+    float eps;              /* finite, >= 0 */
+} mf_norm8_args;
+mf_status mf_norm8(const mf_norm8_args *args, void *stream);
+
+/* The gate: y = x / (1 + exp(-x)) * up. */
+typedef struct {
+    mf_rows8_args row;
+    const void *d_up;       /* [rows][n], row stride up_stride >= n */
+    int64_t up_stride;
+} mf_gate8_args;
+mf_status mf_gate8(const mf_gate8_args *args, void *stream);
+
+/* What rows stand for, rounded to dtype (MF_F32, MF_BF16 or MF_F16): d_out [rows][n], row stride out_stride >= n. */
+mf_status mf_rows8_values(mf_dtype dtype, int64_t rows, int64_t n, const int8_t *d_codes, int64_t codes_stride,
+                          const float *d_scales, void *d_out, int64_t out_stride, void *stream);
+
+/* --- products with 8-bit weights
+ *
+ * y[m][n] = (sum_k x[m][k] w[n][k]) xs[m] ws[n] + bias[n]: the sum of products of
+ * codes is exact, what follows is in fp32, each step rounded, and rounded to dtype
+ * at the end.  Codes may be -128 too.  Rows that come in 16 bits are put into 8
+ * on the way, as by mf_rows8. */
+typedef struct {
+    int64_t n_out, n_in;    /* 1 <= N <= 2^27 - 16, 16 <= K <= 131056, K a multiple of 16 */
+    mf_dtype dtype;         /* MF_BF16 or MF_F16: of bias, y and x where it is not in 8 bits */
+} mf_w8_desc;
+
+/* Bytes of the packed weights. */
+mf_status mf_w8_pack_bytes(const mf_w8_desc *desc, size_t *bytes);
+
+/* Lays weights out for mf_w8_matmul, once, when they are loaded.  d_codes: int8
+ * [N][K]; d_scales: float [N].  d_packed: mf_w8_pack_bytes, 256-byte aligned. */
+mf_status mf_w8_pack(const mf_w8_desc *desc, const int8_t *d_codes, const float *d_scales, void *d_packed, size_t packed_bytes,
+                     void *stream);
+
+typedef struct {
+    mf_w8_desc w;
+    const void *d_packed;   /* as mf_w8_pack wrote it */
+    const void *d_x;        /* [rows][K], row stride x_stride >= K: codes, or values of dtype where d_x_scales is NULL */
+    const float *d_x_scales;/* [rows] or NULL */
+    const void *d_bias;     /* [N] or NULL */
+    void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x */
+    int64_t rows;           /* 0 (nothing is done) .. 2^20 */
+    int64_t x_stride, y_stride;
+} mf_w8_args;
+
+/* Bytes of workspace (possibly 0), a function of the sizes and of whether x is in 8 bits. */
+mf_status mf_w8_workspace_size(const mf_w8_args *args, size_t *bytes);
+
+/* Any number of rows.  Deterministic.  d_ws: mf_w8_workspace_size bytes, 256-byte aligned; need not be initialised. */
+mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void *stream);
+
 /* Human-readable status name. */
 const char *mf_status_string(mf_status s);
 

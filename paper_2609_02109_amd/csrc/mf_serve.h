@@ -1,6 +1,7 @@
 // Shared by the operators of the served steps (mf_w4.hip, mf_kv4.hip,
-// mf_kv4_attn*.hip, mf_serve_api.cpp): the layouts of the packed weights and of
-// the 4-bit cache, kernel argument blocks, launchers.
+// mf_kv4_attn*.hip, mf_rows8.hip, mf_w8.hip, mf_kv8.hip, mf_kv8_attn*,
+// mf_serve_api.cpp, mf_serve8_api.cpp): the layouts of the packed weights and of
+// the caches, kernel argument blocks, launchers.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -158,5 +159,62 @@ KvPlan kv4_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window);
 hipError_t launch_kv4_append(const KvAppendArgs &a, bool f16, hipStream_t s);
 hipError_t launch_kv4_read(const KvReadArgs &a, int dtype, hipStream_t s);
 hipError_t launch_kv4_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
+
+// ------------------------------------------------------------ rows in 8 bits
+enum Rows8Op { kRowsPlain, kRowsNorm, kRowsGate };
+constexpr int kRows8Most = 1 << 17;   // values of a row: 1024 threads of 128
+struct Rows8Args {
+    const void *x, *y;       // y: the residual (may be null) or the gate's factors
+    const void *weight;      // norm
+    void *sum;               // norm with a residual: x + y
+    int8_t *codes;
+    float *scales;
+    long long rows, x_stride, y_stride, sum_stride, codes_stride;
+    int n;
+    float eps;
+};
+hipError_t launch_rows8(const Rows8Args &a, Rows8Op op, bool f16, hipStream_t s);
+struct Values8Args {
+    const int8_t *codes;
+    const float *scales;
+    void *out;
+    long long rows, codes_stride, out_stride;
+    int n;
+};
+hipError_t launch_values8(const Values8Args &a, int dtype, hipStream_t s);
+
+// ------------------------------------------------------- packed 8-bit weights
+// [N / 16][K / 64] records of 1024 bytes: lane l of a wave holds 16 of them, the
+// inputs k = 16 (l / 16) .. + 15 of output l % 16, the A operand of
+// v_mfma_i32_16x16x64_i8.  Outputs past N and inputs past K have code 0.  After
+// the records N scales.
+constexpr int kW8Tile = 16, kW8Chunk = 64, kW8Record = kW8Tile * kW8Chunk;
+constexpr long long kW8MostOut = most_workgroups(512) * kW8Tile;   // as kW4MostOut
+constexpr int kW8MostIn = 131056;   // 2^14 K < 2^31: products of codes down to -128, in 32 bits
+__host__ __device__ constexpr long long w8_chunks(int n_in) { return (n_in + kW8Chunk - 1) / kW8Chunk; }
+struct W8Args {
+    const uint8_t *packed;
+    const float *w_scales;
+    const int8_t *x;
+    const float *x_scales;
+    const void *bias;
+    void *y;
+    long long x_stride, y_stride;
+    int rows, n_out, n_in;
+};
+struct W8PackArgs {
+    const int8_t *codes;
+    const float *scales;
+    uint8_t *packed;
+    int n_out, n_in;
+};
+hipError_t launch_w8_pack(const W8PackArgs &a, hipStream_t s);
+enum W8Form { kW8Few1, kW8Few2, kW8Few4, kW8Tiles };
+struct W8Plan {
+    W8Form form;
+    size_t ws_bytes;
+};
+W8Plan w8_plan(int rows, int n_out, int n_in);
+hipError_t launch_w8(const W8Args &a, const W8Plan &p, bool f16, void *ws, hipStream_t s);
 
 }  // namespace mfs

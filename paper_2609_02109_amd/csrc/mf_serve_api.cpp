@@ -1,42 +1,10 @@
 // C entry points of the served steps' operators: argument checks, sizes, and
 // the kernels' argument blocks.  Nothing here allocates or synchronises.
-#include <hip/hip_runtime.h>
-
-#include <cmath>
-#include <cstdint>
-#include <cstring>
-
-#include "mf_serve.h"
+#include "mf_serve_check.h"
 
 using namespace mfs;
 
 namespace {
-
-// A C caller may pass any int as an enum: read through its representation.
-int as_int(const mf_dtype &d)
-{
-    int v;
-    static_assert(sizeof v == sizeof d, "mf_dtype is int-sized");
-    std::memcpy(&v, &d, sizeof v);
-    return v;
-}
-
-bool half_type(int d) { return d == MF_BF16 || d == MF_F16; }
-bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
-mf_status of(hipError_t e) { return e == hipSuccess ? MF_OK : MF_EDEVICE; }
-
-// Rows of `heads` times D elements at these strides: no two overlap, and the
-// furthest element stays within 2^62 elements.
-bool strides_fit(int64_t rows, int64_t stride, int64_t heads, int64_t head, int64_t d, bool out)
-{
-    const int64_t most = (int64_t)1 << 40;
-    if (stride < 0 || head < 0 || stride > most || head > most) return false;
-    if (!out) return true;
-    // outputs: heads inside rows or rows inside heads
-    if (heads > 1 && head < d) return false;
-    if (rows > 1 && stride < d) return false;
-    return heads <= 1 || rows <= 1 || stride >= (heads - 1) * head + d || head >= (rows - 1) * stride + d;
-}
 
 mf_status check_w4(const mf_w4_desc *d)
 {
@@ -81,34 +49,10 @@ mf_status check_cache(const mf_kv4_cache *c, KvGeom &g)
     return MF_OK;
 }
 
-// The batch of a call; `run`: its device arrays too.
-mf_status check_batch(const mf_kv4_cache *c, const mf_kv4_batch *b, bool run, KvBatch &o)
-{
-    if (!b) return MF_EINVAL;
-    if (b->n_seq < 0 || b->max_new < 0 || b->max_kv < 0 || b->rows < 0 || b->table_cols < 0) return MF_EINVAL;
-    if (b->n_seq > (1 << 20) || b->rows > (1 << 30) || b->max_kv > (1 << 30)) return MF_EUNSUPPORTED;
-    if ((int64_t)b->max_kv > (int64_t)b->table_cols * c->page_size) return MF_EINVAL;
-    if (b->table_stride < 0 || b->table_stride > ((int64_t)1 << 40) || (b->n_seq > 1 && b->table_stride < b->table_cols)) return MF_EINVAL;
-    if (run && b->n_seq > 0 && b->rows > 0) {
-        if (!c->d_pages || !aligned(c->d_pages, 256)) return MF_EINVAL;
-        if (!b->d_q_start || !b->d_kv_len || !aligned(b->d_q_start, 4) || !aligned(b->d_kv_len, 4)) return MF_EINVAL;
-        if (b->table_cols > 0 && (!b->d_page_table || !aligned(b->d_page_table, 4))) return MF_EINVAL;
-    }
-    o.n_seq = b->n_seq;
-    o.max_new = b->max_new < b->rows ? b->max_new : (int)b->rows;
-    o.max_kv = b->max_kv;
-    o.rows = (int)b->rows;
-    o.q_start = b->d_q_start;
-    o.kv_len = b->d_kv_len;
-    o.table = b->d_page_table;
-    o.table_stride = b->table_stride;
-    return MF_OK;
-}
-
 mf_status check_attn(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, bool run, KvAttnArgs &a, KvPlan &p)
 {
     mf_status st = check_cache(cache, a.g);
-    if (st == MF_OK) st = check_batch(cache, batch, run, a.b);
+    if (st == MF_OK) st = check_batch(cache->page_size, cache->d_pages, batch, run, a.b);
     if (st != MF_OK) return st;
     if (!args || !half_type(as_int(args->dtype))) return MF_EINVAL;
     if (args->n_heads < 1 || args->n_heads % cache->n_kv_heads != 0 || args->window < 0) return MF_EINVAL;
@@ -216,7 +160,7 @@ mf_status mf_kv4_append(const mf_kv4_cache *cache, const mf_kv4_batch *batch, co
 {
     KvAppendArgs a;
     mf_status st = check_cache(cache, a.g);
-    if (st == MF_OK) st = check_batch(cache, batch, true, a.b);
+    if (st == MF_OK) st = check_batch(cache->page_size, cache->d_pages, batch, true, a.b);
     if (st != MF_OK) return st;
     if (!args || !half_type(as_int(args->dtype))) return MF_EINVAL;
     const int64_t rows = batch->rows, d = cache->head_dim;
@@ -262,7 +206,7 @@ mf_status mf_kv4_read(const mf_kv4_cache *cache, const mf_kv4_batch *batch, mf_d
 {
     KvReadArgs a;
     mf_status st = check_cache(cache, a.g);
-    if (st == MF_OK) st = check_batch(cache, batch, true, a.b);
+    if (st == MF_OK) st = check_batch(cache->page_size, cache->d_pages, batch, true, a.b);
     if (st != MF_OK) return st;
     const int ty = as_int(dtype);
     if (ty != MF_F32 && !half_type(ty)) return MF_EINVAL;

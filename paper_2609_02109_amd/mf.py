@@ -34,7 +34,9 @@ EXPORTS = ["mf_problem_bytes", "mf_problem_create", "mf_problem_destroy", "mf_sp
            "mf_static_workspace_size", "mf_search_static", "mf_eval_static",
            "mf_ga_workspace_size", "mf_ga_run",
            "mf_w4_pack_bytes", "mf_w4_pack", "mf_w4_workspace_size", "mf_w4_matmul", "mf_kv4_cache_bytes", "mf_kv4_append", "mf_kv4_read",
-           "mf_kv4_workspace_size", "mf_kv4_attention", "mf_status_string"]
+           "mf_kv4_workspace_size", "mf_kv4_attention",
+           "mf_rows8", "mf_norm8", "mf_gate8", "mf_rows8_values", "mf_w8_pack_bytes", "mf_w8_pack", "mf_w8_workspace_size", "mf_w8_matmul",
+           "mf_status_string"]
 
 
 class MfError(RuntimeError):
@@ -143,6 +145,14 @@ def _load():
         "mf_kv4_read": (S, [P, P, S, P, P, P]),
         "mf_kv4_workspace_size": (S, [P, P, P, P]),
         "mf_kv4_attention": (S, [P, P, P, P, C.c_size_t, P]),
+        "mf_rows8": (S, [P, P]),
+        "mf_norm8": (S, [P, P]),
+        "mf_gate8": (S, [P, P]),
+        "mf_rows8_values": (S, [S, C.c_int64, C.c_int64, P, C.c_int64, P, P, C.c_int64, P]),
+        "mf_w8_pack_bytes": (S, [P, P]),
+        "mf_w8_pack": (S, [P, P, P, P, C.c_size_t, P]),
+        "mf_w8_workspace_size": (S, [P, P]),
+        "mf_w8_matmul": (S, [P, P, C.c_size_t, P]),
         "mf_status_string": (C.c_char_p, [S]),
     }
     for name, (res, args) in sig.items():

@@ -1,11 +1,14 @@
-"""The operators of a served model's 4-bit variant, over the C ABI.
+"""The operators of a served model's 4-bit and 8-bit variants, over the C ABI.
 
 The options that a search chooses from are variants (16-bit or 4-bit) and
 runtime parameters of the co-running models.  These are the operators of the
 step that a 4-bit option stands for, to run it or to profile it into an option
 table: products with 4-bit weights (`W4Weight`), and a paged key/value cache
 held in 4 bits (`KV4Cache`) with its append, which turns keys and queries by
-their positions on the way, and its attention.
+their positions on the way, and its attention.  Between the two variants is one
+in 8 bits: products of 8-bit rows with 8-bit weights (`W8Weight`), the steps
+between them whose rows come out in 8 bits (`norm_rows`, `gate_rows`,
+`quantise_rows`), and the same cache and attention in 8 bits (`KV8Cache`).
 
 As in `mf`, this is marshalling only: torch supplies device memory and the
 stream, the kernels of libmf.so do the work.  Calls enqueue on `stream` (None:
@@ -18,6 +21,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import threading
+from typing import NamedTuple
 
 import torch
 
@@ -58,6 +62,29 @@ class AppendArgs(C.Structure):
 class AttnArgs(C.Structure):
     _fields_ = [("dtype", _i32), ("n_heads", _i32), ("d_q", _p), ("d_out", _p), ("d_lse", _p), ("q_stride", _i64),
                 ("q_head_stride", _i64), ("out_stride", _i64), ("out_head_stride", _i64), ("scale", C.c_float), ("window", _i32)]
+
+
+class Rows8Args(C.Structure):
+    _fields_ = [("dtype", _i32), ("rows", _i64), ("n", _i64), ("d_x", _p), ("x_stride", _i64), ("d_codes", _p), ("codes_stride", _i64),
+                ("d_scales", _p)]
+
+
+class Norm8Args(C.Structure):
+    _fields_ = [("row", Rows8Args), ("d_residual", _p), ("residual_stride", _i64), ("d_sum", _p), ("sum_stride", _i64), ("d_weight", _p),
+                ("eps", C.c_float)]
+
+
+class Gate8Args(C.Structure):
+    _fields_ = [("row", Rows8Args), ("d_up", _p), ("up_stride", _i64)]
+
+
+class W8Desc(C.Structure):
+    _fields_ = [("n_out", _i64), ("n_in", _i64), ("dtype", _i32)]
+
+
+class W8Args(C.Structure):
+    _fields_ = [("w", W8Desc), ("d_packed", _p), ("d_x", _p), ("d_x_scales", _p), ("d_bias", _p), ("d_y", _p), ("rows", _i64),
+                ("x_stride", _i64), ("y_stride", _i64)]
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -231,6 +258,192 @@ class W4Weight:
         s = mf.lib.mf_w4_matmul(C.byref(args), ws.data_ptr() if need else None, need, _stream_of(self.device))
         if s:
             _check(s, "mf_w4_matmul")
+        return out
+
+
+def _matrix(t, name, n, dtype, device):
+    """[.., n] as rows of n with a contiguous last dimension (a copy where they are none)."""
+    if not isinstance(t, torch.Tensor) or t.dim() == 0 or t.shape[-1] != n or t.dtype is not dtype or t.device != device:
+        raise ValueError(f"{name}: [.., {n}] {dtype} on {device} is wanted")
+    if t.requires_grad:
+        _no_gradient()
+    if t.dim() != 2:
+        t = t.reshape(-1, n)
+    if t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < n):
+        t = t.contiguous()
+    return t
+
+
+class Rows8(NamedTuple):
+    """Rows in 8 bits: codes int8 [.., N] and a scale float32 [..] for each row; the values are scale * code.
+    Made by `norm_rows`, `gate_rows` and `quantise_rows`, or of tensors at hand."""
+
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def _checked(self):
+        """Codes as a matrix, and the scales."""
+        codes, scales = self
+        _require(isinstance(codes, torch.Tensor) and codes.dtype is torch.int8 and codes.is_cuda and codes.dim() > 0 and codes.shape[-1] > 0,
+                 "codes: an int8 [.., N] tensor on the GPU is wanted")
+        _require(isinstance(scales, torch.Tensor) and scales.dtype is torch.float32 and scales.device == codes.device
+                 and scales.shape == codes.shape[:-1], "scales: float32 [..] beside the codes is wanted")
+        if scales.requires_grad:
+            _no_gradient()
+        return _matrix(codes, "codes", codes.shape[-1], torch.int8, codes.device), scales if scales.is_contiguous() else scales.contiguous()
+
+    def values(self, dtype=torch.float32, stream=None):
+        """What the rows stand for, [.., N] in dtype."""
+        device = self.codes.device
+        if device.type == "cuda" and (stream is not None or device.index != _current_device()):
+            return _on(device, stream, tuple(self), lambda: self.values(dtype))
+        codes, scales = self._checked()
+        _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
+        out = torch.empty(self.codes.shape, dtype=dtype, device=device)
+        n = codes.shape[1]
+        s = mf.lib.mf_rows8_values(_DTYPES[dtype], codes.shape[0], n, codes.data_ptr(), codes.stride(0), scales.data_ptr(), out.data_ptr(), n,
+                                   _stream_of(device))
+        if s:
+            _check(s, "mf_rows8_values")
+        return out
+
+
+def _rows8_of(x, name):
+    """x as a matrix, the Rows8 that it is put into, and the call's arguments."""
+    _require(isinstance(x, torch.Tensor) and x.dtype in _HALF and x.is_cuda and x.dim() > 0 and x.shape[-1] > 0,
+             f"{name}: bfloat16 or float16 [.., N] on the GPU is wanted")
+    m = _matrix(x, name, x.shape[-1], x.dtype, x.device)
+    rows = Rows8(torch.empty(x.shape, dtype=torch.int8, device=x.device), torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device))
+    n = m.shape[1]
+    return m, rows, Rows8Args(_DTYPES[x.dtype], m.shape[0], n, m.data_ptr(), m.stride(0), rows.codes.data_ptr(), n, rows.scales.data_ptr())
+
+
+def _elsewhere(x, stream):
+    """Whether a call with x has to change the current device or stream first."""
+    return stream is not None or (isinstance(x, torch.Tensor) and x.is_cuda and x.device.index != _current_device())
+
+
+def quantise_rows(x, stream=None) -> Rows8:
+    """x [.., N], bfloat16 or float16, in 8 bits."""
+    if _elsewhere(x, stream):
+        return _on(x.device, stream, x, lambda: quantise_rows(x))
+    x, rows, a = _rows8_of(x, "x")
+    s = mf.lib.mf_rows8(C.byref(a), _stream_of(x.device))
+    if s:
+        _check(s, "mf_rows8")
+    return rows
+
+
+def norm_rows(x, weight, residual=None, eps=1e-6, out=None, stream=None):
+    """The root-mean-square norm of h = x + residual (x without one), times weight [N], in 8 bits: (Rows8, h).
+    x, residual and h [.., N] and weight are of one type; out: where h goes with a residual, e.g. the residual itself."""
+    if _elsewhere(x, stream):
+        return _on(x.device, stream, (x, weight, residual, out), lambda: norm_rows(x, weight, residual, eps, out))
+    carried = x
+    x, rows, a = _rows8_of(x, "x")
+    n, dt, dev = x.shape[1], x.dtype, x.device
+    _require(isinstance(weight, torch.Tensor) and tuple(weight.shape) == (n,) and weight.dtype is dt and weight.device == dev,
+             f"weight: [{n}] {dt} on {dev} is wanted")
+    if weight.requires_grad:
+        _no_gradient()
+    weight = weight if weight.is_contiguous() else weight.contiguous()
+    if residual is None:
+        _require(out is None, "out: with a residual only, without one h is x")
+        a = Norm8Args(a, None, 0, None, 0, weight.data_ptr(), eps)
+    else:
+        _require(isinstance(residual, torch.Tensor) and residual.shape == carried.shape, f"residual: {tuple(carried.shape)} is wanted")
+        residual = _matrix(residual, "residual", n, dt, dev)
+        carried = torch.empty(carried.shape, dtype=dt, device=dev) if out is None else _into(out, "out", carried.shape, dt, dev)
+        h = carried if carried.dim() == 2 else carried.view(-1, n)
+        a = Norm8Args(a, residual.data_ptr(), residual.stride(0), h.data_ptr(), h.stride(0), weight.data_ptr(), eps)
+    s = mf.lib.mf_norm8(C.byref(a), _stream_of(dev))
+    if s:
+        _check(s, "mf_norm8")
+    return rows, carried
+
+
+def gate_rows(gate, up, stream=None) -> Rows8:
+    """gate * sigmoid(gate) * up in 8 bits; gate and up [.., N] of one type, e.g. the halves of one product's results."""
+    if _elsewhere(gate, stream):
+        return _on(gate.device, stream, (gate, up), lambda: gate_rows(gate, up))
+    x, rows, a = _rows8_of(gate, "gate")
+    _require(isinstance(up, torch.Tensor) and up.shape == gate.shape, f"up: {tuple(gate.shape)} is wanted")
+    u = _matrix(up, "up", x.shape[1], x.dtype, x.device)
+    a = Gate8Args(a, u.data_ptr(), u.stride(0))
+    s = mf.lib.mf_gate8(C.byref(a), _stream_of(x.device))
+    if s:
+        _check(s, "mf_gate8")
+    return rows
+
+
+class W8Weight:
+    """8-bit weights [N, K] with a scale for every output: w = scale * code.
+
+    codes: int8 [N, K], K a multiple of 16; scales: float32 [N]; dtype: of
+    biases and results, bfloat16 or float16.  Laid out once, here; the arguments
+    may be freed after."""
+
+    def __init__(self, codes, scales, dtype=torch.bfloat16, stream=None):
+        _require(isinstance(codes, torch.Tensor) and codes.dtype is torch.int8 and codes.dim() == 2 and codes.is_cuda,
+                 "codes: an int8 [N, K] tensor on the GPU is wanted")
+        _require(isinstance(scales, torch.Tensor) and scales.dtype is torch.float32 and scales.dim() == 1
+                 and scales.shape[0] == codes.shape[0] and scales.device == codes.device, "scales: float32 [N] beside the codes is wanted")
+        if scales.requires_grad:
+            _no_gradient()
+        _require(dtype in _HALF, "dtype: bfloat16 or float16 is wanted")
+        self.n_out, self.n_in, self.dtype, self.device = int(codes.shape[0]), int(codes.shape[1]), dtype, codes.device
+        self.desc = W8Desc(self.n_out, self.n_in, _DTYPES[dtype])
+        nb = C.c_size_t()
+        _check(mf.lib.mf_w8_pack_bytes(C.byref(self.desc), C.byref(nb)), "mf_w8_pack_bytes")
+        self.packed = _on(self.device, stream, (codes, scales), lambda: self._pack(codes, scales, int(nb.value)))
+        self._packed_ptr = self.packed.data_ptr()
+        self._ws_bytes = {}   # by rows, and whether they come in 8 bits
+
+    def _pack(self, codes, scales, nbytes):
+        codes, scales = codes.contiguous(), scales.contiguous()
+        packed = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        _check(mf.lib.mf_w8_pack(C.byref(self.desc), _ptr(codes), _ptr(scales), _ptr(packed), C.c_size_t(nbytes), _stream_of(self.device)),
+               "mf_w8_pack")
+        return packed
+
+    def matmul(self, x, bias=None, out=None, stream=None):
+        """x @ W.T + bias [N] -> [.., N]; x: Rows8 of [.., K], or [.., K] in the weight's type, which is put into 8 bits on the way."""
+        if stream is not None or self.device.index != _current_device():
+            held = tuple(x) if isinstance(x, tuple) else x
+            return _on(self.device, stream, (held, bias, out, self.packed), lambda: self.matmul(x, bias, out))
+        dt, dev, k, n = self.dtype, self.device, self.n_in, self.n_out
+        if isinstance(x, tuple):
+            lead = x[0].shape[:-1]
+            x, xs = Rows8(*x)._checked()
+            _require(x.shape[1] == k and x.device == dev, f"x: rows of {k} on {dev} are wanted")
+            scales = xs.data_ptr()
+        else:
+            _require(isinstance(x, torch.Tensor), f"x: Rows8, or [.., {k}] {dt}, is wanted")
+            lead, scales = x.shape[:-1], None
+            x = _matrix(x, "x", k, dt, dev)
+        if bias is not None:
+            _require(bias.dtype is dt and bias.device == dev and tuple(bias.shape) == (n,) and bias.is_contiguous(),
+                     f"bias: contiguous [{n}] {dt} on {dev} is wanted")
+            if bias.requires_grad:
+                _no_gradient()
+        m = x.shape[0]
+        if out is None:
+            out = torch.empty((*lead, n), dtype=dt, device=dev)
+        else:
+            _into(out, "out", (*lead, n), dt, dev)
+        y = out if out.dim() == 2 else out.view(-1, n)
+        a = W8Args(self.desc, self._packed_ptr, x.data_ptr(), scales, None if bias is None else bias.data_ptr(), y.data_ptr(), m, x.stride(0),
+                   y.stride(0))
+        key = (m, scales is None)
+        need = self._ws_bytes.get(key)
+        if need is None:
+            nb = C.c_size_t()
+            _check(mf.lib.mf_w8_workspace_size(C.byref(a), C.byref(nb)), "mf_w8_workspace_size")
+            need = self._ws_bytes[key] = nb.value
+        ws = _workspaces.get(need, dev) if need else None
+        s = mf.lib.mf_w8_matmul(C.byref(a), ws.data_ptr() if need else None, need, _stream_of(dev))
+        if s:
+            _check(s, "mf_w8_matmul")
         return out
 
 
