@@ -634,6 +634,50 @@ mf_status mf_w8_workspace_size(const mf_w8_args *args, size_t *bytes);
 /* Any number of rows.  Deterministic.  d_ws: mf_w8_workspace_size bytes, 256-byte aligned; need not be initialised. */
 mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void *stream);
 
+/* --- the paged cache in 8 bits
+ *
+ * Pages as the 4-bit cache's.  The 16 tokens of a page from a multiple of 16 on, a
+ * block, share a scale for the keys of a head and one for its values; codes are
+ * -127..127 and the value held is scale * code.  A call that appends tokens to a
+ * block finds, in fp32, each step rounded,
+ *   x limited to +-65504, need = max |x| over the call's tokens of the block * (float)(1 / 127.), at least 2^-40,
+ *   scale = need where the block is not begun, or its scale so far is 2^-40,
+ *   else the scale so far where need is not above it, else the scale so far doubled until it reaches need,
+ *   code = rint(x * (1 / scale)) limited to -127..127.
+ * A block is begun where the call's first token in it is not its first.  Codes that a
+ * begun block holds become rint(code * (scale so far / scale)) when the scale grows,
+ * so a value held is off by less than one step of the scale at hand, over any number
+ * of calls.  Where a begun block's scale is none (outside of 2^-40 .. 2^11 and no NaN,
+ * as in memory of zeros), scale = need and its earlier tokens become zeros; other memory that
+ * was never written must not be begun.  A NaN makes
+ * the scale NaN, and with it the block's keys or values, until the block is begun anew.
+ * Tokens that are given up (a shorter kv_len) leave their block's scale as it is.
+ * Per token and head: 2 D bytes of codes, and 8 / 16 of scales. */
+typedef struct {
+    int32_t n_pages;        /* >= 1 */
+    int32_t page_size;      /* tokens, a multiple of 16, 16..1024 */
+    int32_t n_kv_heads;     /* 1..1024 */
+    int32_t head_dim;       /* D: 64, 128 or 256 */
+    void *d_pages;          /* mf_kv8_cache_bytes, 256-byte aligned; need not be initialised */
+} mf_kv8_cache;
+
+/* Bytes of d_pages. */
+mf_status mf_kv8_cache_bytes(const mf_kv8_cache *cache, size_t *bytes);
+
+/* As mf_kv4_append, mf_kv4_read, mf_kv4_workspace_size and mf_kv4_attention, with
+ * the same batches and arguments.  What a page number that is not the cache's, or a
+ * token that is not there, does is the same.  Attention: the weights of the values,
+ * times their scales, are rounded to binary16 (down to 2^-34 of a row's largest such
+ * product), queries to 2^-25 of a row's largest value where they are below 2^-28 of it.  No
+ * bit of a row's result depends on blocks of which it sees no token; of a block
+ * that it sees a part of, the scales are all its tokens'.  Blocks of zeros in memory are
+ * tokens of zeros (to attention, their values are below 2^-32). */
+mf_status mf_kv8_append(const mf_kv8_cache *cache, const mf_kv4_batch *batch, const mf_kv4_append_args *args, void *stream);
+mf_status mf_kv8_read(const mf_kv8_cache *cache, const mf_kv4_batch *batch, mf_dtype dtype, void *d_k, void *d_v, void *stream);
+mf_status mf_kv8_workspace_size(const mf_kv8_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, size_t *bytes);
+mf_status mf_kv8_attention(const mf_kv8_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, void *d_ws, size_t ws_bytes,
+                           void *stream);
+
 /* Human-readable status name. */
 const char *mf_status_string(mf_status s);
 

@@ -7,80 +7,12 @@
 // bytes of LDS, [dim][token], of which four tokens are one word; a dword that holds
 // other tokens' codes keeps those.  One wave owns a record, so nothing is written
 // twice and no atomics are needed.
-#include "mf_serve_dev.h"
+#include "mf_kv_rows.h"
 
 namespace mfs {
 namespace {
 
 constexpr float kF16Max = 65504.f;
-
-// A sequence's new tokens as far as they lie in the step's rows and in the
-// cache, whatever the device arrays hold: positions [lo, hi), row = pos + shift.
-struct Span {
-    int lo, hi;
-    long long shift;
-    long long row0, row1;   // its rows in [0, rows)
-};
-
-__device__ __forceinline__ Span span_of(const KvBatch &b, int s)
-{
-    Span p;
-    const long long r0 = b.q_start[s], r1 = b.q_start[s + 1], kv = b.kv_len[s];
-    p.shift = r1 - kv;
-    p.row0 = r0 > 0 ? r0 : 0;
-    p.row1 = r1 < b.rows ? r1 : b.rows;
-    const long long lo = p.row0 - p.shift, hi = p.row1 - p.shift;
-    p.lo = lo <= 0 ? 0 : lo < b.max_kv ? (int)lo : b.max_kv;
-    p.hi = hi <= 0 ? 0 : hi < b.max_kv ? (int)hi : b.max_kv;
-    return p;
-}
-
-template <bool F16>
-__device__ __forceinline__ void widen8(u32x4 raw, float *v)
-{
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = to_float<F16>((uint16_t)(raw[j >> 1] >> (16 * (j & 1))));
-}
-
-// Eight values of a row turned by its position: dims d .. d + 7 of a head at x, of
-// which `own` are loaded.  Each product and sum is rounded by itself (the library is
-// compiled without contraction), as the definition has it.
-template <bool F16>
-__device__ __forceinline__ void turn8(const uint16_t *x, u32x4 own, int d, int rot, int inter, const float *cos, const float *sin, float *v)
-{
-    widen8<F16>(own, v);
-    if (d >= rot) return;
-    const int half = rot >> 1;
-    if (inter) {
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            const float c = cos[(d + j) >> 1], s = sin[(d + j) >> 1], a = v[j], b = v[j + 1];
-            v[j] = a * c - b * s;
-            v[j + 1] = b * c + a * s;
-        }
-        return;
-    }
-    // rot / 2 is a multiple of 8: the partners are eight in a row too
-    const bool second = d >= half;
-    const int t = second ? d - half : d;
-    float y[8];
-    widen8<F16>(load16(x + (second ? t : t + half)), y);
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        const float c = cos[t + j], s = sin[t + j];
-        v[j] = second ? v[j] * c + y[j] * s : v[j] * c - y[j] * s;
-    }
-}
-// The pair of halves (a, b) of dims t .. t + 7.
-__device__ __forceinline__ void turn_pair(float *a, float *b, const float *cos, const float *sin)
-{
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-        const float c = cos[j], s = sin[j], x = a[j], y = b[j];
-        a[j] = x * c - y * s;
-        b[j] = y * c + x * s;
-    }
-}
 
 // Codes and scales of a token's values as the lane (token, l / 16) holds them: v[i][j] is dim 32 i + 8 (l / 16) + j.
 template <int D, int G>
@@ -220,62 +152,6 @@ __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h
     __syncthreads();
 }
 
-// The queries of 16 tokens, heads h0 .. h1: a thread takes 8 dims (with their
-// partners, so that the result may go over its source).  Many tokens: eight of them
-// side by side, the angles kept over the heads; few: eight heads side by side.
-template <bool F16>
-__device__ __forceinline__ void turn_queries(const KvAppendArgs &a, const Span &p, int blk, int h0, int h1, int D, bool few)
-{
-    const int half = a.rot >> 1, base = p.lo + blk * 16;
-    const int units = a.interleaved ? D / 8 : (D - half) / 8;   // a unit below rot / 2 takes its partner along
-    const int u0 = threadIdx.x & 7, b0 = threadIdx.x >> 3;
-    for (int u = u0; u < units; u += 8) {
-        const int d = u * 8, d0 = a.interleaved || d < half ? d : d + half, d1 = !a.interleaved && d < half ? d + half : -1;
-        const bool turned = d0 < a.rot;
-        for (int t = few ? 0 : b0; t < 16; t += few ? 1 : 8) {
-            const int pos = base + t;
-            if (pos >= p.hi) break;
-            const long long row = pos + p.shift;
-            const uint16_t *x = (const uint16_t *)a.q + row * a.q_stride;
-            uint16_t *y = (uint16_t *)a.q_out + row * a.qo_stride;
-            float cos[8], sin[8];
-            if (turned) {
-                const long long at = (long long)pos * half + (a.interleaved ? d >> 1 : d);
-#pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const int e = a.interleaved ? j >> 1 : j;
-                    cos[j] = a.cos[at + e];
-                    sin[j] = a.sin[at + e];
-                }
-            }
-#pragma unroll 4
-            for (int h = h0 + (few ? b0 : 0); h < h1; h += few ? 8 : 1) {
-                float v[2][8];
-                widen8<F16>(load16(x + h * a.q_head + d0), v[0]);
-                if (d1 >= 0) {
-                    widen8<F16>(load16(x + h * a.q_head + d1), v[1]);
-                    turn_pair(v[0], v[1], cos, sin);
-                } else if (turned) {
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const float m = v[0][j], n = v[0][j + 1];
-                        v[0][j] = m * cos[j] - n * sin[j];
-                        v[0][j + 1] = n * cos[j] + m * sin[j];
-                    }
-                }
-#pragma unroll
-                for (int w = 0; w < 2; w++) {
-                    if (w == 1 && d1 < 0) break;
-                    u32x4 o;
-#pragma unroll
-                    for (int j = 0; j < 4; j++) o[j] = pack2<F16>(v[w][2 * j], v[w][2 * j + 1]);
-                    __builtin_memcpy(__builtin_assume_aligned(y + h * a.qo_head + (w ? d1 : d0), 2), &o, 16);
-                }
-            }
-        }
-    }
-}
-
 // Work item: (sequence, 16 positions, head), the numbers past the heads standing for
 // slices of the queries' heads: few tokens or many, there is a wave for each 16 of a head.
 // Bound by the bytes of rows and queries from some thousand rows on (32768 rows of 32 + 2 x
@@ -295,22 +171,6 @@ __global__ __launch_bounds__(64) void append_kernel(KvAppendArgs a, int blocks, 
         return;
     }
     for (int b = (p.lo >> 4) + rest % blocks; b * kKvBlock < p.hi; b += blocks) append_block<F16, D, G>(a, s, h, b, p, lds);
-}
-
-// Eight values of a row to the output, in its type.
-template <int TY>
-__device__ __forceinline__ void put8(void *dst, long long at, const float *v)
-{
-    if constexpr (TY == MF_F32) {
-        float *y = (float *)dst + at;
-#pragma unroll
-        for (int j = 0; j < 8; j++) y[j] = v[j];
-    } else {
-        u32x4 o;
-#pragma unroll
-        for (int j = 0; j < 4; j++) o[j] = pack2<TY == MF_F16>(v[2 * j], v[2 * j + 1]);
-        __builtin_memcpy(__builtin_assume_aligned((uint16_t *)dst + at, 2), &o, 16);
-    }
 }
 
 // Rows back, a wave per 16 positions of a head as in the append; bound by the bytes written
@@ -392,22 +252,6 @@ template <int TY, int D, int G>
 void go_read(const KvReadArgs &a, unsigned grid, int blocks, hipStream_t s)
 {
     hipLaunchKernelGGL((read_kernel<TY, D, G>), dim3(grid), dim3(64), 0, s, a, blocks);
-}
-
-// Launches of workgroups of 64 for n_seq sequences of `items` items and up to `span` tokens each: as many sequences to a
-// launch as have room, and as many workgroups to an item as it has blocks of 16 or the launch has room; a kernel takes further blocks in turn.
-template <class F>
-hipError_t each_launch(int n_seq, int items, int span, const F &launch)
-{
-    const long long room = most_workgroups(64) / items, touched = (span + 14ll) / 16 + 1;
-    for (int first = 0; first < n_seq;) {
-        const int n = (int)(n_seq - first < room ? n_seq - first : room), blocks = (int)(touched < room / n ? touched : room / n);
-        launch(first, (unsigned)((long long)n * items * blocks), blocks);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        first += n;
-    }
-    return hipSuccess;
 }
 
 }  // namespace

@@ -179,12 +179,17 @@ hipError_t go_join(const KvAttnArgs &a, const KvPlan &p, bool f16, long long ite
 
 }  // namespace
 
+hipError_t launch_kv_join(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s)
+{
+    if (p.slots == 0) return hipSuccess;
+    const long long items = p.row_tiles * a.b.n_seq * a.g.n_kv_heads;
+    return a.g.head_dim == 64 ? go_join<64>(a, p, f16, items, s) : a.g.head_dim == 128 ? go_join<128>(a, p, f16, items, s) : go_join<256>(a, p, f16, items, s);
+}
+
 hipError_t launch_kv4_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s)
 {
     const hipError_t e = a.g.head_dim == 64 ? launch_attn_d64(a, p, f16, s) : a.g.head_dim == 128 ? launch_attn_d128(a, p, f16, s) : launch_attn_d256(a, p, f16, s);
-    if (e != hipSuccess || p.slots == 0) return e;
-    const long long items = p.row_tiles * a.b.n_seq * a.g.n_kv_heads;
-    return a.g.head_dim == 64 ? go_join<64>(a, p, f16, items, s) : a.g.head_dim == 128 ? go_join<128>(a, p, f16, items, s) : go_join<256>(a, p, f16, items, s);
+    return e != hipSuccess ? e : launch_kv_join(a, p, f16, s);
 }
 
 }  // namespace mfs

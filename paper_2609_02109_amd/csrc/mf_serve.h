@@ -81,6 +81,9 @@ struct KvGeom {
     int rec;                 // bytes of a record
     unsigned long long magic;   // ceil(2^32 / blocks_per_page): b / blocks_per_page = b magic >> 32 for b < 2^27
 };
+struct KvScales {   // of a record of the 8-bit cache
+    float k, v;
+};
 struct KvBatch {
     int n_seq, max_new, max_kv, rows;
     const int *q_start, *kv_len, *table;
@@ -103,6 +106,18 @@ __device__ __forceinline__ uint8_t *kv_record(const KvGeom &g, const KvBatch &b,
     const int page = b.table[(long long)s * b.table_stride + col];
     if ((unsigned)page >= (unsigned)g.n_pages) return nullptr;
     return g.pages + (((long long)page * g.n_kv_heads + h) * g.blocks_per_page + (blk - col * g.blocks_per_page)) * (long long)g.rec;
+}
+// Its number among all records of the 8-bit cache, -1 where there is none, and all records' scales.
+__device__ __forceinline__ long long kv8_record(const KvGeom &g, const KvBatch &b, int s, int h, int blk)
+{
+    const int col = page_of_block(g, blk);
+    const int page = b.table[(long long)s * b.table_stride + col];
+    if ((unsigned)page >= (unsigned)g.n_pages) return -1;
+    return ((long long)page * g.n_kv_heads + h) * g.blocks_per_page + (blk - col * g.blocks_per_page);
+}
+__device__ __forceinline__ KvScales *kv8_scales(const KvGeom &g)
+{
+    return (KvScales *)(g.pages + (long long)g.n_pages * g.n_kv_heads * g.blocks_per_page * (long long)g.rec);
 }
 #endif
 
@@ -156,9 +171,26 @@ struct KvPlan {
     size_t ws_bytes;
 };
 KvPlan kv4_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window);
+// Adds up the parts that a launch left (either cache's).
+hipError_t launch_kv_join(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
 hipError_t launch_kv4_append(const KvAppendArgs &a, bool f16, hipStream_t s);
 hipError_t launch_kv4_read(const KvReadArgs &a, int dtype, hipStream_t s);
 hipError_t launch_kv4_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
+
+// ------------------------------------------------------------- 8-bit cache
+// As the 4-bit cache, with 32 D bytes a record; a byte is a code + 128:
+//   keys    64 dims in 1 KB: lane l's 16 bytes at 16 l are dims 64 j + 16 (l / 16)
+//           .. + 15 of token l % 16 (two A operands of v_mfma_f32_16x16x32)
+//   values  64 dims in 1 KB: lane l's dword i at 16 l + 4 i is dim 64 j + 16 i +
+//           l % 16 of tokens 4 (l / 16) .. + 3
+// After all records two fp32 numbers for each, in the records' order: the scales
+// of its keys and of its values.
+// Scales are 2^-40 up to 65504 / 127, twice that where a begun block's has grown, or NaN.
+constexpr float kKv8LeastScale = 0x1p-40f, kKv8MostScale = 0x1p11f;
+hipError_t launch_kv8_append(const KvAppendArgs &a, bool f16, hipStream_t s);
+hipError_t launch_kv8_read(const KvReadArgs &a, int dtype, hipStream_t s);
+KvPlan kv8_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window);
+hipError_t launch_kv8_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
 
 // ------------------------------------------------------------ rows in 8 bits
 enum Rows8Op { kRowsPlain, kRowsNorm, kRowsGate };

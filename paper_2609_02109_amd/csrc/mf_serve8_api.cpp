@@ -51,6 +51,23 @@ mf_status check_w8_rows(const mf_w8_args *a)
 size_t w8_records(const mf_w8_desc &d) { return (size_t)((d.n_out + kW8Tile - 1) / kW8Tile) * (size_t)w8_chunks((int)d.n_in) * kW8Record; }
 size_t w8_bytes(const mf_w8_desc &d) { return w8_records(d) + (size_t)d.n_out * sizeof(float); }
 
+mf_status check_cache8(const mf_kv8_cache *c, KvGeom &g)
+{
+    if (!c) return MF_EINVAL;
+    if (c->n_pages < 1 || c->page_size < 1 || c->n_kv_heads < 1 || c->head_dim < 1) return MF_EINVAL;
+    if (c->page_size % kKvBlock != 0 || c->page_size > 1024 || c->n_kv_heads > 1024) return MF_EUNSUPPORTED;
+    if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return MF_EUNSUPPORTED;
+    g.pages = (uint8_t *)c->d_pages;
+    g.n_pages = c->n_pages;
+    g.blocks_per_page = c->page_size / kKvBlock;
+    g.n_kv_heads = c->n_kv_heads;
+    g.head_dim = c->head_dim;
+    g.group = 0;
+    g.rec = 32 * c->head_dim;
+    g.magic = block_magic(g.blocks_per_page);
+    return MF_OK;
+}
+
 // The workspace: what the product itself needs, then the codes and the scales of rows that come in 16 bits.
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t w8_ws(const mf_w8_args &a, const W8Plan &p)
@@ -201,6 +218,59 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
         a.x_scales = r.scales;
     }
     return of(launch_w8(a, p, f16, d_ws, (hipStream_t)stream));
+}
+
+mf_status mf_kv8_cache_bytes(const mf_kv8_cache *cache, size_t *bytes)
+{
+    if (!bytes) return MF_EINVAL;
+    KvGeom g;
+    const mf_status st = check_cache8(cache, g);
+    if (st == MF_OK) *bytes = (size_t)g.n_pages * g.n_kv_heads * g.blocks_per_page * ((size_t)g.rec + sizeof(KvScales));
+    return st;
+}
+
+mf_status mf_kv8_append(const mf_kv8_cache *cache, const mf_kv4_batch *batch, const mf_kv4_append_args *args, void *stream)
+{
+    KvAppendArgs a;
+    bool none = true;
+    mf_status st = check_cache8(cache, a.g);
+    if (st == MF_OK) st = check_append(cache->d_pages, batch, args, a, none);
+    if (st != MF_OK || none) return st;
+    return of(launch_kv8_append(a, as_int(args->dtype) == MF_F16, (hipStream_t)stream));
+}
+
+mf_status mf_kv8_read(const mf_kv8_cache *cache, const mf_kv4_batch *batch, mf_dtype dtype, void *d_k, void *d_v, void *stream)
+{
+    KvReadArgs a;
+    bool none = true;
+    mf_status st = check_cache8(cache, a.g);
+    if (st == MF_OK) st = check_read(cache->d_pages, batch, as_int(dtype), d_k, d_v, a, none);
+    if (st != MF_OK || none) return st;
+    return of(launch_kv8_read(a, as_int(dtype), (hipStream_t)stream));
+}
+
+mf_status mf_kv8_workspace_size(const mf_kv8_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, size_t *bytes)
+{
+    if (!bytes) return MF_EINVAL;
+    KvAttnArgs a;
+    KvPlan p;
+    mf_status st = check_cache8(cache, a.g);
+    if (st == MF_OK) st = check_attn(cache->d_pages, batch, args, false, kv8_plan, a, p);
+    if (st == MF_OK) *bytes = p.ws_bytes;
+    return st;
+}
+
+mf_status mf_kv8_attention(const mf_kv8_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, void *d_ws,
+                           size_t ws_bytes, void *stream)
+{
+    KvAttnArgs a;
+    KvPlan p;
+    bool none = true;
+    mf_status st = check_cache8(cache, a.g);
+    if (st == MF_OK) st = check_attn(cache->d_pages, batch, args, true, kv8_plan, a, p);
+    if (st == MF_OK) st = check_attn_run(batch, args, d_ws, ws_bytes, p, a, none);
+    if (st != MF_OK || none) return st;
+    return of(launch_kv8_attn(a, p, as_int(args->dtype) == MF_F16, (hipStream_t)stream));
 }
 
 }  // extern "C"

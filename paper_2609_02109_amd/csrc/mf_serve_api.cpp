@@ -49,36 +49,6 @@ mf_status check_cache(const mf_kv4_cache *c, KvGeom &g)
     return MF_OK;
 }
 
-mf_status check_attn(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, bool run, KvAttnArgs &a, KvPlan &p)
-{
-    mf_status st = check_cache(cache, a.g);
-    if (st == MF_OK) st = check_batch(cache->page_size, cache->d_pages, batch, run, a.b);
-    if (st != MF_OK) return st;
-    if (!args || !half_type(as_int(args->dtype))) return MF_EINVAL;
-    if (args->n_heads < 1 || args->n_heads % cache->n_kv_heads != 0 || args->window < 0) return MF_EINVAL;
-    if (args->n_heads > 4096) return MF_EUNSUPPORTED;
-    if (!std::isfinite(args->scale) || args->scale <= 0.f) return MF_EINVAL;
-    a.n_heads = args->n_heads;
-    a.per_kv = args->n_heads / cache->n_kv_heads;
-    if (batch->rows * a.per_kv > INT32_MAX - 1024) return MF_EUNSUPPORTED;   // rows of a sequence and key head are an int
-    a.window = args->window;
-    a.scale_log2 = (float)((double)args->scale * 1.4426950408889634);
-    p = kv4_plan(a.g, a.b, a.n_heads, a.window);
-    // all sequences' units of one head are an int
-    if ((((int64_t)batch->max_kv + kAttnUnit - 1) / kAttnUnit + 1) * batch->n_seq > INT32_MAX) return MF_EUNSUPPORTED;
-    // a workgroup's number, and a row's of the join, are an int
-    const int64_t items = p.row_tiles * batch->n_seq * cache->n_kv_heads;
-    if (p.workgroups > INT32_MAX || (p.slots > 0 && (items * p.slot_rows > INT32_MAX || p.slots > INT32_MAX))) return MF_EUNSUPPORTED;
-    a.row_tiles = (int)p.row_tiles;
-    a.splits = p.splits;
-    a.chunk = p.chunk;
-    a.workgroups = (int)p.workgroups;
-    a.whole = p.whole;
-    a.slots = (int)p.slots;
-    a.slot_rows = p.slot_rows;
-    return MF_OK;
-}
-
 }  // namespace
 
 extern "C" {
@@ -159,63 +129,21 @@ mf_status mf_kv4_cache_bytes(const mf_kv4_cache *cache, size_t *bytes)
 mf_status mf_kv4_append(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_append_args *args, void *stream)
 {
     KvAppendArgs a;
+    bool none = true;
     mf_status st = check_cache(cache, a.g);
-    if (st == MF_OK) st = check_batch(cache->page_size, cache->d_pages, batch, true, a.b);
-    if (st != MF_OK) return st;
-    if (!args || !half_type(as_int(args->dtype))) return MF_EINVAL;
-    const int64_t rows = batch->rows, d = cache->head_dim;
-    if ((args->d_cos == nullptr) != (args->d_sin == nullptr)) return MF_EINVAL;
-    if (args->d_q && (!args->d_cos || !args->d_q_out || args->n_heads < 1)) return MF_EINVAL;
-    if (args->n_heads < 0) return MF_EINVAL;
-    if (args->n_heads > 4096) return MF_EUNSUPPORTED;
-    if (args->d_cos) {
-        if (args->rot_dim < 16 || args->rot_dim > d) return MF_EINVAL;
-        if (args->rot_dim % 16 != 0) return MF_EUNSUPPORTED;
-        if (args->n_pos < batch->max_kv || !aligned(args->d_cos, 4) || !aligned(args->d_sin, 4)) return MF_EINVAL;
-    }
-    if (rows == 0 || batch->n_seq == 0 || batch->max_new == 0) return MF_OK;
-    if (!args->d_k || !args->d_v || !aligned(args->d_k, 2) || !aligned(args->d_v, 2) || !aligned(args->d_q, 2) || !aligned(args->d_q_out, 2))
-        return MF_EINVAL;
-    if (!strides_fit(rows, args->k_stride, cache->n_kv_heads, args->k_head_stride, d, false) ||
-        !strides_fit(rows, args->v_stride, cache->n_kv_heads, args->v_head_stride, d, false))
-        return MF_EINVAL;
-    if (args->d_q && (!strides_fit(rows, args->q_stride, args->n_heads, args->q_head_stride, d, false) ||
-                      !strides_fit(rows, args->qo_stride, args->n_heads, args->qo_head_stride, d, true)))
-        return MF_EINVAL;
-    a.k = args->d_k;
-    a.v = args->d_v;
-    a.q = args->d_q;
-    a.q_out = args->d_q_out;
-    a.cos = args->d_cos;
-    a.sin = args->d_sin;
-    a.k_stride = args->k_stride;
-    a.k_head = args->k_head_stride;
-    a.v_stride = args->v_stride;
-    a.v_head = args->v_head_stride;
-    a.q_stride = args->q_stride;
-    a.q_head = args->q_head_stride;
-    a.qo_stride = args->qo_stride;
-    a.qo_head = args->qo_head_stride;
-    a.rot = args->d_cos ? args->rot_dim : 0;
-    a.interleaved = args->interleaved != 0;
-    a.n_heads = args->d_q ? args->n_heads : 0;
+    if (st == MF_OK) st = check_append(cache->d_pages, batch, args, a, none);
+    if (st != MF_OK || none) return st;
     return of(launch_kv4_append(a, as_int(args->dtype) == MF_F16, (hipStream_t)stream));
 }
 
 mf_status mf_kv4_read(const mf_kv4_cache *cache, const mf_kv4_batch *batch, mf_dtype dtype, void *d_k, void *d_v, void *stream)
 {
     KvReadArgs a;
+    bool none = true;
     mf_status st = check_cache(cache, a.g);
-    if (st == MF_OK) st = check_batch(cache->page_size, cache->d_pages, batch, true, a.b);
-    if (st != MF_OK) return st;
-    const int ty = as_int(dtype);
-    if (ty != MF_F32 && !half_type(ty)) return MF_EINVAL;
-    const size_t el = ty == MF_F32 ? 4 : 2;
-    if (!aligned(d_k, el) || !aligned(d_v, el)) return MF_EINVAL;
-    if (batch->rows == 0 || batch->n_seq == 0 || batch->max_new == 0 || (!d_k && !d_v)) return MF_OK;
-    a.k = d_k;
-    a.v = d_v;
-    return of(launch_kv4_read(a, ty, (hipStream_t)stream));
+    if (st == MF_OK) st = check_read(cache->d_pages, batch, as_int(dtype), d_k, d_v, a, none);
+    if (st != MF_OK || none) return st;
+    return of(launch_kv4_read(a, as_int(dtype), (hipStream_t)stream));
 }
 
 mf_status mf_kv4_workspace_size(const mf_kv4_cache *cache, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, size_t *bytes)
@@ -223,7 +151,8 @@ mf_status mf_kv4_workspace_size(const mf_kv4_cache *cache, const mf_kv4_batch *b
     if (!bytes) return MF_EINVAL;
     KvAttnArgs a;
     KvPlan p;
-    const mf_status st = check_attn(cache, batch, args, false, a, p);
+    mf_status st = check_cache(cache, a.g);
+    if (st == MF_OK) st = check_attn(cache->d_pages, batch, args, false, kv4_plan, a, p);
     if (st == MF_OK) *bytes = p.ws_bytes;
     return st;
 }
@@ -233,24 +162,11 @@ mf_status mf_kv4_attention(const mf_kv4_cache *cache, const mf_kv4_batch *batch,
 {
     KvAttnArgs a;
     KvPlan p;
-    const mf_status st = check_attn(cache, batch, args, true, a, p);
-    if (st != MF_OK) return st;
-    if (batch->rows == 0 || batch->n_seq == 0 || batch->max_new == 0) return MF_OK;
-    if (!args->d_q || !args->d_out || !aligned(args->d_q, 2) || !aligned(args->d_out, 2) || !aligned(args->d_lse, 4)) return MF_EINVAL;
-    const int64_t d = cache->head_dim;
-    if (!strides_fit(batch->rows, args->q_stride, args->n_heads, args->q_head_stride, d, false) ||
-        !strides_fit(batch->rows, args->out_stride, args->n_heads, args->out_head_stride, d, true))
-        return MF_EINVAL;
-    if (ws_bytes < p.ws_bytes || (p.ws_bytes > 0 && !d_ws)) return MF_ENOMEM;
-    if (p.ws_bytes > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
-    a.q = args->d_q;
-    a.out = args->d_out;
-    a.lse = args->d_lse;
-    a.q_stride = args->q_stride;
-    a.q_head = args->q_head_stride;
-    a.out_stride = args->out_stride;
-    a.out_head = args->out_head_stride;
-    a.part = (float *)d_ws;
+    bool none = true;
+    mf_status st = check_cache(cache, a.g);
+    if (st == MF_OK) st = check_attn(cache->d_pages, batch, args, true, kv4_plan, a, p);
+    if (st == MF_OK) st = check_attn_run(batch, args, d_ws, ws_bytes, p, a, none);
+    if (st != MF_OK || none) return st;
     return of(launch_kv4_attn(a, p, as_int(args->dtype) == MF_F16, (hipStream_t)stream));
 }
 

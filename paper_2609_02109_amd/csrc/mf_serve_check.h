@@ -61,4 +61,119 @@ inline mf_status check_batch(int page_size, const void *d_pages, const mf_kv4_ba
     return MF_OK;
 }
 
+// The arguments of an append to a cache of geometry a.g; none: there is nothing to do.
+inline mf_status check_append(const void *d_pages, const mf_kv4_batch *batch, const mf_kv4_append_args *args, KvAppendArgs &a, bool &none)
+{
+    const mf_status st = check_batch(a.g.blocks_per_page * kKvBlock, d_pages, batch, true, a.b);
+    if (st != MF_OK) return st;
+    if (!args || !half_type(as_int(args->dtype))) return MF_EINVAL;
+    const int64_t rows = batch->rows, d = a.g.head_dim;
+    if ((args->d_cos == nullptr) != (args->d_sin == nullptr)) return MF_EINVAL;
+    if (args->d_q && (!args->d_cos || !args->d_q_out || args->n_heads < 1)) return MF_EINVAL;
+    if (args->n_heads < 0) return MF_EINVAL;
+    if (args->n_heads > 4096) return MF_EUNSUPPORTED;
+    if (args->d_cos) {
+        if (args->rot_dim < 16 || args->rot_dim > d) return MF_EINVAL;
+        if (args->rot_dim % 16 != 0) return MF_EUNSUPPORTED;
+        if (args->n_pos < batch->max_kv || !aligned(args->d_cos, 4) || !aligned(args->d_sin, 4)) return MF_EINVAL;
+    }
+    none = rows == 0 || batch->n_seq == 0 || batch->max_new == 0;
+    if (none) return MF_OK;
+    if (!args->d_k || !args->d_v || !aligned(args->d_k, 2) || !aligned(args->d_v, 2) || !aligned(args->d_q, 2) || !aligned(args->d_q_out, 2))
+        return MF_EINVAL;
+    if (!strides_fit(rows, args->k_stride, a.g.n_kv_heads, args->k_head_stride, d, false) ||
+        !strides_fit(rows, args->v_stride, a.g.n_kv_heads, args->v_head_stride, d, false))
+        return MF_EINVAL;
+    if (args->d_q && (!strides_fit(rows, args->q_stride, args->n_heads, args->q_head_stride, d, false) ||
+                      !strides_fit(rows, args->qo_stride, args->n_heads, args->qo_head_stride, d, true)))
+        return MF_EINVAL;
+    a.k = args->d_k;
+    a.v = args->d_v;
+    a.q = args->d_q;
+    a.q_out = args->d_q_out;
+    a.cos = args->d_cos;
+    a.sin = args->d_sin;
+    a.k_stride = args->k_stride;
+    a.k_head = args->k_head_stride;
+    a.v_stride = args->v_stride;
+    a.v_head = args->v_head_stride;
+    a.q_stride = args->q_stride;
+    a.q_head = args->q_head_stride;
+    a.qo_stride = args->qo_stride;
+    a.qo_head = args->qo_head_stride;
+    a.rot = args->d_cos ? args->rot_dim : 0;
+    a.interleaved = args->interleaved != 0;
+    a.n_heads = args->d_q ? args->n_heads : 0;
+    return MF_OK;
+}
+
+inline mf_status check_read(const void *d_pages, const mf_kv4_batch *batch, int ty, void *d_k, void *d_v, KvReadArgs &a, bool &none)
+{
+    const mf_status st = check_batch(a.g.blocks_per_page * kKvBlock, d_pages, batch, true, a.b);
+    if (st != MF_OK) return st;
+    if (ty != MF_F32 && !half_type(ty)) return MF_EINVAL;
+    const size_t el = ty == MF_F32 ? 4 : 2;
+    if (!aligned(d_k, el) || !aligned(d_v, el)) return MF_EINVAL;
+    none = batch->rows == 0 || batch->n_seq == 0 || batch->max_new == 0 || (!d_k && !d_v);
+    a.k = d_k;
+    a.v = d_v;
+    return MF_OK;
+}
+
+// The arguments of attention over a cache of geometry a.g; `plan` lays its work over the card.
+template <class P>
+mf_status check_attn(const void *d_pages, const mf_kv4_batch *batch, const mf_kv4_attn_args *args, bool run, const P &plan, KvAttnArgs &a, KvPlan &p)
+{
+    const int page_size = a.g.blocks_per_page * kKvBlock;
+    const mf_status st = check_batch(page_size, d_pages, batch, run, a.b);
+    if (st != MF_OK) return st;
+    if (!args || !half_type(as_int(args->dtype))) return MF_EINVAL;
+    if (args->n_heads < 1 || args->n_heads % a.g.n_kv_heads != 0 || args->window < 0) return MF_EINVAL;
+    if (args->n_heads > 4096) return MF_EUNSUPPORTED;
+    if (!std::isfinite(args->scale) || args->scale <= 0.f) return MF_EINVAL;
+    a.n_heads = args->n_heads;
+    a.per_kv = args->n_heads / a.g.n_kv_heads;
+    if (batch->rows * a.per_kv > INT32_MAX - 1024) return MF_EUNSUPPORTED;   // rows of a sequence and key head are an int
+    a.window = args->window;
+    a.scale_log2 = (float)((double)args->scale * 1.4426950408889634);
+    p = plan(a.g, a.b, a.n_heads, a.window);
+    // all sequences' units of one head are an int
+    if ((((int64_t)batch->max_kv + kAttnUnit - 1) / kAttnUnit + 1) * batch->n_seq > INT32_MAX) return MF_EUNSUPPORTED;
+    // a workgroup's number, and a row's of the join, are an int
+    const int64_t items = p.row_tiles * batch->n_seq * a.g.n_kv_heads;
+    if (p.workgroups > INT32_MAX || (p.slots > 0 && (items * p.slot_rows > INT32_MAX || p.slots > INT32_MAX))) return MF_EUNSUPPORTED;
+    a.row_tiles = (int)p.row_tiles;
+    a.splits = p.splits;
+    a.chunk = p.chunk;
+    a.workgroups = (int)p.workgroups;
+    a.whole = p.whole;
+    a.slots = (int)p.slots;
+    a.slot_rows = p.slot_rows;
+    return MF_OK;
+}
+
+// The operands and the workspace of attention, after check_attn; none: there is nothing to do.
+inline mf_status check_attn_run(const mf_kv4_batch *batch, const mf_kv4_attn_args *args, void *d_ws, size_t ws_bytes, const KvPlan &p, KvAttnArgs &a,
+                                bool &none)
+{
+    none = batch->rows == 0 || batch->n_seq == 0 || batch->max_new == 0;
+    if (none) return MF_OK;
+    if (!args->d_q || !args->d_out || !aligned(args->d_q, 2) || !aligned(args->d_out, 2) || !aligned(args->d_lse, 4)) return MF_EINVAL;
+    const int64_t d = a.g.head_dim;
+    if (!strides_fit(batch->rows, args->q_stride, args->n_heads, args->q_head_stride, d, false) ||
+        !strides_fit(batch->rows, args->out_stride, args->n_heads, args->out_head_stride, d, true))
+        return MF_EINVAL;
+    if (ws_bytes < p.ws_bytes || (p.ws_bytes > 0 && !d_ws)) return MF_ENOMEM;
+    if (p.ws_bytes > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
+    a.q = args->d_q;
+    a.out = args->d_out;
+    a.lse = args->d_lse;
+    a.q_stride = args->q_stride;
+    a.q_head = args->q_head_stride;
+    a.out_stride = args->out_stride;
+    a.out_head = args->out_head_stride;
+    a.part = (float *)d_ws;
+    return MF_OK;
+}
+
 }  // namespace mfs

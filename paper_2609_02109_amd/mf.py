@@ -36,7 +36,7 @@ EXPORTS = ["mf_problem_bytes", "mf_problem_create", "mf_problem_destroy", "mf_sp
            "mf_w4_pack_bytes", "mf_w4_pack", "mf_w4_workspace_size", "mf_w4_matmul", "mf_kv4_cache_bytes", "mf_kv4_append", "mf_kv4_read",
            "mf_kv4_workspace_size", "mf_kv4_attention",
            "mf_rows8", "mf_norm8", "mf_gate8", "mf_rows8_values", "mf_w8_pack_bytes", "mf_w8_pack", "mf_w8_workspace_size", "mf_w8_matmul",
-           "mf_status_string"]
+           "mf_kv8_cache_bytes", "mf_kv8_append", "mf_kv8_read", "mf_kv8_workspace_size", "mf_kv8_attention", "mf_status_string"]
 
 
 class MfError(RuntimeError):
@@ -153,6 +153,11 @@ def _load():
         "mf_w8_pack": (S, [P, P, P, P, C.c_size_t, P]),
         "mf_w8_workspace_size": (S, [P, P]),
         "mf_w8_matmul": (S, [P, P, C.c_size_t, P]),
+        "mf_kv8_cache_bytes": (S, [P, P]),
+        "mf_kv8_append": (S, [P, P, P, P]),
+        "mf_kv8_read": (S, [P, P, S, P, P, P]),
+        "mf_kv8_workspace_size": (S, [P, P, P, P]),
+        "mf_kv8_attention": (S, [P, P, P, P, C.c_size_t, P]),
         "mf_status_string": (C.c_char_p, [S]),
     }
     for name, (res, args) in sig.items():

@@ -47,6 +47,10 @@ class Cache(C.Structure):
                 ("d_pages", _p)]
 
 
+class Cache8(C.Structure):
+    _fields_ = [("n_pages", _i32), ("page_size", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("d_pages", _p)]
+
+
 class Batch(C.Structure):
     _fields_ = [("n_seq", _i32), ("max_new", _i32), ("max_kv", _i32), ("rows", _i64), ("d_q_start", _p), ("d_kv_len", _p),
                 ("d_page_table", _p), ("table_stride", _i64), ("table_cols", _i32)]
@@ -457,7 +461,7 @@ def rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, device="cuda"):
 
 class KV4Batch:
     """The sequences of one step (mf_kv4_batch), shared by its append, reads
-    and attention; made by `KV4Cache.batch`.  The device tensors are read by
+    and attention; made by the cache's `batch`.  The device tensors are read by
     every call, so a server may update them in place between steps."""
 
     def __init__(self, q_start, kv_len, page_table, rows, max_new, max_kv):
@@ -476,22 +480,18 @@ class KV4Batch:
                          page_table.stride(0), int(page_table.shape[1]))
 
 
-class KV4Cache:
-    """A paged key/value cache in 4 bits: n_pages pages of page_size tokens for
-    n_kv_heads heads of head_dim values; `group` neighbouring values share a
-    scale and an offset.  `bytes_per_token` is what a token costs."""
+class _KVCache:
+    """What the paged caches share: n_pages pages of page_size tokens for n_kv_heads heads of head_dim values."""
 
-    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, group=64, device="cuda"):
-        self.device = torch.device(device)
-        self.raw = Cache(_int32(n_pages, "n_pages"), _int32(page_size, "page_size"), _int32(n_kv_heads, "n_kv_heads"),
-                         _int32(head_dim, "head_dim"), _int32(group, "group"), None)
+    def _lay_out(self, raw, bytes_call, n_pages, page_size, n_kv_heads, head_dim, kind, device):
+        self.raw, self.device = raw, torch.device(device)
         nb = C.c_size_t()
-        _check(mf.lib.mf_kv4_cache_bytes(C.byref(self.raw), C.byref(nb)), "mf_kv4_cache_bytes")
+        _check(getattr(mf.lib, bytes_call)(C.byref(self.raw), C.byref(nb)), bytes_call)
         self.pages = torch.empty(int(nb.value), dtype=torch.uint8, device=self.device)
         self.device = self.pages.device
         self.raw.d_pages = self.pages.data_ptr()
         self.n_kv_heads, self.head_dim, self.page_size = int(n_kv_heads), int(head_dim), int(page_size)
-        self._shape = (self.n_kv_heads, self.head_dim, int(group), self.page_size)
+        self._shape = (self.n_kv_heads, self.head_dim, kind, self.page_size)
         self.bytes_per_token = int(nb.value) // (int(n_pages) * self.page_size)
 
     def batch(self, q_start, kv_len, page_table, rows, max_new, max_kv) -> KV4Batch:
@@ -547,9 +547,9 @@ class KV4Cache:
                 qs, os = q.stride(), q_out.stride()
                 a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], *turn, heads, q.data_ptr(),
                                q_out.data_ptr(), qs[0], qs[1], os[0], os[1])
-        s = mf.lib.mf_kv4_append(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream_of(dev))
+        s = getattr(mf.lib, self._APPEND)(C.byref(self.raw), C.byref(batch.raw), C.byref(a), _stream_of(dev))
         if s:
-            _check(s, "mf_kv4_append")
+            _check(s, self._APPEND)
         return q_out
 
     def read(self, batch: KV4Batch, dtype=torch.float32, stream=None):
@@ -561,10 +561,10 @@ class KV4Cache:
         _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
         k = torch.empty((batch.rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
         v = torch.empty_like(k)
-        s = mf.lib.mf_kv4_read(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(),
+        s = getattr(mf.lib, self._READ)(C.byref(self.raw), C.byref(batch.raw), _DTYPES[dtype], k.data_ptr(), v.data_ptr(),
                                _stream_of(self.device))
         if s:
-            _check(s, "mf_kv4_read")
+            _check(s, self._READ)
         return k, v
 
     def attention(self, batch: KV4Batch, q, scale=None, window=0, lse=False, out=None, stream=None):
@@ -589,10 +589,36 @@ class KV4Cache:
         need = batch._ws_bytes.get(key)
         if need is None:
             nb = C.c_size_t()
-            _check(mf.lib.mf_kv4_workspace_size(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), "mf_kv4_workspace_size")
+            _check(getattr(mf.lib, self._WORKSPACE)(C.byref(self.raw), C.byref(batch.raw), C.byref(a), C.byref(nb)), self._WORKSPACE)
             need = batch._ws_bytes[key] = nb.value
         ws = _workspaces.get(need, self.device) if need else None
-        s = mf.lib.mf_kv4_attention(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws.data_ptr() if need else None, need, _stream_of(self.device))
+        s = getattr(mf.lib, self._ATTENTION)(C.byref(self.raw), C.byref(batch.raw), C.byref(a), ws.data_ptr() if need else None, need, _stream_of(self.device))
         if s:
-            _check(s, "mf_kv4_attention")
+            _check(s, self._ATTENTION)
         return out if ls is None else (out, ls)
+
+
+class KV4Cache(_KVCache):
+    """A paged key/value cache in 4 bits: n_pages pages of page_size tokens for
+    n_kv_heads heads of head_dim values; `group` neighbouring values share a
+    scale and an offset.  `bytes_per_token` is what a token costs."""
+
+    _APPEND, _READ, _WORKSPACE, _ATTENTION = "mf_kv4_append", "mf_kv4_read", "mf_kv4_workspace_size", "mf_kv4_attention"
+
+    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, group=64, device="cuda"):
+        raw = Cache(_int32(n_pages, "n_pages"), _int32(page_size, "page_size"), _int32(n_kv_heads, "n_kv_heads"), _int32(head_dim, "head_dim"),
+                    _int32(group, "group"), None)
+        self._lay_out(raw, "mf_kv4_cache_bytes", n_pages, page_size, n_kv_heads, head_dim, int(group), device)
+
+
+class KV8Cache(_KVCache):
+    """A paged key/value cache in 8 bits, used as the one in 4 bits: n_pages pages of
+    page_size tokens for n_kv_heads heads of head_dim values; 16 tokens of a head
+    share a scale for their keys and one for their values.  A step that begins inside
+    such a block needs the block's earlier tokens in the cache, or zeroed memory."""
+
+    _APPEND, _READ, _WORKSPACE, _ATTENTION = "mf_kv8_append", "mf_kv8_read", "mf_kv8_workspace_size", "mf_kv8_attention"
+
+    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, device="cuda"):
+        raw = Cache8(_int32(n_pages, "n_pages"), _int32(page_size, "page_size"), _int32(n_kv_heads, "n_kv_heads"), _int32(head_dim, "head_dim"), None)
+        self._lay_out(raw, "mf_kv8_cache_bytes", n_pages, page_size, n_kv_heads, head_dim, "8-bit", device)
