@@ -15,7 +15,9 @@ __device__ __forceinline__ u32x4 load8(const uint16_t *x, int k, int n)
 {
     if (k + 8 <= n) return load16(x + k);
     uint32_t w[4] = {0, 0, 0, 0};
-    for (int j = 0; k + j < n; j++) w[j >> 1] |= (uint32_t)x[k + j] << (16 * (j & 1));
+#pragma unroll
+    for (int j = 0; j < 7; j++)   // with indexes that are known: else the array is in memory
+        if (k + j < n) w[j >> 1] |= (uint32_t)x[k + j] << (16 * (j & 1));
     return (u32x4){w[0], w[1], w[2], w[3]};
 }
 __device__ __forceinline__ void store8(uint16_t *y, int k, int n, u32x4 v)
@@ -24,7 +26,9 @@ __device__ __forceinline__ void store8(uint16_t *y, int k, int n, u32x4 v)
         __builtin_memcpy(__builtin_assume_aligned(y + k, 2), &v, 16);
         return;
     }
-    for (int j = 0; k + j < n; j++) y[k + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+#pragma unroll
+    for (int j = 0; j < 7; j++)
+        if (k + j < n) y[k + j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
 }
 template <bool F16>
 __device__ __forceinline__ void widen8(u32x4 raw, float *v)
@@ -55,6 +59,52 @@ __device__ __forceinline__ X over_row(X v, X (&lds)[T / 64], const F &f)
     return v;
 }
 
+// Eight codes of a row from k on.
+__device__ __forceinline__ void put_codes(int8_t *out, int k, int n, const Row8 &r, const float *v)
+{
+    uint32_t c[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; j++) c[j >> 2] |= code8(r, v[j]) << (8 * (j & 3));
+    if (k + 8 <= n) {
+        __builtin_memcpy(out + k, c, 8);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 7; j++)
+        if (k + j < n) out[k + j] = (int8_t)(c[j >> 2] >> (8 * (j & 3)));
+}
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ float add(float p, float q) { return p + q; }
+__device__ __forceinline__ uint32_t larger(uint32_t p, uint32_t q) { return max(p, q); }
+
+// Eight elements of y before the norm's factors, in fp32: x, the sum of x and the residual (stored on the way), or the gate.
+template <bool F16, int OP>
+__device__ __forceinline__ void begin8(const Rows8Args &a, long long row, int k, u32x4 x, u32x4 y, float *v)
+{
+    widen8<F16>(x, v);
+    if (OP == kRowsPlain || (OP == kRowsNorm && !a.y)) return;
+    float u[8];
+    widen8<F16>(y, u);
+    if (OP == kRowsGate) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = gated(v[j], u[j]);
+        return;
+    }
+    u32x4 h;
+#pragma unroll
+    for (int j = 0; j < 4; j++) h[j] = pack2<F16>(v[2 * j] + u[2 * j], v[2 * j + 1] + u[2 * j + 1]);
+    store8((uint16_t *)a.sum + row * a.sum_stride, k, a.n, h);
+    widen8<F16>(h, v);   // what is carried on is what is normed
+}
+template <bool F16>
+__device__ __forceinline__ void weigh8(const Rows8Args &a, int k, float r, float *v)
+{
+    float w[8];
+    widen8<F16>(load8((const uint16_t *)a.weight, k, a.n), w);
+#pragma unroll
+    for (int j = 0; j < 8; j++) v[j] = v[j] * r * w[j];
+}
+
 template <bool F16, int OP, int T, int V>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rows8_kernel(Rows8Args a)
 {
@@ -75,69 +125,84 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows8_kernel(Rows8Args a)
             if (OP == kRowsGate || (OP == kRowsNorm && a.y)) with[i] = load8(y, k, n);
         }
         float sum = 0.f;
-        uint32_t top = 0;   // the largest magnitude's bits: infinities and NaN are above all others
+        uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < V; i++) {
             const int k = 8 * (t + i * T);
-            widen8<F16>(raw[i], v[i]);
-            float u[8];
-            if (OP == kRowsGate || OP == kRowsNorm) widen8<F16>(with[i], u);
-            if (OP == kRowsGate) {
 #pragma unroll
-                for (int j = 0; j < 8; j++) v[i][j] = gated(v[i][j], u[j]);
-            }
+            for (int j = 0; j < 8; j++) v[i][j] = 0.f;
+            if (k < n) begin8<F16, OP>(a, row, k, raw[i], with[i], v[i]);
             if (OP == kRowsNorm) {
-                if (a.y) {
-                    u32x4 h;
-#pragma unroll
-                    for (int j = 0; j < 4; j++) h[j] = pack2<F16>(v[i][2 * j] + u[2 * j], v[i][2 * j + 1] + u[2 * j + 1]);
-                    if (k < n) store8((uint16_t *)a.sum + row * a.sum_stride, k, n, h);
-                    widen8<F16>(h, v[i]);   // what is carried on is what is normed
-                }
 #pragma unroll
                 for (int j = 0; j < 8; j++) sum += v[i][j] * v[i][j];
             }
         }
         if (OP == kRowsNorm) {
-            sum = over_row<T>(sum, sums, [](float p, float q) { return p + q; });
+            sum = over_row<T>(sum, sums, add);
             const float r = 1.f / sqrtf(sum / (float)n + a.eps);
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                const int k = 8 * (t + i * T);
-                if (k >= n) continue;
-                float w[8];
-                widen8<F16>(load8((const uint16_t *)a.weight, k, n), w);
-#pragma unroll
-                for (int j = 0; j < 8; j++) v[i][j] = v[i][j] * r * w[j];
-            }
+            for (int i = 0; i < V; i++)
+                if (8 * (t + i * T) < n) weigh8<F16>(a, 8 * (t + i * T), r, v[i]);
             if (!(sum < INFINITY)) top = 0x7fffffffu;
         }
 #pragma unroll
         for (int i = 0; i < V; i++)
 #pragma unroll
-            for (int j = 0; j < 8; j++) top = max(top, __float_as_uint(v[i][j]) & 0x7fffffffu);
-        top = over_row<T>(top, tops, [](uint32_t p, uint32_t q) { return max(p, q); });
-        const bool bad = top >= 0x7f800000u;
-        float scale = __uint_as_float(top) * (float)(1.0 / 127.0);
-        if (scale < 0x1p-126f) scale = 0.f;   // below it 1 / scale may leave fp32
-        const float inv = scale > 0.f && !bad ? 1.f / scale : 0.f;
-        if (t == 0) a.scales[row] = bad ? NAN : scale;
+            for (int j = 0; j < 8; j++) top = max(top, magnitude(v[i][j]));
+        const Row8 r = row8_of(over_row<T>(top, tops, larger));
+        if (t == 0) a.scales[row] = r.scale;
         int8_t *out = a.codes + row * a.codes_stride;
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            const int k = 8 * (t + i * T);
-            if (k >= n) continue;
-            uint32_t c[2] = {0, 0};
+        for (int i = 0; i < V; i++)
+            if (8 * (t + i * T) < n) put_codes(out, 8 * (t + i * T), n, r, v[i]);
+    }
+}
+
+// Rows that registers do not hold: three passes over them (two without a norm), the later ones over what the caches have.
+template <bool F16, int OP>
+__global__ __launch_bounds__(1024) void rows8_wide_kernel(Rows8Args a)
+{
+    constexpr int T = 1024;
+    __shared__ float sums[T / 64];
+    __shared__ uint32_t tops[T / 64];
+    const int n = a.n;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const uint16_t *x = (const uint16_t *)a.x + row * a.x_stride, *y = (const uint16_t *)a.y + row * a.y_stride;
+        const uint16_t *h = OP == kRowsNorm && a.y ? (const uint16_t *)a.sum + row * a.sum_stride : x;
+        const u32x4 none = {0, 0, 0, 0};
+        float sum = 0.f, r = 1.f;
+        if (OP == kRowsNorm) {
+            for (int k = 8 * (int)threadIdx.x; k < n; k += 8 * T) {
+                float v[8];
+                begin8<F16, OP>(a, row, k, load8(x, k, n), a.y ? load8(y, k, n) : none, v);
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const int q = bad ? 0 : (int)fminf(fmaxf(rintf(v[i][j] * inv), -127.f), 127.f);
-                c[j >> 2] |= (uint32_t)(q & 255) << (8 * (j & 3));
+                for (int j = 0; j < 8; j++) sum += v[j] * v[j];
             }
-            if (k + 8 <= n) {
-                __builtin_memcpy(out + k, c, 8);
+            sum = over_row<T>(sum, sums, add);
+            r = 1.f / sqrtf(sum / (float)n + a.eps);
+        }
+        // what a thread has stored of h is its own to read
+        const auto get = [&](int k, float *v) {
+            if (OP == kRowsNorm) {
+                widen8<F16>(load8(h, k, n), v);
+                weigh8<F16>(a, k, r, v);
             } else {
-                for (int j = 0; k + j < n; j++) out[k + j] = (int8_t)(c[j >> 2] >> (8 * (j & 3)));
+                begin8<F16, OP>(a, row, k, load8(x, k, n), OP == kRowsGate ? load8(y, k, n) : none, v);
             }
+        };
+        uint32_t top = !(sum < INFINITY) ? 0x7fffffffu : 0u;
+        for (int k = 8 * (int)threadIdx.x; k < n; k += 8 * T) {
+            float v[8];
+            get(k, v);
+#pragma unroll
+            for (int j = 0; j < 8; j++) top = max(top, magnitude(v[j]));
+        }
+        const Row8 q = row8_of(over_row<T>(top, tops, larger));
+        if (threadIdx.x == 0) a.scales[row] = q.scale;
+        for (int k = 8 * (int)threadIdx.x; k < n; k += 8 * T) {
+            float v[8];
+            get(k, v);
+            put_codes(a.codes + row * a.codes_stride, k, n, q, v);
         }
     }
 }
@@ -156,10 +221,14 @@ __global__ __launch_bounds__(256) void values8_kernel(Values8Args a)
         int8_t q[8] = {};
         if (many == 8) __builtin_memcpy(q, c, 8);
         else
-            for (int j = 0; j < many; j++) q[j] = c[j];
+#pragma unroll
+            for (int j = 0; j < 7; j++)
+                if (j < many) q[j] = c[j];
         const long long at = row * a.out_stride + k;
         if constexpr (TY == MF_F32) {
-            for (int j = 0; j < many; j++) ((float *)a.out)[at + j] = (float)q[j] * s;
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (j < many) ((float *)a.out)[at + j] = (float)q[j] * s;
         } else {
             u32x4 o;
 #pragma unroll
@@ -187,8 +256,9 @@ hipError_t pick(const Rows8Args &a, hipStream_t s)
     if (a.n <= 4096) return go<F16, OP, 256, 2>(a, s);
     if (a.n <= 8192) return go<F16, OP, 256, 4>(a, s);
     if (a.n <= 16384) return go<F16, OP, 256, 8>(a, s);
-    if (a.n <= 65536) return go<F16, OP, 1024, 8>(a, s);
-    return go<F16, OP, 1024, 16>(a, s);
+    const long long most = most_workgroups(1024);
+    hipLaunchKernelGGL((rows8_wide_kernel<F16, OP>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(1024), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace

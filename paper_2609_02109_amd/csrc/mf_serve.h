@@ -216,19 +216,20 @@ struct Values8Args {
 hipError_t launch_values8(const Values8Args &a, int dtype, hipStream_t s);
 
 // ------------------------------------------------------- packed 8-bit weights
-// [N / 16][K / 64] records of 1024 bytes: lane l of a wave holds 16 of them, the
-// inputs k = 16 (l / 16) .. + 15 of output l % 16, the A operand of
+// [N / 16][K / 64] records of 1024 bytes, an even number of them a tile: lane l of a
+// wave holds 16 of them, the inputs k = 16 (l / 16) .. + 15 of output l % 16, the A operand of
 // v_mfma_i32_16x16x64_i8.  Outputs past N and inputs past K have code 0.  After
-// the records N scales.
+// the records the scales of all tiles' outputs, 0 past N.
 constexpr int kW8Tile = 16, kW8Chunk = 64, kW8Record = kW8Tile * kW8Chunk;
 constexpr long long kW8MostOut = most_workgroups(512) * kW8Tile;   // as kW4MostOut
 constexpr int kW8MostIn = 131056;   // 2^14 K < 2^31: products of codes down to -128, in 32 bits
-__host__ __device__ constexpr long long w8_chunks(int n_in) { return (n_in + kW8Chunk - 1) / kW8Chunk; }
+__host__ __device__ constexpr long long w8_chunks(int n_in) { return (n_in + 2 * kW8Chunk - 1) / (2 * kW8Chunk) * 2; }
 struct W8Args {
     const uint8_t *packed;
     const float *w_scales;
     const int8_t *x;
-    const float *x_scales;
+    const float *x_scales;   // null: x16, rows of the type, are put into 8 bits by the product itself
+    const void *x16;
     const void *bias;
     void *y;
     long long x_stride, y_stride;
@@ -241,12 +242,16 @@ struct W8PackArgs {
     int n_out, n_in;
 };
 hipError_t launch_w8_pack(const W8PackArgs &a, hipStream_t s);
-enum W8Form { kW8Few1, kW8Few2, kW8Few4, kW8Tiles };
-struct W8Plan {
-    W8Form form;
-    size_t ws_bytes;
+enum W8Form {
+    kW8Few16, kW8Few8x2,                                    // up to 16 rows: waves of a workgroup (x tiles of outputs)
+    kW8Rows32, kW8Rows32x4,                                 // up to 32
+    kW8Block32, kW8Block64, kW8Block64x4, kW8Block128x4,    // rows of a block (x tiles of outputs, else two)
+    kW8Tiles128, kW8Tiles256                                // by 256 outputs
 };
-W8Plan w8_plan(int rows, int n_out, int n_in);
-hipError_t launch_w8(const W8Args &a, const W8Plan &p, bool f16, void *ws, hipStream_t s);
+// How the work is laid over the card, and whether rows in 16 bits are put into 8 in the product's own kernel: functions of
+// the sizes alone.
+W8Form w8_form(int rows, int n_out, int n_in);
+bool w8_takes_16(int rows, int n_in);
+hipError_t launch_w8(const W8Args &a, bool f16, hipStream_t s);
 
 }  // namespace mfs

@@ -49,7 +49,7 @@ mf_status check_w8_rows(const mf_w8_args *a)
 }
 
 size_t w8_records(const mf_w8_desc &d) { return (size_t)((d.n_out + kW8Tile - 1) / kW8Tile) * (size_t)w8_chunks((int)d.n_in) * kW8Record; }
-size_t w8_bytes(const mf_w8_desc &d) { return w8_records(d) + (size_t)d.n_out * sizeof(float); }
+size_t w8_bytes(const mf_w8_desc &d) { return w8_records(d) + (size_t)((d.n_out + kW8Tile - 1) / kW8Tile) * kW8Tile * sizeof(float); }
 
 mf_status check_cache8(const mf_kv8_cache *c, KvGeom &g)
 {
@@ -68,11 +68,12 @@ mf_status check_cache8(const mf_kv8_cache *c, KvGeom &g)
     return MF_OK;
 }
 
-// The workspace: what the product itself needs, then the codes and the scales of rows that come in 16 bits.
+// The workspace: codes and scales of rows that come in 16 bits, where the product does not put them into 8 itself.
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
-size_t w8_ws(const mf_w8_args &a, const W8Plan &p)
+size_t w8_ws(const mf_w8_args &a)
 {
-    return a.d_x_scales ? p.ws_bytes : up256(p.ws_bytes) + up256((size_t)a.rows * (size_t)a.w.n_in) + (size_t)a.rows * sizeof(float);
+    if (a.rows == 0 || a.d_x_scales || w8_takes_16((int)a.rows, (int)a.w.n_in)) return 0;
+    return up256((size_t)a.rows * (size_t)a.w.n_in) + (size_t)a.rows * sizeof(float);
 }
 
 }  // namespace
@@ -170,7 +171,7 @@ mf_status mf_w8_workspace_size(const mf_w8_args *args, size_t *bytes)
 {
     if (!args || !bytes) return MF_EINVAL;
     const mf_status st = check_w8_rows(args);
-    if (st == MF_OK) *bytes = args->rows > 0 ? w8_ws(*args, w8_plan((int)args->rows, (int)args->w.n_out, (int)args->w.n_in)) : 0;
+    if (st == MF_OK) *bytes = w8_ws(*args);
     return st;
 }
 
@@ -185,10 +186,14 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
         !aligned(args->d_x_scales, 4) || !aligned(args->d_y, 2) || !aligned(args->d_bias, 2))
         return MF_EINVAL;
     if (!row_stride(args->rows, args->x_stride, w.n_in, false) || !row_stride(args->rows, args->y_stride, w.n_out, true)) return MF_EINVAL;
+    const size_t need = w8_ws(*args);
+    if (need > 0 && (ws_bytes < need || !d_ws)) return MF_ENOMEM;
+    if (need > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
     W8Args a;
     a.packed = (const uint8_t *)args->d_packed;
     a.w_scales = (const float *)(a.packed + w8_records(w));
     a.x = (const int8_t *)args->d_x;
+    a.x16 = args->d_x;
     a.x_scales = args->d_x_scales;
     a.bias = args->d_bias;
     a.y = args->d_y;
@@ -198,17 +203,13 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
     a.n_out = (int)w.n_out;
     a.n_in = (int)w.n_in;
     const bool f16 = as_int(w.dtype) == MF_F16;
-    const W8Plan p = w8_plan(a.rows, a.n_out, a.n_in);
-    const size_t need = w8_ws(*args, p);
-    if (need > 0 && (ws_bytes < need || !d_ws)) return MF_ENOMEM;
-    if (need > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
-    if (!args->d_x_scales) {
+    if (need > 0) {
         Rows8Args r = {};
         r.x = args->d_x;
         r.x_stride = args->x_stride;
         r.rows = a.rows;
         r.n = a.n_in;
-        r.codes = (int8_t *)d_ws + up256(p.ws_bytes);
+        r.codes = (int8_t *)d_ws;
         r.codes_stride = a.n_in;
         r.scales = (float *)(r.codes + up256((size_t)a.rows * a.n_in));
         const hipError_t e = launch_rows8(r, kRowsPlain, f16, (hipStream_t)stream);
@@ -217,7 +218,7 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
         a.x_stride = r.codes_stride;
         a.x_scales = r.scales;
     }
-    return of(launch_w8(a, p, f16, d_ws, (hipStream_t)stream));
+    return of(launch_w8(a, f16, (hipStream_t)stream));
 }
 
 mf_status mf_kv8_cache_bytes(const mf_kv8_cache *cache, size_t *bytes)

@@ -111,6 +111,25 @@ __device__ __forceinline__ u32x4 codes8(uint32_t w, const CodeBits &b)
     return (u32x4){codes2<F16, 0>(w, b), codes2<F16, 1>(w, b), codes2<F16, 2>(w, b), codes2<F16, 3>(w, b)};
 }
 
+// A row of y in 8 bits: what its largest magnitude (as bits, for infinities and NaN are above all others) makes of it.
+struct Row8 {
+    float scale, inv;
+    bool bad;   // an infinity or a NaN: the scale is a NaN, the codes are 0
+};
+__device__ __forceinline__ Row8 row8_of(uint32_t top)
+{
+    Row8 r;
+    r.bad = top >= 0x7f800000u;
+    const float scale = __uint_as_float(top) * (float)(1.0 / 127.0);
+    r.scale = r.bad ? __uint_as_float(0x7fc00000u) : scale < 0x1p-126f ? 0.f : scale;   // below that 1 / scale may leave fp32
+    r.inv = r.scale > 0.f ? 1.f / scale : 0.f;
+    return r;
+}
+__device__ __forceinline__ uint32_t code8(const Row8 &r, float y)
+{
+    return r.bad ? 0u : (uint32_t)(int)fminf(fmaxf(rintf(y * r.inv), -127.f), 127.f) & 255u;
+}
+
 // D += A B, 16 x 16 x 32: lane l holds A[l % 16][8 (l / 16) ..+8], B[8 (l / 16) ..+8][l % 16], D[4 (l / 16) + r][l % 16].
 template <bool F16>
 __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)

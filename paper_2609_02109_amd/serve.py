@@ -288,23 +288,25 @@ class Rows8(NamedTuple):
     def _checked(self):
         """Codes as a matrix, and the scales."""
         codes, scales = self
-        _require(isinstance(codes, torch.Tensor) and codes.dtype is torch.int8 and codes.is_cuda and codes.dim() > 0 and codes.shape[-1] > 0,
-                 "codes: an int8 [.., N] tensor on the GPU is wanted")
-        _require(isinstance(scales, torch.Tensor) and scales.dtype is torch.float32 and scales.device == codes.device
-                 and scales.shape == codes.shape[:-1], "scales: float32 [..] beside the codes is wanted")
+        if not isinstance(codes, torch.Tensor) or codes.dtype is not torch.int8 or not codes.is_cuda or codes.dim() == 0 or codes.shape[-1] == 0:
+            raise ValueError("codes: an int8 [.., N] tensor on the GPU is wanted")
+        if (not isinstance(scales, torch.Tensor) or scales.dtype is not torch.float32 or scales.device != codes.device
+                or scales.shape != codes.shape[:-1]):
+            raise ValueError("scales: float32 [..] beside the codes is wanted")
         if scales.requires_grad:
             _no_gradient()
-        return _matrix(codes, "codes", codes.shape[-1], torch.int8, codes.device), scales if scales.is_contiguous() else scales.contiguous()
+        if codes.dim() != 2 or not codes.is_contiguous():
+            codes = _matrix(codes, "codes", codes.shape[-1], torch.int8, codes.device)
+        return codes, scales if scales.is_contiguous() else scales.contiguous()
 
     def values(self, dtype=torch.float32, stream=None):
         """What the rows stand for, [.., N] in dtype."""
-        device = self.codes.device
-        if device.type == "cuda" and (stream is not None or device.index != _current_device()):
-            return _on(device, stream, tuple(self), lambda: self.values(dtype))
+        if _elsewhere(self[0], stream):
+            return _on(self[0].device, stream, tuple(self), lambda: self.values(dtype))
         codes, scales = self._checked()
-        _require(dtype in _DTYPES, "dtype: float32, bfloat16 or float16 is wanted")
-        out = torch.empty(self.codes.shape, dtype=dtype, device=device)
-        n = codes.shape[1]
+        if dtype not in _DTYPES:
+            raise ValueError("dtype: float32, bfloat16 or float16 is wanted")
+        out, n, device = codes.new_empty(self[0].shape, dtype=dtype), codes.shape[1], codes.device
         s = mf.lib.mf_rows8_values(_DTYPES[dtype], codes.shape[0], n, codes.data_ptr(), codes.stride(0), scales.data_ptr(), out.data_ptr(), n,
                                    _stream_of(device))
         if s:
@@ -314,17 +316,24 @@ class Rows8(NamedTuple):
 
 def _rows8_of(x, name):
     """x as a matrix, the Rows8 that it is put into, and the call's arguments."""
-    _require(isinstance(x, torch.Tensor) and x.dtype in _HALF and x.is_cuda and x.dim() > 0 and x.shape[-1] > 0,
-             f"{name}: bfloat16 or float16 [.., N] on the GPU is wanted")
-    m = _matrix(x, name, x.shape[-1], x.dtype, x.device)
-    rows = Rows8(torch.empty(x.shape, dtype=torch.int8, device=x.device), torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device))
-    n = m.shape[1]
-    return m, rows, Rows8Args(_DTYPES[x.dtype], m.shape[0], n, m.data_ptr(), m.stride(0), rows.codes.data_ptr(), n, rows.scales.data_ptr())
+    if not isinstance(x, torch.Tensor) or x.dtype not in _HALF or not x.is_cuda or x.dim() == 0 or x.shape[-1] == 0:
+        raise ValueError(f"{name}: bfloat16 or float16 [.., N] on the GPU is wanted")
+    shape, dt = x.shape, x.dtype
+    n = shape[-1]
+    if len(shape) == 2 and x.is_contiguous() and not x.requires_grad:
+        m, codes, rows, stride = x, torch.empty_like(x, dtype=torch.int8), shape[0], n
+    else:
+        m, codes = _matrix(x, name, n, dt, x.device), x.new_empty(shape, dtype=torch.int8)
+        rows, stride = m.shape[0], m.stride(0)
+    scales = x.new_empty(shape[:-1], dtype=torch.float32)
+    return m, Rows8(codes, scales), Rows8Args(_DTYPES[dt], rows, n, m.data_ptr(), stride, codes.data_ptr(), n, scales.data_ptr())
 
 
 def _elsewhere(x, stream):
     """Whether a call with x has to change the current device or stream first."""
-    return stream is not None or (isinstance(x, torch.Tensor) and x.is_cuda and x.device.index != _current_device())
+    if stream is not None:
+        return True
+    return isinstance(x, torch.Tensor) and x.is_cuda and x.device.index != _current_device()
 
 
 def quantise_rows(x, stream=None) -> Rows8:
@@ -345,19 +354,24 @@ def norm_rows(x, weight, residual=None, eps=1e-6, out=None, stream=None):
         return _on(x.device, stream, (x, weight, residual, out), lambda: norm_rows(x, weight, residual, eps, out))
     carried = x
     x, rows, a = _rows8_of(x, "x")
-    n, dt, dev = x.shape[1], x.dtype, x.device
-    _require(isinstance(weight, torch.Tensor) and tuple(weight.shape) == (n,) and weight.dtype is dt and weight.device == dev,
-             f"weight: [{n}] {dt} on {dev} is wanted")
+    n, dt, dev = a.n, x.dtype, x.device
+    if not isinstance(weight, torch.Tensor) or weight.shape != (n,) or weight.dtype is not dt or weight.device != dev:
+        raise ValueError(f"weight: [{n}] {dt} on {dev} is wanted")
     if weight.requires_grad:
         _no_gradient()
-    weight = weight if weight.is_contiguous() else weight.contiguous()
+    if not weight.is_contiguous():
+        weight = weight.contiguous()
     if residual is None:
         _require(out is None, "out: with a residual only, without one h is x")
         a = Norm8Args(a, None, 0, None, 0, weight.data_ptr(), eps)
     else:
-        _require(isinstance(residual, torch.Tensor) and residual.shape == carried.shape, f"residual: {tuple(carried.shape)} is wanted")
+        if not isinstance(residual, torch.Tensor) or residual.shape != carried.shape:
+            raise ValueError(f"residual: {tuple(carried.shape)} is wanted")
         residual = _matrix(residual, "residual", n, dt, dev)
-        carried = torch.empty(carried.shape, dtype=dt, device=dev) if out is None else _into(out, "out", carried.shape, dt, dev)
+        if out is None:
+            carried = _like(carried)
+        else:
+            carried = _into(out, "out", carried.shape, dt, dev)
         h = carried if carried.dim() == 2 else carried.view(-1, n)
         a = Norm8Args(a, residual.data_ptr(), residual.stride(0), h.data_ptr(), h.stride(0), weight.data_ptr(), eps)
     s = mf.lib.mf_norm8(C.byref(a), _stream_of(dev))
@@ -417,12 +431,15 @@ class W8Weight:
             return _on(self.device, stream, (held, bias, out, self.packed), lambda: self.matmul(x, bias, out))
         dt, dev, k, n = self.dtype, self.device, self.n_in, self.n_out
         if isinstance(x, tuple):
-            lead = x[0].shape[:-1]
-            x, xs = Rows8(*x)._checked()
-            _require(x.shape[1] == k and x.device == dev, f"x: rows of {k} on {dev} are wanted")
+            rows = x if type(x) is Rows8 else Rows8(*x)
+            x, xs = rows._checked()
+            if x.shape[1] != k or x.device != dev:
+                raise ValueError(f"x: rows of {k} on {dev} are wanted")
+            lead = rows[0].shape[:-1]
             scales = xs.data_ptr()
         else:
-            _require(isinstance(x, torch.Tensor), f"x: Rows8, or [.., {k}] {dt}, is wanted")
+            if not isinstance(x, torch.Tensor):
+                raise ValueError(f"x: Rows8, or [.., {k}] {dt}, is wanted")
             lead, scales = x.shape[:-1], None
             x = _matrix(x, "x", k, dt, dev)
         if bias is not None:
@@ -432,10 +449,11 @@ class W8Weight:
                 _no_gradient()
         m = x.shape[0]
         if out is None:
-            out = torch.empty((*lead, n), dtype=dt, device=dev)
+            y = x.new_empty((m, n), dtype=dt)
+            out = y if len(lead) == 1 else y.view(*lead, n)
         else:
             _into(out, "out", (*lead, n), dt, dev)
-        y = out if out.dim() == 2 else out.view(-1, n)
+            y = out if out.dim() == 2 else out.view(-1, n)
         a = W8Args(self.desc, self._packed_ptr, x.data_ptr(), scales, None if bias is None else bias.data_ptr(), y.data_ptr(), m, x.stride(0),
                    y.stride(0))
         key = (m, scales is None)

@@ -11,7 +11,9 @@ result's type (2^-8 bfloat16, 2^-11 binary16) and e = 2^-24, fp32's:
   is then within half a code and 127 * 2 * 2^-16 of one.
 * gate: the exponent is rounded by |g| e, four operations more: below 2^-16 for |g| <= 200.
 * products: the sum is exact; its conversion, two products and the bias's addition
-  are off by at most 4 e of the larger terms, and the result is rounded once.
+  are off by at most 4 e of the larger terms, and the result is rounded once.  Half a
+  step is u |y| down to the type's smallest normal number; below it steps are even,
+  2^-24 in binary16, so that half of one is 2^-25 there (bfloat16's are below all of this).
 """
 import math
 
@@ -197,14 +199,16 @@ def _rows(m, k, seed):
 def _check(y, codes, scales, wc, ws, bias, dt):
     part = (codes.double() @ wc.double().T) * scales.double()[:, None] * ws.double()
     want = part if bias is None else part + bias.double()
-    tol = UNIT[dt] * want.abs() + 4 * E * (part.abs() + (0 if bias is None else bias.double().abs())) + 1e-30
+    tol = UNIT[dt] * want.abs() + 4 * E * (part.abs() + (0 if bias is None else bias.double().abs())) + (2.0 ** -25 if dt == "f16" else 1e-30)
     err = (y.cpu().double() - want).abs()
     assert (err <= tol).all(), float((err / tol).max())
 
 
 SIZES = [(1, 16, 16), (1, 1, 64), (2, 17, 80), (3, 515, 160), (16, 64, 256), (17, 250, 400), (32, 1000, 1120), (33, 100, 576), (64, 4096, 512),
          (65, 48, 2048), (77, 333, 4112), (128, 128, 128), (129, 257, 144), (200, 33, 96), (300, 700, 1040), (5, 31, 16384), (16, 20000, 128),
-         (513, 1025, 272), (4, 8, 131056)]
+         (513, 1025, 272), (4, 8, 131056),
+         # the forms for many rows or outputs
+         (20, 17000, 80), (4, 6000, 8192), (5, 300, 8208), (130, 5000, 400), (500, 4100, 272), (3000, 2500, 144), (4090, 4090, 208)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
