@@ -54,9 +54,8 @@ __device__ __forceinline__ u32x4 value_operand(uint32_t a, uint32_t b)
     return o;
 }
 
-// Blocks of a step: where their records are, which there are, and what their scales come to.
+// Blocks of a step: which there are, and what their scales come to.
 struct Step8 {
-    const uint8_t *rec[2];
     int ok;
     float ks[2], lv[2], iv[2];   // the keys' scale; log2 of the values' scale, and 1 / it
 };
@@ -67,64 +66,88 @@ __device__ __forceinline__ bool sees8(const Sight &v, int ok, int t0, int qt, in
     return (ok >> (e >> 2) & 1) && tok >= v.lo && tok <= v.hi;
 }
 
-// keys_done, values_done: called where the step has no more use for its keys and its values, to
-// fetch the next step's into their place.  full: every row sees every token.  c: softmax scale times log2 e, and the
-// row's power of two; first: what its scores begin at.
-template <int D, int RT, class FK, class FV>
-__device__ __forceinline__ void attn8_step(f32x4 (&o)[RT][D / 16], float (&base)[RT], float (&l)[RT], const u32x4 (&q)[RT][D / 32],
-                                           const float (&first)[RT], const Attn8Tokens<D> &x, const Sight (&see)[RT], bool full,
-                                           const Step8 &now, int t0, const float (&c)[RT], const FK &keys_done, const FV &values_done)
+// What a wave keeps for its rows (lane l's is row l % 16 of each tile): queries q, what they see, c (softmax scale times log2 e,
+// and the row's power of two), first (what its scores begin at), base, l, and o (dims 16 d + 4 (l / 16) ..). As arrays
+// by themselves: in a struct they take 30 registers more.
+//
+// key_at(u, n), value_at(n): operands (dims 64 (n / 2) + 16 (l / 16) + 8 (n % 2) .. of block u's keys, dims 16 n + l % 16 of the
+// values).
+template <int D, int RT, class AK>
+__device__ __forceinline__ void attn8_scores(const u32x4 (&q)[RT][D / 32], const float (&first)[RT], f32x4 (&sc)[RT][2], const AK &key_at)
 {
-    constexpr int NC = D / 64;
-    const int qt = (threadIdx.x & 63) >> 4;
-    f32x4 sc[RT][2];
 #pragma unroll
     for (int u = 0; u < 2; u++) {
 #pragma unroll
         for (int t = 0; t < RT; t++) sc[t][u] = (f32x4){first[t], first[t], first[t], first[t]};
 #pragma unroll
-        for (int j = 0; j < NC; j++)
+        for (int n = 0; n < D / 32; n++) {
+            const u32x4 A = key_at(u, n);
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const u32x4 A = key_operand(x.kc[u][j][2 * i], x.kc[u][j][2 * i + 1]);
-#pragma unroll
-                for (int t = 0; t < RT; t++) sc[t][u] = mfma<true>(A, q[t][2 * j + i], sc[t][u]);
-            }
+            for (int t = 0; t < RT; t++) sc[t][u] = mfma<true>(A, q[t][n], sc[t][u]);
+        }
     }
-    keys_done();
-    u32x4 w[RT];
-    float e[RT][8];
-    for (bool raised = false;; raised = true) {   // twice at most
-        int highest[RT], over = 0;
-        constexpr int most = (15 + 14) << 10;   // 2^14 in binary16
+}
+
+// x anew: what is computed from it is computed here, not before a loop or a branch and kept in registers.
+__device__ __forceinline__ int again(int x)
+{
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
+// What S times 32 tokens from t0 on add to the rows, by their scores.  full: every row sees every token.
+template <int D, int RT, int S, class AV>
+__device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Sight (&see)[RT], const float (&c)[RT], float (&base)[RT], float (&l)[RT],
+                                           f32x4 (&o)[RT][D / 16], bool full, const Step8 (&now)[S], int t0, const AV &value_at)
+{
+    const int qt = (threadIdx.x & 63) >> 4;
+    u32x4 w[S][RT];
+    float sum[S][RT][2];   // of a block's weights
+    int highest[RT];
+    constexpr int most = (15 + 14) << 10;   // 2^14 in binary16
+    const auto weigh = [&] {
+        int over = 0;
 #pragma unroll
         for (int t = 0; t < RT; t++) {
+            u16x2 high = {0, 0};
 #pragma unroll
-            for (int i = 0; i < 8; i++) e[t][i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i >> 2][i & 3], now.ks[i >> 2] * c[t], now.lv[i >> 2] - base[t]));
-            if (!full) {
+            for (int k = 0; k < S; k++) {
+                float e[8];
 #pragma unroll
                 for (int i = 0; i < 8; i++)
-                    if (!sees8(see[t], now.ok, t0, qt, i)) e[t][i] = 0.f;
-            }
+                    e[i] = __builtin_amdgcn_exp2f(fmaf(sc[k][t][i >> 2][i & 3], now[k].ks[i >> 2] * c[t], now[k].lv[i >> 2] - base[t]));
+                if (!full) {
+                    const int at = again(t0 + 32 * k);   // else the comparisons are made for every step
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[t][i] = pack2<true>(e[t][2 * i], e[t][2 * i + 1]);
-            // none is negative: as whole numbers they are in the same order
-            const u16x2 high = __builtin_elementwise_max(__builtin_elementwise_max(bits<u16x2>(w[t][0]), bits<u16x2>(w[t][1])),
-                                                         __builtin_elementwise_max(bits<u16x2>(w[t][2]), bits<u16x2>(w[t][3])));
+                    for (int i = 0; i < 8; i++)
+                        if (!sees8(see[t], now[k].ok, at, qt, i)) e[i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) w[k][t][i] = pack2<true>(e[2 * i], e[2 * i + 1]);
+#pragma unroll
+                for (int u = 0; u < 2; u++) sum[k][t][u] = (e[4 * u] + e[4 * u + 1]) + (e[4 * u + 2] + e[4 * u + 3]);   // before they are rounded
+                // none is negative: as whole numbers they are in the same order
+#pragma unroll
+                for (int i = 0; i < 4; i++) high = __builtin_elementwise_max(high, bits<u16x2>(w[k][t][i]));
+            }
             highest[t] = max(high[0], high[1]);
             over = max(over, highest[t]);
         }
-        if (raised || !__any(over >= most)) break;
+        return __any(over >= most);
+    };
+    if (weigh()) {
 #pragma unroll
         for (int t = 0; t < RT; t++) {
             // only the rows that need it, so that no row's result depends on another's
             const bool hit = quarters_max((float)highest[t]) >= (float)most;
             float mx = kNoBase;
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float s = fmaf(sc[t][i >> 2][i & 3], now.ks[i >> 2] * c[t], now.lv[i >> 2]);
-                if (full || sees8(see[t], now.ok, t0, qt, i)) mx = fmaxf(mx, s);
-            }
+            for (int k = 0; k < S; k++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float s = fmaf(sc[k][t][i >> 2][i & 3], now[k].ks[i >> 2] * c[t], now[k].lv[i >> 2]);
+                    if (full || sees8(see[t], now[k].ok, t0 + 32 * k, qt, i)) mx = fmaxf(mx, s);
+                }
             mx = quarters_max(mx) - 10.f;
             const float to = hit ? fmaxf(mx, base[t]) : base[t], a = __builtin_amdgcn_exp2f(base[t] - to);
             base[t] = to;
@@ -132,122 +155,59 @@ __device__ __forceinline__ void attn8_step(f32x4 (&o)[RT][D / 16], float (&base)
 #pragma unroll
             for (int d = 0; d < D / 16; d++) o[t][d] *= a;
         }
+        weigh();
     }
 #pragma unroll
-    for (int t = 0; t < RT; t++)
+    for (int k = 0; k < S; k++)
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            const float sum = (e[t][4 * u] + e[t][4 * u + 1]) + (e[t][4 * u + 2] + e[t][4 * u + 3]), more = fmaf(sum, now.iv[u], l[t]);
-            // scales of blocks that the row does not see may be anything, not a number too
-            l[t] = full || sum != 0.f ? more : l[t];
+        for (int t = 0; t < RT; t++)
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const float more = fmaf(sum[k][t][u], now[k].iv[u], l[t]);
+                // scales of blocks that the row does not see may be anything, not a number too
+                l[t] = full || sum[k][t][u] != 0.f ? more : l[t];
+            }
+#pragma unroll
+    for (int k = 0; k < S; k++)
+#pragma unroll
+        for (int n = 0; n < D / 16; n++) {
+            const u32x4 A = value_at(k, n);
+#pragma unroll
+            for (int t = 0; t < RT; t++) o[t][n] = mfma<true>(A, w[k][t], o[t][n]);
         }
-#pragma unroll
-    for (int j = 0; j < NC; j++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const u32x4 A = value_operand(x.vc[0][j][i], x.vc[1][j][i]);
-#pragma unroll
-            for (int t = 0; t < RT; t++) o[t][4 * j + i] = mfma<true>(A, w[t], o[t][4 * j + i]);
-        }
-    values_done();
 }
 
-// Rows row0 .. of one sequence and key head over its tokens [begin, end):
-// into the output (slot < 0) or a slot of the parts.
-// NW: waves that share the rows and take different tokens; 0: the wave has rows of its own.
-template <bool F16, int D, int RT, int NW>
-__device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, const SeqRows &sr, int row0, int row_end, int begin, int end,
-                                           long long slot)
+// The rows of a wave's tiles in the step's tensors; rows past the last are computed as the last and not stored.
+template <int RT>
+__device__ __forceinline__ void rows_of(const KvAttnArgs &a, int h, const SeqRows &sr, int row0, int last, int (&qrow)[RT], int (&qhead)[RT])
 {
-    constexpr int NS = D / 32, NC = D / 64, DT = D / 16;
-    const int lane = threadIdx.x & 63, wave = wave_id(), col = lane & 15, qt = lane >> 4;
-    const int last = min(row_end, row0 + RT * 16) - 1, limit = sr.limit;
-
-    // rows past the last are computed as the last and not stored
-    u32x4 q[RT][NS];
-    Sight see[RT];
-    int qrow[RT], qhead[RT];
 #pragma unroll
     for (int t = 0; t < RT; t++) {
-        const int r = min(row0 + 16 * t + col, last);
-        const int i = r / a.per_kv;
+        const int r = min(row0 + 16 * t + (int)(threadIdx.x & 15), last), i = r / a.per_kv;
         qrow[t] = sr.q0 + i;
         qhead[t] = h * a.per_kv + (r - i * a.per_kv);
-        see[t] = sight_of(sr.first_p + i, a.window, limit);
-        const uint16_t *x = (const uint16_t *)a.q + (long long)qrow[t] * a.q_stride + (long long)qhead[t] * a.q_head + qt * 16;
-#pragma unroll
-        for (int d = 0; d < NS; d++) q[t][d] = load16(x + 64 * (d >> 1) + 8 * (d & 1));
     }
-    const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
-
-    const int *table = a.b.table + (long long)s * a.b.table_stride;
-    const KvScales *scales = kv8_scales(a.g);
-    constexpr int STRIDE = kAttnStep * (NW == 0 ? 1 : NW);
-    // The records of the next 32 steps, and what their scales come to: lane 2 i + u has block u
-    // of step i, -1 where there is none.  One gather for 32 steps: a page number
-    // that is fetched for the step at hand costs it a trip to memory.
-    long long starts;
-    float ks, lv, iv;
-    const auto find = [&](int t0) {
-        const int at = t0 + (lane >> 1) * STRIDE, blk = (at >> 4) + (lane & 1);
-        starts = -1;
-        KvScales sc = {1.f, 1.f};
-        if (at < end && blk * kKvBlock < limit) {
-            const int pc = page_of_block(a.g, blk), page = table[pc];
-            if ((unsigned)page < (unsigned)a.g.n_pages) {
-                const long long record = ((long long)page * a.g.n_kv_heads + h) * a.g.blocks_per_page + (blk - pc * a.g.blocks_per_page);
-                starts = record * a.g.rec;
-                sc = scales[record];
-            }
-        }
-        ks = sc.k;
-        if (sc.v < kKv8LeastScale) sc.v = kKv8LeastScale;   // memory of zeros
-        lv = __builtin_amdgcn_logf(sc.v);   // of base 2
-        iv = 1.f / sc.v;
-    };
-    const auto lane_of = [](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); };
-    // where there is no record the first one is read, and masked
-    const auto step_at = [&](int i) {
-        Step8 r;
-        r.ok = 0;
+}
+// The rows' queries and what they see, on their way while the first step's tokens are.
+template <bool F16, int D, int RT>
+__device__ __forceinline__ void load_queries(const KvAttnArgs &a, int h, const SeqRows &sr, int row0, int last, u32x4 (&q)[RT][D / 32], Sight (&see)[RT])
+{
+    int qrow[RT], qhead[RT];
+    rows_of<RT>(a, h, sr, row0, last, qrow, qhead);
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            const int l = 2 * i + u;
-            const long long at = (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(starts >> 32), l) << 32 |
-                                             (unsigned)__builtin_amdgcn_readlane((int)starts, l));
-            r.ok |= (at >= 0) << u;
-            r.rec[u] = a.g.pages + (at < 0 ? 0 : at);
-            r.ks[u] = lane_of(ks, l);
-            r.lv[u] = lane_of(lv, l);
-            r.iv[u] = lane_of(iv, l);
-        }
-        return r;
-    };
-    Attn8Tokens<D> x;
-    const auto keys_of = [&](const Step8 &r) {
+    for (int t = 0; t < RT; t++) {
+        see[t] = sight_of(sr.first_p + (qrow[t] - sr.q0), a.window, sr.limit);
+        const uint16_t *x = (const uint16_t *)a.q + (long long)qrow[t] * a.q_stride + (long long)qhead[t] * a.q_head + ((threadIdx.x & 63) >> 4) * 16;
 #pragma unroll
-        for (int u = 0; u < 2; u++)
-#pragma unroll
-            for (int j = 0; j < NC; j++) x.kc[u][j] = ((const u32x4 *)r.rec[u])[64 * j + lane];
-    };
-    const auto values_of = [&](const Step8 &r) {
-#pragma unroll
-        for (int u = 0; u < 2; u++)
-#pragma unroll
-            for (int j = 0; j < NC; j++) x.vc[u][j] = ((const u32x4 *)(r.rec[u] + 16 * D))[64 * j + lane];
-    };
-    // the first step's records are on their way while the queries are made ready
-    int t0 = begin + (NW == 0 ? 0 : wave * kAttnStep), i = 0;
-    Step8 now = {{a.g.pages, a.g.pages}, 0, {1.f, 1.f}, {0.f, 0.f}, {1.f, 1.f}};
-    if (t0 < end) {
-        find(t0);
-        now = step_at(0);
-        keys_of(now);
-        values_of(now);
+        for (int d = 0; d < D / 32; d++) q[t][d] = load16(x + 64 * (d >> 1) + 8 * (d & 1));
     }
-
-    float c[RT], first[RT], base[RT], l[RT];
-    f32x4 o[RT][DT];
+}
+// Queries to operands, nothing seen yet.
+template <bool F16, int D, int RT>
+__device__ __forceinline__ void make_ready(const KvAttnArgs &a, u32x4 (&q)[RT][D / 32], float (&c)[RT], float (&first)[RT], float (&base)[RT],
+                                           float (&l)[RT], f32x4 (&o)[RT][D / 16])
+{
+    constexpr int NS = D / 32, DT = D / 16;
 #pragma unroll
     for (int t = 0; t < RT; t++) {
         float big = 0.f;
@@ -275,29 +235,247 @@ __device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, co
 #pragma unroll
         for (int d = 0; d < DT; d++) o[t][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
+}
+
+// The records of some steps of a sequence's and head's tokens, and what their scales come to: lane 2 i + u has block u of step
+// i of 32, STRIDE tokens apart.  One gather for 32 steps: a page number that is fetched for the step at hand costs it
+// a trip to memory.
+struct Records8 {
+    long long start;           // where there is no record that of the first one, which is read, and masked
+    unsigned long long there;   // bit l: there is one
+    float ks, lv, iv;
+    __device__ __forceinline__ void find(const KvAttnArgs &a, const int *table, int h, int t0, int stride, int end, int limit)
+    {
+        const int lane = threadIdx.x & 63, at = t0 + (lane >> 1) * stride, blk = (at >> 4) + (lane & 1);
+        start = 0;
+        bool is = false;
+        KvScales sc = {1.f, 1.f};
+        if (at < end && blk * kKvBlock < limit) {
+            const int pc = page_of_block(a.g, blk), page = table[pc];
+            is = (unsigned)page < (unsigned)a.g.n_pages;
+            if (is) {
+                const long long record = ((long long)page * a.g.n_kv_heads + h) * a.g.blocks_per_page + (blk - pc * a.g.blocks_per_page);
+                start = record * a.g.rec;
+                sc = kv8_scales(a.g)[record];
+            }
+        }
+        there = __ballot(is);
+        ks = sc.k;
+        if (sc.v < kKv8LeastScale) sc.v = kKv8LeastScale;   // memory of zeros
+        lv = __builtin_amdgcn_logf(sc.v);   // of base 2
+        iv = 1.f / sc.v;
+    }
+    static __device__ __forceinline__ float lane_of(float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); }
+    __device__ __forceinline__ long long start_of(int l) const
+    {
+        return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(start >> 32), l) << 32 |
+                           (unsigned)__builtin_amdgcn_readlane((int)start, l));
+    }
+    __device__ __forceinline__ const uint8_t *record(const KvAttnArgs &a, int l) const { return a.g.pages + start_of(l); }
+    __device__ __forceinline__ Step8 step(int i) const
+    {
+        Step8 r;
+        r.ok = (int)(there >> (2 * i)) & 3;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const int l = 2 * i + u;
+            r.ks[u] = lane_of(ks, l);
+            r.lv[u] = lane_of(lv, l);
+            r.iv[u] = lane_of(iv, l);
+        }
+        return r;
+    }
+};
+
+// Rows row0 .. of one sequence and key head over its tokens [begin, end):
+// into the output (slot < 0) or a slot of the parts.
+// NW waves share the rows and take different tokens, which each makes operands of in registers.
+template <bool F16, int D, int RT, int NW>
+__device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, const SeqRows &sr, int row0, int row_end, int begin, int end,
+                                           long long slot)
+{
+    constexpr int NC = D / 64;
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    const int last = min(row_end, row0 + RT * 16) - 1, limit = sr.limit;
+
+    u32x4 q[RT][D / 32];
+    Sight see[RT];
+    float c[RT], first[RT], base[RT], l[RT];
+    f32x4 o[RT][D / 16];
+    load_queries<F16, D, RT>(a, h, sr, row0, last, q, see);
+    const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
+
+    const int *table = a.b.table + (long long)s * a.b.table_stride;
+    constexpr int STRIDE = kAttnStep * NW;
+    Records8 records;
+    Attn8Tokens<D> x;
+    const auto keys = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const uint8_t *rec = records.record(a, 2 * i + u);
+#pragma unroll
+            for (int j = 0; j < NC; j++) x.kc[u][j] = ((const u32x4 *)rec)[64 * j + lane];
+        }
+    };
+    const auto values = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const uint8_t *rec = records.record(a, 2 * i + u) + 16 * D;
+#pragma unroll
+            for (int j = 0; j < NC; j++) x.vc[u][j] = ((const u32x4 *)rec)[64 * j + lane];
+        }
+    };
+    // the first step's records are on their way while the queries are made ready
+    int t0 = begin + wave * kAttnStep, i = 0;
+    Step8 now[1] = {{0, {1.f, 1.f}, {0.f, 0.f}, {1.f, 1.f}}};
+    if (t0 < end) {
+        records.find(a, table, h, t0, STRIDE, end, limit);
+        now[0] = records.step(0);
+        keys(0);
+        values(0);
+    }
+
+    make_ready<F16, D, RT>(a, q, c, first, base, l, o);
 
     while (t0 < end) {
-        const bool full = now.ok == 3 && t0 >= see1.lo && t0 + kAttnStep - 1 <= see0.hi;
+        const bool full = now[0].ok == 3 && t0 >= see1.lo && t0 + kAttnStep - 1 <= see0.hi;
         if (++i == 32) {
-            find(t0 + STRIDE);
+            records.find(a, table, h, t0 + STRIDE, STRIDE, end, limit);
             i = 0;
         }
-        const Step8 next = step_at(i);   // past the end: records that are none
-        attn8_step<D, RT>(o, base, l, q, first, x, see, full, now, t0, c, [&] { keys_of(next); }, [&] { values_of(next); });
-        now = next;
+        const Step8 next = records.step(i);   // past the end: records that are none
+        const auto value_at = [&](int, int n) { return value_operand(x.vc[0][n >> 2][n & 3], x.vc[1][n >> 2][n & 3]); };
+        f32x4 sc[1][RT][2];
+        attn8_scores<D, RT>(q, first, sc[0], [&](int u, int n) { return key_operand(x.kc[u][n >> 1][2 * (n & 1)], x.kc[u][n >> 1][2 * (n & 1) + 1]); });
+        // the next step's keys and values are fetched where this one has no more use for its own
+        keys(i);
+        attn8_step<D, RT, 1>(sc, see, c, base, l, o, full, now, t0, value_at);
+        values(i);
+        now[0] = next;
         t0 += STRIDE;
     }
 
     // the lanes' own sums together
 #pragma unroll
     for (int t = 0; t < RT; t++) l[t] = quarters_sum(l[t]);
-    end_item<F16, D, RT, NW>(a, row0, last, qrow, qhead, base, l, o, slot);
+    int qrow[RT], qhead[RT];
+    const int r0 = again(row0);
+    rows_of<RT>(a, h, sr, r0, last, qrow, qhead);
+    end_item<F16, D, RT, NW>(a, r0, last, qrow, qhead, base, l, o, slot);
 }
 
+// By rows (many query tokens): a workgroup takes a tile of attn_rows rows, its waves 16 RT of them each, over a part of
+// their tokens.  The waves go over the same tokens: each makes a quarter of a step's operands and leaves
+// them in LDS for all, for the step after the one that is computed.
 template <bool F16, int D, int RT>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn8_rows_kernel(KvAttnArgs a)
 {
-    rows_work<RT>(a, [&](auto... item) { attn8_item<F16, D, RT, 0>(a, item...); });
+    static_assert(kAttnWaves == 4, "quarters");
+    constexpr int WG_ROWS = attn_rows(RT, true), NC = D / 64, KEYS = 4 * NC, ALL = 8 * NC;   // operands of 32 tokens
+    constexpr int S = D == 64 ? 2 : 1;   // heads of 64: 64 tokens a step (2 x 1024 query tokens of 16 heads over 12000: 245 us, 32 tokens 262; of 128 525 and 517)
+    __shared__ u32x4 lds[2][S][ALL][64];
+    const int wg = a.first + (int)blockIdx.x, split = wg % a.splits, item = wg / a.splits;
+    const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
+    const SeqRows sr = seq_rows(a.b, seq_raw(a.b, s));
+    const int row_end = (int)min((long long)sr.n * a.per_kv, (long long)(tile + 1) * WG_ROWS), wg0 = tile * WG_ROWS;
+    if (wg0 >= row_end) return;
+    const int lane = threadIdx.x & 63, wave = wave_id(), limit = sr.limit;
+    // a wave without rows makes operands and computes the tile's last row, which it does not store
+    const int row0 = min(wg0 + wave * RT * 16, row_end - 1), last = min(row_end, row0 + RT * 16) - 1;
+    const bool own = wg0 + wave * RT * 16 < row_end;
+    u32x4 q[RT][D / 32];
+    Sight see[RT];
+    float c[RT], first[RT], base[RT], l[RT];
+    f32x4 o[RT][D / 16];
+    load_queries<F16, D, RT>(a, h, sr, row0, last, q, see);
+    const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
+    const Range t = range_of(sr, wg0 / a.per_kv, (row_end - 1) / a.per_kv, a.window);
+    const long long part = t.from + (long long)split * a.chunk;
+    const int begin = (int)min(part, (long long)t.to), end = split + 1 == a.splits ? t.to : (int)min(part + a.chunk, (long long)t.to);
+
+    const int *table = a.b.table + (long long)s * a.b.table_stride;
+    Records8 records;
+    // this wave's quarter of 32 tokens: keys of block wave / 2, 2 NC dwords a lane; NC dwords of both blocks' values
+    uint32_t kc[S][2 * NC], vc[S][2][NC];
+    const auto fetch = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < S; k++) {
+            const uint8_t *key = records.record(a, 2 * (i + k) + (wave >> 1)) + lane * 16;
+#pragma unroll
+            for (int n = 0; n < NC; n++)
+                __builtin_memcpy(kc[k] + 2 * n, __builtin_assume_aligned(key + (((wave & 1) * NC + n) >> 1) * 1024 + (((wave & 1) * NC + n) & 1) * 8, 8), 8);
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const uint8_t *value = records.record(a, 2 * (i + k) + u) + 16 * D + lane * 16;
+                __builtin_memcpy(vc[k][u], __builtin_assume_aligned(value + (wave * NC >> 2) * 1024 + (wave * NC & 3) * 4, 4 * NC), 4 * NC);
+            }
+        }
+    };
+    const auto put = [&](int buf) {
+#pragma unroll
+        for (int k = 0; k < S; k++) {
+#pragma unroll
+            for (int n = 0; n < NC; n++) lds[buf][k][wave * NC + n][lane] = key_operand(kc[k][2 * n], kc[k][2 * n + 1]);
+#pragma unroll
+            for (int n = 0; n < NC; n++) lds[buf][k][KEYS + wave * NC + n][lane] = value_operand(vc[k][0][n], vc[k][1][n]);
+        }
+    };
+    constexpr int STEP = S * kAttnStep;
+    int i = 0;   // of the tokens fetched last, in the gather
+    Step8 now[S], next[S];
+#pragma unroll
+    for (int k = 0; k < S; k++) now[k] = next[k] = {0, {1.f, 1.f}, {0.f, 0.f}, {1.f, 1.f}};
+    if (begin < end) {
+        records.find(a, table, h, begin, kAttnStep, end, limit);
+#pragma unroll
+        for (int k = 0; k < S; k++) {
+            now[k] = records.step(k);
+            next[k] = records.step(S + k);
+        }
+        fetch(0);
+    }
+    make_ready<F16, D, RT>(a, q, c, first, base, l, o);
+    if (begin < end) {
+        put(0);
+        fetch(i = S);
+        lds_barrier();
+    }
+    int buf = 0;
+    for (int t0 = begin; t0 < end; t0 += STEP) {
+        put(buf ^ 1);   // past the end: of records that are none, not used
+        if ((i += S) == 32) {
+            records.find(a, table, h, t0 + 2 * STEP, kAttnStep, end, limit);
+            i = 0;
+        }
+        Step8 then[S];
+#pragma unroll
+        for (int k = 0; k < S; k++) then[k] = records.step(i + k);
+        fetch(i);
+        if (t0 <= see1.hi && t0 + STEP > see0.lo) {
+            f32x4 sc[S][RT][2];
+            int ok = 3;
+#pragma unroll
+            for (int k = 0; k < S; k++) {
+                attn8_scores<D, RT>(q, first, sc[k], [&](int u, int n) { return lds[buf][k][u * 2 * NC + n][lane]; });
+                ok &= now[k].ok;
+            }
+            attn8_step<D, RT, S>(sc, see, c, base, l, o, ok == 3 && t0 >= see1.lo && t0 + STEP - 1 <= see0.hi, now, t0,
+                                 [&](int k, int n) { return lds[buf][k][KEYS + n][lane]; });
+        }
+#pragma unroll
+        for (int k = 0; k < S; k++) {
+            now[k] = next[k];
+            next[k] = then[k];
+        }
+        buf ^= 1;
+        lds_barrier();
+    }
+#pragma unroll
+    for (int r = 0; r < RT; r++) l[r] = quarters_sum(l[r]);
+    int qrow[RT], qhead[RT];
+    const int r0 = again(row0);
+    rows_of<RT>(a, h, sr, r0, last, qrow, qhead);
+    if (own) end_item<F16, D, RT, 0>(a, r0, last, qrow, qhead, base, l, o, a.splits == 1 ? -1 : (long long)item * a.splits + split);
 }
 
 template <bool F16, int D, int RT, int NW, bool WHOLE>

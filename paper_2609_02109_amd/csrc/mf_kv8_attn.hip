@@ -38,16 +38,22 @@ KvPlan kv8_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window)
         p.slot_rows = wg_rows;
     } else {
         p.row_tiles = 1;
-        const long long longest = heads * 16 < 1024 ? 1024 : heads * 16 < 4096 ? heads * 16 : 4096;
-        p.whole = span <= longest;
+        // Whole heads have neither shares to find nor parts to join, which is 3 us and more, but the longest decides, and
+        // few heads leave most of the card idle.  us, whole and in shares (heads of 128; one length, then all lengths up to it):
+        //   4 x 8 of 1500: 11.7, 11.9 and 11.7, 14.3; of 3000: 17.6, 14.4 and 17.3, 14.7
+        //   8 x 8 of 2000: 14.5, 15.6 and 13.3, 13.0; of 4000: 22.1, 20.3 and 21.5, 19.3
+        //   16 x 8 of 8000: 41.5, 47.7 and 37.1, 34.6; of 16000: 101.7, 100.7 and 91.6, 70.1
+        //   32 x 8 of 8000: 91.5, 100.3 and 55.7, 61.8; of 20000: 221.5, 236.1 and 143.5, 135.8
+        // (heads of 64: 16 x 8 of 8000: 29.8, 31.0 and 29.3, 24.6; of 256: 16 x 8 of 8000: 99.7, 103.4 and 84.5, 62.3)
+        p.whole = span <= (heads < 64 ? 1536 : heads < 128 ? 2048 : 8192);
         if (p.whole) {
+            // few heads: more waves to each (1 x 8 of 1500: 8 waves 11.5, 4 12.4; 128 x 8 of 500: 33.2 and 24.5)
             p.waves = heads < 512 ? 8 : 4;
             p.workgroups = heads;
         } else {
-            // as many as are on the card at once, by the kernels' registers; two units each at least
-            const int per_cu = p.rt == 2 || g.head_dim == 256 ? 2 : g.head_dim == 64 ? 4 : 3;
+            // two workgroups a compute unit, two units each at least (24 x 8 of 10000: 97.8 us, three 98.5, four 107.1)
             const long long units = (span + kAttnUnit - 1) / kAttnUnit, most = (units * heads + 1) / 2;
-            p.workgroups = most < 256 * per_cu ? most : 256 * per_cu;
+            p.workgroups = most < 512 ? most : 512;
             p.slots = 2 * p.workgroups;
         }
         p.slot_rows = (int)rows;
