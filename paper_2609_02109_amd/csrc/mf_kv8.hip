@@ -16,14 +16,6 @@
 namespace mfs {
 namespace {
 
-// The largest magnitude's bits over the wave.
-__device__ __forceinline__ uint32_t wave_top(uint32_t x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
-    return x;
-}
-
 constexpr float kMostValue = 65504.f;
 
 // A block's scale as it was and will be, and what takes codes from one to the other (1: they stay as they are).
@@ -73,7 +65,7 @@ __device__ __forceinline__ uint32_t top_of(const float (&v)[D / 64][16])
     for (int j = 0; j < D / 64; j++)
 #pragma unroll
         for (int e = 0; e < 16; e++) top = max(top, __float_as_uint(v[j][e]) & 0x7fffffffu);
-    return wave_top(top);
+    return over_wave(top, [](uint32_t p, uint32_t q) { return max(p, q); });
 }
 
 template <bool F16, int D>

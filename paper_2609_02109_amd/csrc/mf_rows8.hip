@@ -4,7 +4,10 @@
 //
 // A row belongs to T threads, which hold it in registers as fp32 (8 V values each)
 // between the sum of squares, the largest value and the codes: what comes from
-// memory comes once.
+// memory comes once.  Bound by the bytes from some hundred rows on (8192 rows of
+// 8192, norm with a residual: 85 us for 470 MB, 5.5 TB/s; 4500 of 10240, gate:
+// 37 us for 230 MB, 6.2 TB/s; what they stand for: 34 us for 201 MB), below that by the trip to memory
+// and the waves' meetings (one row of 4096: 2.9 us).
 #include "mf_serve_dev.h"
 
 namespace mfs {
@@ -47,11 +50,10 @@ __device__ __forceinline__ float gated(float g, float u)
 template <int T, class X, class F>
 __device__ __forceinline__ X over_row(X v, X (&lds)[T / 64], const F &f)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = f(v, (X)__shfl_xor(v, d));
+    v = over_wave(v, f);
     if constexpr (T > 64) {
         if ((threadIdx.x & 63) == 0) lds[wave_id()] = v;
-        __syncthreads();
+        lds_barrier();
         v = lds[0];
 #pragma unroll
         for (int w = 1; w < T / 64; w++) v = f(v, lds[w]);
@@ -97,10 +99,10 @@ __device__ __forceinline__ void begin8(const Rows8Args &a, long long row, int k,
     widen8<F16>(h, v);   // what is carried on is what is normed
 }
 template <bool F16>
-__device__ __forceinline__ void weigh8(const Rows8Args &a, int k, float r, float *v)
+__device__ __forceinline__ void weigh8(u32x4 weight, float r, float *v)
 {
     float w[8];
-    widen8<F16>(load8((const uint16_t *)a.weight, k, a.n), w);
+    widen8<F16>(weight, w);
 #pragma unroll
     for (int j = 0; j < 8; j++) v[j] = v[j] * r * w[j];
 }
@@ -115,14 +117,19 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows8_kernel(Rows8Args a)
     for (long long row = (long long)blockIdx.x * PER + (int)threadIdx.x / T; row < a.rows; row += (long long)gridDim.x * PER) {
         const uint16_t *x = (const uint16_t *)a.x + row * a.x_stride, *y = (const uint16_t *)a.y + row * a.y_stride;
         float v[V][8];
-        u32x4 raw[V], with[V];
+        u32x4 raw[V], with[V], weight[V];
 #pragma unroll
         for (int i = 0; i < V; i++) {
             const int k = 8 * (t + i * T);
-            raw[i] = with[i] = (u32x4){0, 0, 0, 0};
+            raw[i] = with[i] = weight[i] = (u32x4){0, 0, 0, 0};
             if (k >= n) continue;
             raw[i] = load8(x, k, n);
             if (OP == kRowsGate || (OP == kRowsNorm && a.y)) with[i] = load8(y, k, n);
+        }
+        if (OP == kRowsNorm) {
+#pragma unroll
+            for (int i = 0; i < V; i++)
+                if (8 * (t + i * T) < n) weight[i] = load8((const uint16_t *)a.weight, 8 * (t + i * T), n);
         }
         float sum = 0.f;
         uint32_t top = 0;
@@ -142,7 +149,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows8_kernel(Rows8Args a)
             const float r = 1.f / sqrtf(sum / (float)n + a.eps);
 #pragma unroll
             for (int i = 0; i < V; i++)
-                if (8 * (t + i * T) < n) weigh8<F16>(a, 8 * (t + i * T), r, v[i]);
+                if (8 * (t + i * T) < n) weigh8<F16>(weight[i], r, v[i]);
             if (!(sum < INFINITY)) top = 0x7fffffffu;
         }
 #pragma unroll
@@ -185,7 +192,7 @@ __global__ __launch_bounds__(1024) void rows8_wide_kernel(Rows8Args a)
         const auto get = [&](int k, float *v) {
             if (OP == kRowsNorm) {
                 widen8<F16>(load8(h, k, n), v);
-                weigh8<F16>(a, k, r, v);
+                weigh8<F16>(load8((const uint16_t *)a.weight, k, n), r, v);
             } else {
                 begin8<F16, OP>(a, row, k, load8(x, k, n), OP == kRowsGate ? load8(y, k, n) : none, v);
             }
@@ -247,15 +254,19 @@ hipError_t go(const Rows8Args &a, hipStream_t s)
     return hipGetLastError();
 }
 
+// As many threads to a row as leave each one or two pieces of eight, whether rows are few or many (us, norm with a residual and
+// gate; T threads of V pieces): 1 x 4096: 512 of one 2.9 and 2.5, 256 of two 3.4 and 2.9; 8192 x 4096: 36.5 and 26.2, 38.3 and 26.5;
+// 8192 x 8192: 512 of two 85 and 61, 256 of four 94 and 62, 1024 of one 86 and 63; 4500 x 10240: 1024 of two 82 and 37,
+// 256 of eight 116 and 47.  Short rows: 8192 x 1024: 64 of two 12.1 and 9.1, 256 of one 13.6 and 11.4; 1 x 1024: 3.0, 2.5.
 template <bool F16, int OP>
 hipError_t pick(const Rows8Args &a, hipStream_t s)
 {
     if (a.n <= 512) return go<F16, OP, 64, 1>(a, s);
     if (a.n <= 1024) return go<F16, OP, 64, 2>(a, s);
     if (a.n <= 2048) return go<F16, OP, 256, 1>(a, s);
-    if (a.n <= 4096) return go<F16, OP, 256, 2>(a, s);
-    if (a.n <= 8192) return go<F16, OP, 256, 4>(a, s);
-    if (a.n <= 16384) return go<F16, OP, 256, 8>(a, s);
+    if (a.n <= 4096) return go<F16, OP, 512, 1>(a, s);
+    if (a.n <= 8192) return go<F16, OP, 512, 2>(a, s);
+    if (a.n <= 16384) return go<F16, OP, 1024, 2>(a, s);
     const long long most = most_workgroups(1024);
     hipLaunchKernelGGL((rows8_wide_kernel<F16, OP>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(1024), 0, s, a);
     return hipGetLastError();

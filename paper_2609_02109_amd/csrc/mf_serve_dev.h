@@ -168,4 +168,24 @@ __device__ __forceinline__ float quarters_sum(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// f over all lanes of a wave, in each of them (f: of 32 bits, in any order).  No trip through LDS, which a __shfl is.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_bits(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+template <class X, class F>
+__device__ __forceinline__ X over_wave(X v, const F &f)
+{
+    static_assert(sizeof(X) == 4, "32 bits");
+    v = f(v, bits<X>(dpp_bits<0xb1>(bits<uint32_t>(v))));    // the neighbour, the other pair of four, the other four of eight, the other eight of sixteen
+    v = f(v, bits<X>(dpp_bits<0x4e>(bits<uint32_t>(v))));
+    v = f(v, bits<X>(dpp_bits<0x141>(bits<uint32_t>(v))));
+    v = f(v, bits<X>(dpp_bits<0x140>(bits<uint32_t>(v))));
+    auto r = __builtin_amdgcn_permlane16_swap(bits<uint32_t>(v), bits<uint32_t>(v), false, false);
+    v = f(bits<X>((uint32_t)r[0]), bits<X>((uint32_t)r[1]));
+    r = __builtin_amdgcn_permlane32_swap(bits<uint32_t>(v), bits<uint32_t>(v), false, false);
+    return f(bits<X>((uint32_t)r[0]), bits<X>((uint32_t)r[1]));
+}
+
 }  // namespace mfs

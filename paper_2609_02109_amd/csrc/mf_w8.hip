@@ -156,8 +156,7 @@ __global__ __launch_bounds__(NW * 64) void w8_few_kernel(W8Args a)
             for (int i = 0; i < MOST; i++)
 #pragma unroll
                 for (int j = 0; j < 4; j++) top = max(top, __float_as_uint(value(i, j)) & 0x7fffffffu);
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+            top = over_wave(top, [](uint32_t p, uint32_t q) { return max(p, q); });
             if (m > 0) lds_barrier();   // the row before has read its own
             if (lane == 0) tops[wave] = top;
             lds_barrier();
