@@ -624,7 +624,7 @@ typedef struct {
     const float *d_x_scales;/* [rows] or NULL */
     const void *d_bias;     /* [N] or NULL */
     void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x */
-    int64_t rows;           /* 0 (nothing is done) .. 2^20 */
+    int64_t rows;           /* 0 (nothing is done) .. 2^20, times N at most 2^37 */
     int64_t x_stride, y_stride;
 } mf_w8_args;
 
@@ -642,12 +642,13 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
  * block finds, in fp32, each step rounded,
  *   x limited to +-65504, need = max |x| over the call's tokens of the block * (float)(1 / 127.), at least 2^-40,
  *   scale = need where the block is not begun, or its scale so far is 2^-40,
- *   else the scale so far where need is not above it, else the scale so far doubled until it reaches need,
+ *   else the scale so far where need is not above it, else the scale so far doubled until it reaches need, at most
+ *   65504 * (float)(1 / 127.),
  *   code = rint(x * (1 / scale)) limited to -127..127.
  * A block is begun where the call's first token in it is not its first.  Codes that a
  * begun block holds become rint(code * (scale so far / scale)) when the scale grows,
  * so a value held is off by less than one step of the scale at hand, over any number
- * of calls.  Where a begun block's scale is none (outside of 2^-40 .. 2^11 and no NaN,
+ * of calls (one and a half where the scale has come to its most).  Where a begun block's scale is none (outside of 2^-40 .. 2^10 and no NaN,
  * as in memory of zeros), scale = need and its earlier tokens become zeros; other memory that
  * was never written must not be begun.  A NaN makes
  * the scale NaN, and with it the block's keys or values, until the block is begun anew.
@@ -668,7 +669,8 @@ mf_status mf_kv8_cache_bytes(const mf_kv8_cache *cache, size_t *bytes);
  * the same batches and arguments.  What a page number that is not the cache's, or a
  * token that is not there, does is the same.  Attention: the weights of the values,
  * times their scales, are rounded to binary16 (down to 2^-34 of a row's largest such
- * product), queries to 2^-25 of a row's largest value where they are below 2^-28 of it.  No
+ * product), queries to 2^-39 of a row's largest value where they are below 2^-28 of it;
+ * scale times that value is to stay below 2^90.  No
  * bit of a row's result depends on blocks of which it sees no token; of a block
  * that it sees a part of, the scales are all its tokens'.  Blocks of zeros in memory are
  * tokens of zeros (to attention, their values are below 2^-32). */

@@ -32,7 +32,8 @@ __device__ __forceinline__ Grown grow(uint32_t top, float old, bool begun)
     g.scale = need;
     if (held && old != kKv8LeastScale) {   // the least scale: zeros so far, or next to it
         const int ob = __float_as_int(old), nb = __float_as_int(need);
-        g.scale = need <= old ? old : __int_as_float(ob + (((nb - ob + 0x7fffff) >> 23) << 23));
+        // doubled no further than the largest value needs, so that none held is larger (in binary16, an infinity)
+        g.scale = need <= old ? old : fminf(__int_as_float(ob + (((nb - ob + 0x7fffff) >> 23) << 23)), kMostValue * (float)(1.0 / 127.0));
     }
     if (bad || (held && old != old)) g.scale = NAN;
     g.keep = !begun || g.scale != g.scale || g.scale == old ? 1.f : held ? old / g.scale : 0.f;
@@ -112,6 +113,25 @@ __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h
 #pragma unroll
             for (int e = 0; e < 2; e++)
                 turn_pair(v[j] + 8 * e, v[j + NC / 2] + 8 * e, cos + 64 * j + 16 * qt + 8 * e, sin + 64 * j + 16 * qt + 8 * e);
+    } else if (D == 64 && a.rot == D && !a.interleaved) {
+        // the halves are in lanes l and l ^ 32: both get both
+        const bool second = lane >= 32;
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+            u32x4 lo, hi;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const auto r = __builtin_amdgcn_permlane32_swap(kraw[0][e][i], kraw[0][e][i], false, false);
+                lo[i] = r[0];
+                hi[i] = r[1];
+            }
+            float x[8], y[8];
+            widen8<F16>(lo, x);
+            widen8<F16>(hi, y);
+            turn_pair(x, y, cos + 16 * (qt & 1) + 8 * e, sin + 16 * (qt & 1) + 8 * e);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[0][8 * e + i] = second ? y[i] : x[i];
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < NC; j++)

@@ -162,6 +162,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows8_kernel(Rows8Args a)
 #pragma unroll
         for (int i = 0; i < V; i++)
             if (8 * (t + i * T) < n) put_codes(out, 8 * (t + i * T), n, r, v[i]);
+        if (T > 64 && row + gridDim.x < a.rows) lds_barrier();   // the next row's largest value goes where this one's is read
     }
 }
 
@@ -211,6 +212,7 @@ __global__ __launch_bounds__(1024) void rows8_wide_kernel(Rows8Args a)
             get(k, v);
             put_codes(a.codes + row * a.codes_stride, k, n, q, v);
         }
+        if (row + gridDim.x < a.rows) lds_barrier();   // as above
     }
 }
 

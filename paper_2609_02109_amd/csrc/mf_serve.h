@@ -185,8 +185,8 @@ hipError_t launch_kv4_attn(const KvAttnArgs &a, const KvPlan &p, bool f16, hipSt
 //           l % 16 of tokens 4 (l / 16) .. + 3
 // After all records two fp32 numbers for each, in the records' order: the scales
 // of its keys and of its values.
-// Scales are 2^-40 up to 65504 / 127, twice that where a begun block's has grown, or NaN.
-constexpr float kKv8LeastScale = 0x1p-40f, kKv8MostScale = 0x1p11f;
+// Scales are 2^-40 up to 65504 / 127, or NaN.
+constexpr float kKv8LeastScale = 0x1p-40f, kKv8MostScale = 0x1p10f;
 hipError_t launch_kv8_append(const KvAppendArgs &a, bool f16, hipStream_t s);
 hipError_t launch_kv8_read(const KvReadArgs &a, int dtype, hipStream_t s);
 KvPlan kv8_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window);

@@ -45,7 +45,8 @@ mf_status check_w8_rows(const mf_w8_args *a)
     const mf_status st = check_w8(&a->w);
     if (st != MF_OK) return st;
     if (a->rows < 0) return MF_EINVAL;
-    return a->rows > (1 << 20) || a->rows * (a->w.n_out / 4 + 1) > INT32_MAX * (int64_t)256 ? MF_EUNSUPPORTED : MF_OK;
+    // blocks of 128 rows and 256 outputs are a grid's first dimension: 2^37 outputs are 2^22 of them, of 512 threads
+    return a->rows > (1 << 20) || a->rows * a->w.n_out > (int64_t)1 << 37 ? MF_EUNSUPPORTED : MF_OK;
 }
 
 size_t w8_records(const mf_w8_desc &d) { return (size_t)((d.n_out + kW8Tile - 1) / kW8Tile) * (size_t)w8_chunks((int)d.n_in) * kW8Record; }
@@ -101,6 +102,10 @@ mf_status mf_norm8(const mf_norm8_args *args, void *stream)
     if (args->d_residual) {
         if (!args->d_sum || !aligned(args->d_residual, 2) || !aligned(args->d_sum, 2)) return MF_EINVAL;
         if (!row_stride(r.rows, args->residual_stride, r.n, false) || !row_stride(r.rows, args->sum_stride, r.n, true)) return MF_EINVAL;
+        // over itself a row has to lie as it does
+        if (r.rows > 1 && ((args->d_sum == r.d_x && args->sum_stride != r.x_stride) ||
+                           (args->d_sum == args->d_residual && args->sum_stride != args->residual_stride)))
+            return MF_EINVAL;
         a.y = args->d_residual;
         a.sum = args->d_sum;
         a.y_stride = args->residual_stride;

@@ -431,6 +431,7 @@ class W8Weight:
             return _on(self.device, stream, (held, bias, out, self.packed), lambda: self.matmul(x, bias, out))
         dt, dev, k, n = self.dtype, self.device, self.n_in, self.n_out
         if isinstance(x, tuple):
+            _require(len(x) == 2, "x: codes and scales are wanted")
             rows = x if type(x) is Rows8 else Rows8(*x)
             x, xs = rows._checked()
             if x.shape[1] != k or x.device != dev:

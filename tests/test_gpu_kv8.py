@@ -27,7 +27,8 @@ pytestmark = pytest.mark.gpu
 
 DT = {"bf16": torch.bfloat16, "f16": torch.float16}
 UNIT = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}
-LEAST, MOST = 2.0 ** -40, 2.0 ** 11
+LEAST, MOST = 2.0 ** -40, 2.0 ** 10
+CAP = torch.tensor(65504.0) * torch.tensor(np.float32(1 / 127.0))
 
 
 @pytest.fixture(scope="module")
@@ -68,7 +69,7 @@ class Held:
             held = (torch.isnan(old) | ((old >= LEAST) & (old < MOST))) if t0 > 16 * b else torch.zeros_like(old, dtype=torch.bool)
             grown = old.clone()
             for _ in range(60):
-                grown = torch.where(grown < need, grown * 2, grown)
+                grown = torch.where(grown < need, (grown * 2).clamp(max=CAP), grown)
             scale = torch.where(held & (old != LEAST), grown, need)
             scale = torch.where(nan | (held & torch.isnan(old)), torch.full_like(scale, math.nan), scale)
             keep = torch.where(held & ~torch.isnan(scale), old / scale, torch.ones_like(scale))   # other codes are 0 here
@@ -214,6 +215,22 @@ def test_scales_that_grow(serve, D):
     x, got = torch.cat(c.k).float().clamp(-65504, 65504), c.cache.read(c.batch(new=c.kv))[0].cpu()
     step = torch.cat([h.scales.repeat_interleave(16, 0)[:n] for h, n in zip(c.hk, c.kv)])[..., None]
     assert ((got - x).abs() < step).all() and ((got - x).abs() > 0.55 * step).any()
+
+
+def test_the_largest_values_stay_numbers(serve):
+    # a block that is near the most a scale can be, and tokens at the type's end after it
+    c = Case(serve, [16, 20], None, heads=2, D=64, page=16, dt="f16", seed=18)
+    c.k[0][:3], c.v[0][:5] = 65280.0, -40000.0
+    c.k[0][9], c.v[0][10, 1] = 65504.0, 65504.0
+    c.k[1][16], c.v[1][17] = -65504.0, float("inf")
+    c.fill(8)
+    c.check_read()
+    k, v = c.cache.read(c.batch(new=c.kv), torch.float16)
+    assert torch.isfinite(k).all() and torch.isfinite(v).all()
+    c.new = [3, 2]
+    q = torch.zeros(5, 4, 64).half()
+    got = check(c, 2, q=q)
+    assert torch.isfinite(got[0]).all()
 
 
 def test_append_of_odd_values(serve):
@@ -447,6 +464,33 @@ def test_a_row_does_not_depend_on_later_blocks(serve, big):
         c.fill(1)
         got = check(c, 2, q=q, window=window)
         assert torch.equal(got[0][:20], want[0][:20]) and torch.equal(got[1][:20], want[1][:20]) and not torch.equal(got[0][20:], want[0][20:])
+
+
+def test_a_cache_past_32_bits(serve):
+    # pages beyond 4 GiB: 40,000 of 131,328 bytes; a few sequences in the last ones
+    c = Case(serve, [40, 100, 2100], [1, 2, 1], heads=8, D=128, page=64, dt="bf16", seed=19)
+    big = serve.KV8Cache(40_000, 64, 8, 128)
+    assert big.pages.numel() > 2 ** 32
+    c.cache, c.n_pages = big, 40_000
+    c.table = (39_999 - c.table).to(torch.int32)
+    c.fill(2)
+    c.check_read()
+    check(c, 2)
+
+
+def test_sequences_that_share_pages(serve):
+    """A prefix that two sequences have in common, in the same pages; the rest is each's own."""
+    c = Case(serve, [70, 90], [1, 1], heads=2, D=128, page=32, dt="bf16", seed=20)
+    c.table[1, :2] = c.table[0, :2]
+    c.k[1][:64], c.v[1][:64] = c.k[0][:64], c.v[0][:64]
+    c.put([64, 0], [64, 0])
+    for held in (c.hk, c.hv):
+        held[1].codes, held[1].scales = held[0].codes.clone(), held[0].scales.clone()
+    c.put([6, 26], [70, 90])
+    c.check_read()
+    for per in (1, 4):
+        check(c, per)
+    check(c, 40, new=[1, 1])
 
 
 def test_attention_with_a_nan(serve):

@@ -38,7 +38,8 @@ def test_rows_refusals(kw, want):
     (None, 0, None, 0, None, 1e-6, mf.MF_EINVAL), (None, 0, None, 0, 3, 1e-6, mf.MF_EINVAL), (None, 0, None, 0, 2, -1.0, mf.MF_EINVAL),
     (None, 0, None, 0, 2, NAN, mf.MF_EINVAL), (None, 0, None, 0, 2, INF, mf.MF_EINVAL), (2, 64, None, 64, 2, 1e-6, mf.MF_EINVAL),
     (3, 64, 2, 64, 2, 1e-6, mf.MF_EINVAL), (2, 64, 3, 64, 2, 1e-6, mf.MF_EINVAL), (2, 63, 2, 64, 2, 1e-6, mf.MF_EINVAL),
-    (2, 64, 2, 63, 2, 1e-6, mf.MF_EINVAL), (2, -1, 2, 64, 2, 1e-6, mf.MF_EINVAL)])
+    (2, 64, 2, 63, 2, 1e-6, mf.MF_EINVAL), (2, -1, 2, 64, 2, 1e-6, mf.MF_EINVAL), (2, 64, 2, 66, 2, 1e-6, mf.MF_EINVAL),
+    (2, 64, 1024, 66, 2, 1e-6, mf.MF_EINVAL)])
 def test_norm_refusals(res, rs, total, ss, weight, eps, want):
     assert mf.lib.mf_norm8(C.byref(serve.Norm8Args(_row(), res, rs, total, ss, weight, eps)), None) == want
 
@@ -82,7 +83,7 @@ def _w8(n=64, k=256, dt=mf.MF_BF16, rows=1, x=1024, scales=4096, y=8192, packed=
     (dict(packed=1025), mf.MF_EINVAL), (dict(x=None), mf.MF_EINVAL), (dict(x=1025, scales=None), mf.MF_EINVAL), (dict(scales=4098), mf.MF_EINVAL),
     (dict(y=None), mf.MF_EINVAL), (dict(y=8193), mf.MF_EINVAL), (dict(bias=3), mf.MF_EINVAL), (dict(rows=2, xs=255), mf.MF_EINVAL),
     (dict(xs=-1), mf.MF_EINVAL), (dict(rows=2, ys=63), mf.MF_EINVAL), (dict(rows=2, ys=2 ** 41), mf.MF_EINVAL), (dict(k=40), mf.MF_EUNSUPPORTED),
-    (dict(rows=0), mf.MF_OK), (dict(rows=0, packed=None), mf.MF_OK)])
+    (dict(rows=2 ** 20, n=2 ** 17 + 1, k=16), mf.MF_EUNSUPPORTED), (dict(rows=0), mf.MF_OK), (dict(rows=0, packed=None), mf.MF_OK)])
 def test_product_refusals(kw, want):
     assert mf.lib.mf_w8_matmul(C.byref(_w8(**kw)), None, 0, None) == want
 
