@@ -563,7 +563,7 @@ typedef struct {
     int64_t n;              /* values of a row, 1 .. 2^17 */
     const void *d_x;        /* [rows][n], row stride x_stride >= n */
     int64_t x_stride;
-    int8_t *d_codes;        /* [rows][n], row stride codes_stride >= n */
+    int8_t *d_codes;        /* [rows][n], row stride codes_stride >= n; not over d_x */
     int64_t codes_stride;
     float *d_scales;        /* [rows] */
 } mf_rows8_args;
@@ -623,7 +623,7 @@ typedef struct {
     const void *d_x;        /* [rows][K], row stride x_stride >= K: codes, or values of dtype where d_x_scales is NULL */
     const float *d_x_scales;/* [rows] or NULL */
     const void *d_bias;     /* [N] or NULL */
-    void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x */
+    void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x (EINVAL) */
     int64_t rows;           /* 0 (nothing is done) .. 2^20, times N at most 2^37 */
     int64_t x_stride, y_stride;
 } mf_w8_args;

@@ -9,6 +9,18 @@ namespace {
 // Row strides of `n` elements each that a call's rows may have.
 bool row_stride(int64_t rows, int64_t stride, int64_t n, bool out) { return strides_fit(rows, stride, 1, 0, n, out) && (rows <= 1 || stride >= n); }
 
+// Whether `rows` rows of x_row bytes from x on, x_step bytes apart, and of y have no byte together; ones that lie between one
+// another at different steps are taken to have.
+bool apart(int64_t rows, const void *x, int64_t x_step, int64_t x_row, const void *y, int64_t y_step, int64_t y_row)
+{
+    typedef __int128 wide;   // a row may begin 2^70 bytes behind the first
+    const wide x0 = (uintptr_t)x, y0 = (uintptr_t)y, x1 = x0 + (wide)(rows - 1) * x_step + x_row, y1 = y0 + (wide)(rows - 1) * y_step + y_row;
+    if (x1 <= y0 || y1 <= x0) return true;
+    if (rows == 1 || x_step != y_step || x_step == 0) return false;
+    const wide in = ((y0 - x0) % x_step + x_step) % x_step;   // of y's rows in the steps from x on
+    return in >= x_row && in + y_row <= x_step;
+}
+
 // What every call over rows has.
 mf_status check_rows8(const mf_rows8_args *r)
 {
@@ -16,7 +28,8 @@ mf_status check_rows8(const mf_rows8_args *r)
     if (r->rows > (1 << 30) || r->n > kRows8Most) return MF_EUNSUPPORTED;
     if (r->rows == 0) return MF_OK;
     if (!r->d_x || !r->d_codes || !r->d_scales || !aligned(r->d_x, 2) || !aligned(r->d_scales, 4)) return MF_EINVAL;
-    return row_stride(r->rows, r->x_stride, r->n, false) && row_stride(r->rows, r->codes_stride, r->n, true) ? MF_OK : MF_EINVAL;
+    if (!row_stride(r->rows, r->x_stride, r->n, false) || !row_stride(r->rows, r->codes_stride, r->n, true)) return MF_EINVAL;
+    return apart(r->rows, r->d_x, 2 * r->x_stride, 2 * r->n, r->d_codes, r->codes_stride, r->n) ? MF_OK : MF_EINVAL;
 }
 
 Rows8Args rows8_of(const mf_rows8_args &r)
@@ -102,10 +115,12 @@ mf_status mf_norm8(const mf_norm8_args *args, void *stream)
     if (args->d_residual) {
         if (!args->d_sum || !aligned(args->d_residual, 2) || !aligned(args->d_sum, 2)) return MF_EINVAL;
         if (!row_stride(r.rows, args->residual_stride, r.n, false) || !row_stride(r.rows, args->sum_stride, r.n, true)) return MF_EINVAL;
-        // over itself a row has to lie as it does
-        if (r.rows > 1 && ((args->d_sum == r.d_x && args->sum_stride != r.x_stride) ||
-                           (args->d_sum == args->d_residual && args->sum_stride != args->residual_stride)))
-            return MF_EINVAL;
+        // over a row itself, which has to lie as it does, or over none
+        const auto itself_or_apart = [&](const void *x, int64_t stride) {
+            if (x == args->d_sum && (r.rows == 1 || stride == args->sum_stride)) return true;
+            return apart(r.rows, x, 2 * stride, 2 * r.n, args->d_sum, 2 * args->sum_stride, 2 * r.n);
+        };
+        if (!itself_or_apart(r.d_x, r.x_stride) || !itself_or_apart(args->d_residual, args->residual_stride)) return MF_EINVAL;
         a.y = args->d_residual;
         a.sum = args->d_sum;
         a.y_stride = args->residual_stride;
@@ -191,6 +206,8 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
         !aligned(args->d_x_scales, 4) || !aligned(args->d_y, 2) || !aligned(args->d_bias, 2))
         return MF_EINVAL;
     if (!row_stride(args->rows, args->x_stride, w.n_in, false) || !row_stride(args->rows, args->y_stride, w.n_out, true)) return MF_EINVAL;
+    const int64_t size = args->d_x_scales ? 1 : 2;
+    if (!apart(args->rows, args->d_x, size * args->x_stride, size * w.n_in, args->d_y, 2 * args->y_stride, 2 * w.n_out)) return MF_EINVAL;
     const size_t need = w8_ws(*args);
     if (need > 0 && (ws_bytes < need || !d_ws)) return MF_ENOMEM;
     if (need > 0 && !aligned(d_ws, 256)) return MF_EINVAL;

@@ -264,6 +264,28 @@ def test_product_strides_and_shapes(serve, m):
     assert torch.equal(W.matmul(serve.quantise_rows(x[0, 1:1 + k].cuda())), W.matmul(x[0, 1:1 + k].cuda()))
 
 
+@pytest.mark.parametrize("m", [1, 6, 40])
+def test_outputs_beside_inputs_and_over_them(serve, m):
+    from paper_2609_02109_amd import mf
+    k = n = 160
+    wc, ws = _weights(n, k, 13)
+    W = serve.W8Weight(wc.cuda(), ws.cuda())
+    x = torch.randn(m, k, generator=_gen(14)).bfloat16().cuda()
+    w = torch.ones(k, dtype=torch.bfloat16, device="cuda")
+    # inputs and outputs as the columns of one buffer
+    both = torch.cat([x, torch.zeros_like(x)], 1)
+    assert torch.equal(W.matmul(both[:, :k], out=both[:, k:]), W.matmul(x)) and torch.equal(both[:, :k], x)
+    rows, h = serve.norm_rows(both[:, :k], w, residual=both[:, k:], out=both[:, k:])
+    want = serve.norm_rows(x, w, residual=W.matmul(x))
+    assert torch.equal(h, want[1]) and torch.equal(rows.codes, want[0].codes) and torch.equal(both[:, :k], x)
+    # over the inputs, or a part of them
+    for call in (lambda: W.matmul(both[:, :k], out=both[:, :k]), lambda: W.matmul(both[:, :k], out=both[:, 8:8 + k]),
+                 lambda: serve.norm_rows(both[:, :k], w, residual=x, out=both[:, 8:8 + k])):
+        with pytest.raises(mf.MfError) as e:
+            call()
+        assert e.value.status == mf.MF_EINVAL
+
+
 @pytest.mark.parametrize("m", [5, 20, 90])
 def test_rows_do_not_mix(serve, m):
     # a row with a NaN or an infinity is NaN, and the others are as without it

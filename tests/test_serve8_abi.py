@@ -88,6 +88,32 @@ def test_product_refusals(kw, want):
     assert mf.lib.mf_w8_matmul(C.byref(_w8(**kw)), None, 0, None) == want
 
 
+# outputs over inputs: rows of 64 values of 2 bytes at x = 1024, a step of 128 bytes (256 where wide)
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("at,want_narrow,want_wide", [
+    (1024 - 128, mf.MF_EINVAL, None), (1024, mf.MF_EINVAL, mf.MF_EINVAL), (1024 + 2, mf.MF_EINVAL, mf.MF_EINVAL), (1024 + 126, mf.MF_EINVAL, mf.MF_EINVAL),
+    (1024 + 130, mf.MF_EINVAL, mf.MF_EINVAL), (1024 + 254, mf.MF_EINVAL, mf.MF_EINVAL)])
+def test_outputs_over_inputs_are_refused(wide, at, want_narrow, want_wide):
+    step, want = (128, want_wide) if wide else (64, want_narrow)
+    if want is None:
+        return   # between the rows, or before them: it would run
+    a = _w8(n=64, k=64, rows=4, x=1024, scales=None, xs=step, y=at, ys=step)
+    assert mf.lib.mf_w8_matmul(C.byref(a), None, 0, None) == want
+    if at != 1024:   # a sum may be over its row itself
+        r = _row(rows=4, xs=step, codes=1 << 20)
+        assert mf.lib.mf_norm8(C.byref(serve.Norm8Args(r, 1 << 16, step, at, step, 2, 1e-6)), None) == want
+        r = _row(rows=4, x=1 << 16, xs=step, codes=1 << 20)
+        assert mf.lib.mf_norm8(C.byref(serve.Norm8Args(r, 1024, step, at, step, 2, 1e-6)), None) == want
+
+
+def test_codes_over_rows_are_refused():
+    for at in (1024, 1025, 1024 + 4 * 128 - 1, 1024 - 255):
+        assert mf.lib.mf_rows8(C.byref(_row(rows=4, codes=at)), None) == mf.MF_EINVAL
+    # at other steps between one another
+    assert mf.lib.mf_rows8(C.byref(_row(rows=4, xs=128, codes=1024 + 128, cs=64)), None) == mf.MF_EINVAL
+    assert mf.lib.mf_rows8(C.byref(_row(rows=2 ** 30, xs=2 ** 40, codes=1 << 50, cs=2 ** 40)), None) == mf.MF_EINVAL
+
+
 def test_product_workspace():
     size = lambda **kw: _bytes(mf.lib.mf_w8_workspace_size, _w8(**kw))
     # rows in 8 bits need none, nor do a few in 16, which the product takes as they are
