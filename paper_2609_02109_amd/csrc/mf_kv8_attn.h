@@ -17,8 +17,8 @@
 // binary16 (11 bits; everything else is fp32).  So the base goes by what a
 // token can add to the result, not by its weight alone: w below 2^14, and what is 2^-34 of a row's
 // largest has bits left, whatever sizes the blocks' values are of.  The sum of p adds w / scale.
-// The largest is looked for only where a weight shows that it is needed: when one
-// reaches 2^14 the base goes to the largest so far (in powers of two) less 10, and the step's
+// The largest is looked for only where the weights show that it is needed: when four
+// together reach 2^14 the base goes to the largest so far less 10 (both as powers of two), and the step's
 // weights are computed again.
 // Values' operands are whole numbers: 1024 + u, a number of binary16's with the bits 0x6400 | u, less 1152.
 #pragma once
@@ -103,13 +103,13 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
     const int qt = (threadIdx.x & 63) >> 4;
     u32x4 w[S][RT];
     float sum[S][RT][2];   // of a block's weights
-    int highest[RT];
-    constexpr int most = (15 + 14) << 10;   // 2^14 in binary16
+    float highest[RT];
+    constexpr float most = 16384.f;
     const auto weigh = [&] {
-        int over = 0;
+        float over = 0.f;
 #pragma unroll
         for (int t = 0; t < RT; t++) {
-            u16x2 high = {0, 0};
+            highest[t] = 0.f;
 #pragma unroll
             for (int k = 0; k < S; k++) {
                 float e[8];
@@ -125,13 +125,12 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
 #pragma unroll
                 for (int i = 0; i < 4; i++) w[k][t][i] = pack2<true>(e[2 * i], e[2 * i + 1]);
 #pragma unroll
-                for (int u = 0; u < 2; u++) sum[k][t][u] = (e[4 * u] + e[4 * u + 1]) + (e[4 * u + 2] + e[4 * u + 3]);   // before they are rounded
-                // none is negative: as whole numbers they are in the same order
-#pragma unroll
-                for (int i = 0; i < 4; i++) high = __builtin_elementwise_max(high, bits<u16x2>(w[k][t][i]));
+                for (int u = 0; u < 2; u++) {
+                    sum[k][t][u] = (e[4 * u] + e[4 * u + 1]) + (e[4 * u + 2] + e[4 * u + 3]);   // before they are rounded
+                    highest[t] = fmaxf(highest[t], sum[k][t][u]);
+                }
             }
-            highest[t] = max(high[0], high[1]);
-            over = max(over, highest[t]);
+            over = fmaxf(over, highest[t]);
         }
         return __any(over >= most);
     };
@@ -139,7 +138,7 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
 #pragma unroll
         for (int t = 0; t < RT; t++) {
             // only the rows that need it, so that no row's result depends on another's
-            const bool hit = quarters_max((float)highest[t]) >= (float)most;
+            const bool hit = quarters_max(highest[t]) >= most;
             float mx = kNoBase;
 #pragma unroll
             for (int k = 0; k < S; k++)
@@ -162,11 +161,7 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
 #pragma unroll
         for (int t = 0; t < RT; t++)
 #pragma unroll
-            for (int u = 0; u < 2; u++) {
-                const float more = fmaf(sum[k][t][u], now[k].iv[u], l[t]);
-                // scales of blocks that the row does not see may be anything, not a number too
-                l[t] = full || sum[k][t][u] != 0.f ? more : l[t];
-            }
+            for (int u = 0; u < 2; u++) l[t] = fmaf(sum[k][t][u], now[k].iv[u], l[t]);
 #pragma unroll
     for (int k = 0; k < S; k++)
 #pragma unroll
@@ -263,7 +258,7 @@ struct Records8 {
         ks = sc.k;
         if (sc.v < kKv8LeastScale) sc.v = kKv8LeastScale;   // memory of zeros
         lv = __builtin_amdgcn_logf(sc.v);   // of base 2
-        iv = 1.f / sc.v;
+        iv = sc.v == sc.v ? 1.f / sc.v : 1.f;   // a number, so that it adds nothing to rows that do not see the block; the others have lv
     }
     static __device__ __forceinline__ float lane_of(float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l)); }
     __device__ __forceinline__ long long start_of(int l) const
@@ -371,15 +366,17 @@ __device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, co
 // By rows (many query tokens): a workgroup takes a tile of attn_rows rows, its waves 16 RT of them each, over a part of
 // their tokens.  The waves go over the same tokens: each makes a quarter of a step's operands and leaves
 // them in LDS for all, for the step after the one that is computed.  Bound by issue: of the SIMDs' cycles vector
-// instructions take 49 % (a weight's factor, power of two, sum, rounding and check) and matrix instructions 32 %, with two
+// instructions take 46 % (a weight's factor, power of two, sum, rounding and check) and matrix instructions 33 %, with two
 // waves a SIMD by registers to put one over the other (2 x 1000 to 1024 query tokens over 8000 to 12000, 32 heads over 8 of
-// 128: 430 us, 810 TFLOP/s).
+// 128: 413 us, 850 TFLOP/s).
 template <bool F16, int D, int RT>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn8_rows_kernel(KvAttnArgs a)
 {
     static_assert(kAttnWaves == 4, "quarters");
     constexpr int WG_ROWS = attn_rows(RT, true), NC = D / 64, KEYS = 4 * NC, ALL = 8 * NC;   // operands of 32 tokens
-    constexpr int S = D == 64 ? 2 : 1;   // heads of 64: 64 tokens a step (2 x 1024 query tokens of 16 heads over 12000: 245 us, 32 tokens 262; of 128 525 and 517)
+    // 64 tokens a step (2 x 1024 query tokens, 16 heads of 64 over 12000: 200 us, 32 a step 214, 128 a step 209; 32 over 8 heads of
+    // 128 over 11000: 395 and 402); of heads of 256, 64 leave room for one workgroup
+    constexpr int S = D < 256 ? 2 : 1;
     __shared__ u32x4 lds[2][S][ALL][64];
     const int wg = a.first + (int)blockIdx.x, split = wg % a.splits, item = wg / a.splits;
     const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
