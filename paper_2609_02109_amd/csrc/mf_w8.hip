@@ -321,7 +321,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN <= 4 ? 1 : 2) void w8_tiles_k
 // of 16 outputs.  The waves of a part share the rows: 128 inputs of them go into LDS (pieces as in w8_tiles_kernel) while the
 // inputs before are computed, so that they come from memory once for 16 TW outputs; rows and weights are DEEP steps
 // ahead in registers (loads return in order: the one that is awaited has to be as old as all the
-// others).  At the end the parts add up through LDS.  blockIdx.y: the block of rows.  77 x 5003 x 4112: 11.1 us, of which 4.4
+// others).  At the end the parts add up through LDS.  blockIdx.y: the block of rows.  77 x 5003 x 4112: 11.3 us, of which 4.4
 // are the bytes.
 template <bool F16, int MT, int KP, int TW, int DEEP>
 __global__ __launch_bounds__(KP * TW * 64) void w8_rows_kernel(W8Args a)
@@ -444,7 +444,10 @@ template <bool F16, int MT, int KP, int TW, int DEEP>
 hipError_t go_rows(const W8Args &a, hipStream_t s)
 {
     const unsigned tiles = (unsigned)((a.n_out + kW8Tile - 1) / kW8Tile);
-    hipLaunchKernelGGL((w8_rows_kernel<F16, MT, KP, TW, DEEP>), dim3((tiles + TW - 1) / TW, (a.rows + MT * 16 - 1) / (MT * 16)), dim3(KP * TW * 64), 0, s, a);
+    const unsigned nb = (tiles + TW - 1) / TW, mb = (a.rows + MT * 16 - 1) / (MT * 16);
+    // workgroups go to the eight L2 caches in turn: with a multiple of 8 in a row all blocks of rows of the same outputs to the
+    // same one (77 x 5000 x 4096: 10.2 us, else 11.8; 130 x 4100 x 4096: 9.9 and 13.4); what is past the outputs stores nothing
+    hipLaunchKernelGGL((w8_rows_kernel<F16, MT, KP, TW, DEEP>), dim3(mb == 1 ? nb : (nb + 7) / 8 * 8, mb), dim3(KP * TW * 64), 0, s, a);
     return hipGetLastError();
 }
 
@@ -483,7 +486,7 @@ hipError_t launch_w8_pack(const W8PackArgs &a, hipStream_t s)
 // * past that blocks of rows and outputs: what a block takes grows less than its size, but 256 are on the card at
 //   once.  So the form with the least of rounds of 256 blocks times a block's time (us, of 4096 inputs: 32 x 32
 //   7.7, 64 x 32 9.4, 64 x 64 12, 128 x 64 16.5, 128 x 256 35, 256 x 256 56): 64 x 4096 x 4096: 7.7, by 64 x 32 9.4; 77 x
-//   5003 x 4112: 12.1 by 64 x 64, by 64 x 32 15.4; 512 x 4096 x 4096: 17.2 by 128 x 64, by 64 x 64 18.9; 4096 x 8192 x 8192: 230 by
+//   5003 x 4112: 11.3 by 64 x 64, by 64 x 32 15.4; 512 x 4096 x 4096: 17.2 by 128 x 64, by 64 x 64 18.9; 4096 x 8192 x 8192: 230 by
 //   256 x 256, by 128 x 256 269.
 W8Form w8_form(int rows, int n_out)
 {
