@@ -7,7 +7,7 @@
 // are turned through 16 D bytes of LDS, [dim][token].  One wave owns a record, so
 // nothing is written twice and no atomics are needed.
 //
-// Bound by the bytes where rows are many (4 prompts of 8192 tokens, 32 heads of queries over 8 of 128: 167 us for 742 MB, 4.4
+// Bound by the bytes where rows are many (4 prompts of 8192 tokens, 32 heads of queries over 8 of 128: 146 us for 742 MB, 5.1
 // TB/s; read back 34 us), else by trips to memory, one after another: page number, rows, scale, codes (8 rows: 5.6 us,
 // read back 4.3).
 //

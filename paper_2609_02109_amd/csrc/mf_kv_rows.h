@@ -76,19 +76,19 @@ __device__ __forceinline__ void turn_pair(float *a, float *b, const float *cos, 
 
 // The queries of 16 tokens, heads h0 .. h1: a thread takes 8 dims (with their
 // partners, so that the result may go over its source).  Many tokens: eight of them
-// side by side, the angles kept over the heads; few: eight heads side by side.
+// side by side, the angles kept over the heads; few: eight heads side by side, and as many tokens as there are threads left.
 template <bool F16>
 __device__ __forceinline__ void turn_queries(const KvAppendArgs &a, const Span &p, int blk, int h0, int h1, int D, bool few)
 {
     const int half = a.rot >> 1, base = p.lo + blk * 16;
     const int units = a.interleaved ? D / 8 : (D - half) / 8;   // a unit below rot / 2 takes its partner along
-    // threads side by side over a head: as many as have a unit (append of 13 x 300 rows of 20 + 2 x 4 heads of 64: eight of them 12.7 us, four 9.8)
+    // threads side by side over a head: as many as have a unit (append of 13 x 300 rows of 20 + 2 x 4 heads of 64: eight of them 13.4 us, four 11.0)
     const int side = units <= 4 ? 4 : 8, groups = 64 / side;
     const int u0 = threadIdx.x & (side - 1), b0 = threadIdx.x / side;
     for (int u = u0; u < units; u += side) {
         const int d = u * 8, d0 = a.interleaved || d < half ? d : d + half, d1 = !a.interleaved && d < half ? d + half : -1;
         const bool turned = d0 < a.rot;
-        for (int t = few ? 0 : b0; t < 16; t += few ? 1 : groups) {
+        for (int t = few ? b0 >> 3 : b0; t < 16; t += few ? groups >> 3 : groups) {
             const int pos = base + t;
             if (pos >= p.hi) break;
             const long long row = pos + p.shift;
@@ -104,12 +104,15 @@ __device__ __forceinline__ void turn_queries(const KvAppendArgs &a, const Span &
                     sin[j] = a.sin[at + e];
                 }
             }
-#pragma unroll 4
-            for (int h = h0 + (few ? b0 : 0); h < h1; h += few ? groups : 1) {
+            const auto load = [&](u32x4 (&raw)[2], int h) {
+                raw[0] = load16(x + h * a.q_head + d0);
+                if (d1 >= 0) raw[1] = load16(x + h * a.q_head + d1);
+            };
+            const auto turn = [&](const u32x4 (&raw)[2], int h) {
                 float v[2][8];
-                widen8<F16>(load16(x + h * a.q_head + d0), v[0]);
+                widen8<F16>(raw[0], v[0]);
                 if (d1 >= 0) {
-                    widen8<F16>(load16(x + h * a.q_head + d1), v[1]);
+                    widen8<F16>(raw[1], v[1]);
                     turn_pair(v[0], v[1], cos, sin);
                 } else if (turned) {
 #pragma unroll
@@ -127,6 +130,24 @@ __device__ __forceinline__ void turn_queries(const KvAppendArgs &a, const Span &
                     for (int j = 0; j < 4; j++) o[j] = pack2<F16>(v[w][2 * j], v[w][2 * j + 1]);
                     __builtin_memcpy(__builtin_assume_aligned(y + h * a.qo_head + (w ? d1 : d0), 2), &o, 16);
                 }
+            };
+            if (few) {
+                for (int h = h0 + (b0 & 7); h < h1; h += 8) {
+                    u32x4 raw[2];
+                    load(raw, h);
+                    turn(raw, h);
+                }
+                continue;
+            }
+            // the result may be over its source, so that no load goes ahead of a store by itself: four heads are fetched, then turned
+            // (4 x 8192 rows of 32 heads of 128 beside 8: 146 us, one by one 167; 2 x 1024 of 16 heads of 256: 25 and 45)
+            for (int h = h0; h < h1; h += 4) {
+                u32x4 raw[4][2];
+#pragma unroll
+                for (int i = 0; i < 4; i++) load(raw[i], min(h + i, h1 - 1));
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    if (h + i < h1) turn(raw[i], h + i);
             }
         }
     }
