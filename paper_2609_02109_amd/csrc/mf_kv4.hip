@@ -155,7 +155,7 @@ __device__ __forceinline__ void append_block(const KvAppendArgs &a, int s, int h
 // Work item: (sequence, 16 positions, head), the numbers past the heads standing for
 // slices of the queries' heads: few tokens or many, there is a wave for each 16 of a head.
 // Bound by the bytes of rows and queries from some thousand rows on (32768 rows of 32 + 2 x
-// 8 heads of 128: 178 us for 747 MB, 4.2 TB/s, a copy 5.2), below that by one trip to
+// 8 heads of 128: 142 us for 747 MB, 5.3 TB/s, a copy 5.2), below that by one trip to
 // memory after another (a row each of 8 requests: 5.8 us).
 template <bool F16, int D, int G>
 __global__ __launch_bounds__(64) void append_kernel(KvAppendArgs a, int blocks, int slices, int few)
