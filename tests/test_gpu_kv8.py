@@ -178,6 +178,33 @@ def test_append_turns_keys_and_queries(serve, D, rot, inter):
     assert torch.equal(qd, qr)
 
 
+@pytest.mark.parametrize("per", [1, 5, 9, 20, 33])   # heads of queries to a head of keys
+@pytest.mark.parametrize("new,D,rot,inter", [([2, 7, 1], 64, 64, False), ([2, 7, 0], 64, 32, True), ([3, 1, 5], 128, 96, False), ([3, 1, 5], 256, 256, True),
+                                             ([8, 1, 0], 64, 64, False), ([40, 17, 3], 64, 16, True), ([40, 17, 3], 128, 128, False), ([9, 33, 16], 256, 64, False)])
+def test_append_turns_any_number_of_queries(serve, new, D, rot, inter, per):
+    c = Case(serve, [70, 50, 33], new, heads=1, D=D, seed=per)
+    rows = sum(new)
+    angles = serve.rope_table(80, rot)
+    q = torch.randn(rows, per, D, generator=c.gen).bfloat16()
+    k, v = c.rows(c.k, c.new, c.kv).cuda(), c.rows(c.v, c.new, c.kv).cuda()
+    at = torch.cat([torch.arange(a - n, a) for a, n in zip(c.kv, c.new)])
+    want = turned(q.double(), *(t.cpu().double()[at] for t in angles), inter)
+    partner = turned(q.double().abs(), torch.ones(rows, rot // 2), -torch.ones(rows, rot // 2), inter).abs() + q.double().abs()
+    for cache in (c.cache, serve.KV4Cache(c.n_pages, c.page, 1, D, group=64)):
+        cache.pages.zero_()
+        start = torch.tensor([0, *np.cumsum(new)], dtype=torch.int32).cuda()
+        b = cache.batch(start, torch.tensor(c.kv, dtype=torch.int32).cuda(), c.table.cuda(), rows=rows, max_new=max(new), max_kv=70)
+        # rows inside wider ones, whose other values stay as they are
+        wide = torch.full((rows + 1, per * D + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+        to = wide[:rows, :per * D].view(rows, per, D)
+        cache.append(b, k, v, cos=angles[0], sin=angles[1], q=q.cuda(), q_out=to, interleaved=inter)
+        assert ((to.cpu().double() - want).abs() <= UNIT["bf16"] * want.abs() + 3 * 2.0 ** -24 * partner).all()
+        assert (wide[rows] == 7).all() and (wide[:, per * D:] == 7).all()
+        over = q.cuda()
+        cache.append(b, k, v, cos=angles[0], sin=angles[1], q=over, q_out=over, interleaved=inter)
+        assert torch.equal(over, to)
+
+
 def test_append_strides(serve):
     # k and v as slices of one projection with an odd row length, then [heads, rows, D]
     for turn in (False, True):
@@ -386,6 +413,15 @@ def test_attention_rows_split_over_tokens(serve):
     c = Case(serve, [5000, 120], [40, 40], heads=1, D=128, page=64, dt="f16", seed=7)
     c.fill(1)
     check(c, 2)
+
+
+@pytest.mark.parametrize("kv,window", [([1057, 33], 0), ([1570, 1100], 0), ([3000, 40], 1100)])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_rows_in_parts_of_odd_lengths(serve, D, kv, window):
+    # parts of 17 and 25 times 32 tokens: a step of 64 goes past the end of one
+    c = Case(serve, kv, [33, 21], heads=2, D=D, page=32, dt="bf16", seed=sum(kv))
+    c.fill(1)
+    check(c, 2, window=window)
 
 
 def test_attention_many_sequences(serve):
