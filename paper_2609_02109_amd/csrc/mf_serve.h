@@ -250,7 +250,7 @@ enum W8Form {
 };
 // How the work is laid over the card, and whether rows in 16 bits are put into 8 in the product's own kernel: functions of
 // the sizes alone.
-W8Form w8_form(int rows, int n_out);
+W8Form w8_form(int rows, int n_out, int n_in);
 bool w8_takes_16(int rows, int n_in);
 hipError_t launch_w8(const W8Args &a, bool f16, hipStream_t s);
 

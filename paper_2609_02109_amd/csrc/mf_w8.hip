@@ -53,6 +53,12 @@ struct Ends {
         bias[0] = bias[1] = 0;
         if (m >= a.rows || n >= a.n_out) return;
         if (a.x_scales) xs = a.x_scales[m];   // else the kernel knows
+        fetch(a, n);
+    }
+    __device__ __forceinline__ void fetch(const W8Args &a, int n)
+    {
+        bias[0] = bias[1] = 0;
+        if (n >= a.n_out) return;
         ws = *(const f32x4 *)(a.w_scales + n);   // whole tiles of scales
         if (!a.bias) return;
         const uint16_t *b = (const uint16_t *)a.bias + n;
@@ -62,17 +68,21 @@ struct Ends {
             for (int r = 0; r < 3; r++)   // with indexes that are known: else the array is in memory
                 if (n + r < a.n_out) bias[r >> 1] |= (uint32_t)b[r] << (16 * (r & 1));
     }
-    __device__ __forceinline__ void store(const W8Args &a, int m, int n, i32x4 acc) const
+    __device__ __forceinline__ u32x2 outputs(const W8Args &a, i32x4 acc) const
     {
-        if (m >= a.rows || n >= a.n_out) return;
         float v[4];
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             v[r] = (float)acc[r] * xs * ws[r];
             if (a.bias) v[r] += to_float<F16>((uint16_t)(bias[r >> 1] >> (16 * (r & 1))));
         }
+        return (u32x2){pack2<F16>(v[0], v[1]), pack2<F16>(v[2], v[3])};
+    }
+    __device__ __forceinline__ void store(const W8Args &a, int m, int n, i32x4 acc) const
+    {
+        if (m >= a.rows || n >= a.n_out) return;
         uint16_t *y = (uint16_t *)a.y + (long long)m * a.y_stride + n;
-        const u32x2 o = {pack2<F16>(v[0], v[1]), pack2<F16>(v[2], v[3])};
+        const u32x2 o = outputs(a, acc);
         if (n + 4 <= a.n_out) __builtin_memcpy(__builtin_assume_aligned(y, 2), &o, 8);
         else
 #pragma unroll
@@ -80,13 +90,6 @@ struct Ends {
                 if (n + r < a.n_out) y[r] = (uint16_t)(o[r >> 1] >> (16 * (r & 1)));
     }
 };
-template <bool F16>
-__device__ __forceinline__ void store4(const W8Args &a, int m, int n, i32x4 acc)
-{
-    Ends<F16> e;
-    e.fetch(a, m, n);
-    e.store(a, m, n, acc);
-}
 
 // Few rows (up to 16; bound by the weights' bytes, and below some 32 MB of them by two trips to memory and the sum through
 // LDS).  A workgroup takes NT tiles of 16 outputs; its NW waves take every NW-th D chunks of 64 inputs, each chunk's place in
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(NW * 64) void w8_few_kernel(W8Args a)
 // a step, in three buffers: a step reads one, the next one is whole, and the one after is being written, so that a wave's
 // operands are read ahead over the barrier between steps.  The weights come as operands from memory, 64
 // inputs fetched where those before them in the registers have been used.  Bound by the matrix instructions: 4096 x 8192 x
-// 8192 in 226 to 260 us, 2.4 to 2.1 POP/s (a library's product of 8192^3: 2.1), which are busy 55 % of the cycles, vector
+// 8192 in 217 us, 2.5 POP/s (a library's product of 8192^3: 2.1), which are busy 55 % of the cycles, vector
 // instructions 23 %; a compute unit holds one workgroup (96 KB of LDS), which waits at a barrier a step.
 template <bool F16, int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, WM * WN <= 4 ? 1 : 2) void w8_tiles_kernel(W8Args a)
@@ -308,12 +311,37 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN <= 4 ? 1 : 2) void w8_tiles_k
         next = after;
         after = done;
     }
+    // no load goes ahead of a store by itself: all scales first (4096 x 4096 x 1024: 26.8 us, each with its store 32.4)
+    Ends<F16> ends[NT];
+    float xs[MT];
+#pragma unroll
+    for (int t = 0; t < NT; t++) ends[t].fetch(a, (tile0 + t) * kW8Tile + qt * 4);
+#pragma unroll
+    for (int m = 0; m < MT; m++) xs[m] = a.x_scales[min(m0 + mw + 16 * m + col, a.rows - 1)];
 #pragma unroll
     for (int m = 0; m < MT; m++)
 #pragma unroll
-        for (int t = 0; t < NT; t++) {
-            const int row = m0 + mw + 16 * m + col, n = (tile0 + t) * kW8Tile + qt * 4;
-            store4<F16>(a, row, n, acc[m][t]);
+        for (int t = 0; t < NT; t += 2) {
+            // of two tiles' outputs 4 qt .. + 3 of a row to outputs 8 qt .. + 7, so that lanes side by side have 64 bytes of it
+            // (the same: 23.2 us, with 32 bytes 26.8)
+            ends[t].xs = ends[t + 1].xs = xs[m];
+            const u32x2 p = ends[t].outputs(a, acc[m][t]), q = ends[t + 1].outputs(a, acc[m][t + 1]);
+            u32x4 o;
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const auto far = __builtin_amdgcn_permlane32_swap(p[i], q[i], false, false);
+                const auto near = __builtin_amdgcn_permlane16_swap(far[0], far[1], false, false);
+                o[i] = near[0];
+                o[2 + i] = near[1];
+            }
+            const int row = m0 + mw + 16 * m + col, n = (tile0 + t) * kW8Tile + qt * 8;
+            if (row >= a.rows || n >= a.n_out) continue;
+            uint16_t *y = (uint16_t *)a.y + (long long)row * a.y_stride + n;
+            if (n + 8 <= a.n_out) __builtin_memcpy(__builtin_assume_aligned(y, 2), &o, 16);
+            else
+#pragma unroll
+                for (int j = 0; j < 7; j++)
+                    if (n + j < a.n_out) y[j] = (uint16_t)(o[j >> 1] >> (16 * (j & 1)));
         }
 }
 
@@ -454,7 +482,7 @@ hipError_t go_rows(const W8Args &a, hipStream_t s)
 template <bool F16>
 hipError_t pick(const W8Args &a, hipStream_t s)
 {
-    switch (w8_form(a.rows, a.n_out)) {
+    switch (w8_form(a.rows, a.n_out, a.n_in)) {
         case kW8Few16: return go_few<F16, 1, 16, 2>(a, s);
         case kW8Few8x2: return go_few<F16, 2, 8, 2>(a, s);
         case kW8Rows32: return go_rows<F16, 2, 2, 2, 4>(a, s);
@@ -483,12 +511,13 @@ hipError_t launch_w8_pack(const W8PackArgs &a, hipStream_t s)
 //   that the rows are read half as often (16 x 8192 x 8192: 13.3, one 16.2; 16 x 28672 x 4096: 24.2, one 28.5).
 // * up to 32 the rows go through LDS, for two tiles (32 x 4096 x 4096: 7.1, the form for 16 rows with two of them 7.8; 32 x 8192 x
 //   8192: 15.2 and 23), or four of many outputs (32 x 28672 x 4096: 25.8, two 28.7).
-// * past that blocks of rows and outputs: what a block takes grows less than its size, but 256 are on the card at
-//   once.  So the form with the least of rounds of 256 blocks times a block's time (us, of 4096 inputs: 32 x 32
-//   7.7, 64 x 32 9.4, 64 x 64 12, 128 x 64 16.5, 128 x 256 35, 256 x 256 56): 64 x 4096 x 4096: 7.7, by 64 x 32 9.4; 77 x
-//   5003 x 4112: 11.3 by 64 x 64, by 64 x 32 15.4; 512 x 4096 x 4096: 17.2 by 128 x 64, by 64 x 64 18.9; 4096 x 8192 x 8192: 230 by
-//   256 x 256, by 128 x 256 269.
-W8Form w8_form(int rows, int n_out)
+// * past that blocks of rows and outputs, by what each form would take: a + b k + (c + d k) r us, k its inputs over 4096, r its
+//   blocks over the 256 compute units (tiles, of which a unit holds one: rounded up).  Fitted to 75 sizes of 33 to 4096 rows, 260
+//   to 29000 outputs and 400 to 14000 inputs, timed with every form: within 10 to 15 % of them, and the form that it takes is
+//   2.4 % behind the best at the mean and 23 % at most.  Blocks of 32 x 32, 64 x 32, 64 x 64, 128 x 64, 128 x 256, 256 x 256:
+//   64 x 4096 x 4096: 6.7, 8.5, 9.5, 14, 27, 45; 512 x 4096 x 4096: 32, 27, 18, 18, 29, 46; 1032 x 14180 x 1600: 128, 108, 60, 67, 38, 54;
+//   4096 x 8192 x 8192: 1350, 750, 490, 410, 260, 217.
+W8Form w8_form(int rows, int n_out, int n_in)
 {
     const long long tiles = (n_out + kW8Tile - 1) / kW8Tile;
     if (rows <= 16) return tiles <= 256 ? kW8Few16 : kW8Few8x2;
@@ -496,14 +525,17 @@ W8Form w8_form(int rows, int n_out)
     const struct {
         W8Form form;
         int rows, outputs;
-        float us;
-    } forms[] = {{kW8Block32, 32, 32, 7.7f},      {kW8Block64, 64, 32, 9.4f},    {kW8Block64x4, 64, 64, 12.f},
-                 {kW8Block128x4, 128, 64, 16.5f}, {kW8Tiles128, 128, 256, 35.f}, {kW8Tiles256, 256, 256, 56.f}};
+        float a, b, c, d;
+    } forms[] = {{kW8Block32, 32, 32, 2.9f, 1.3f, 0.6f, 3.7f},    {kW8Block64, 64, 32, 3.3f, 2.9f, 1.3f, 5.3f},
+                 {kW8Block64x4, 64, 64, 3.3f, 4.5f, 1.3f, 6.6f},  {kW8Block128x4, 128, 64, 3.7f, 8.5f, 4.1f, 8.2f},
+                 {kW8Tiles128, 128, 256, 0.f, 0.f, 6.3f, 25.f},   {kW8Tiles256, 256, 256, 0.f, 0.f, 9.4f, 40.f}};
     W8Form best = kW8Block32;
     float least = INFINITY;
+    const float k = (float)n_in / 4096.f;
     for (const auto &f : forms) {
         const long long blocks = ((rows + f.rows - 1ll) / f.rows) * ((n_out + f.outputs - 1ll) / f.outputs);
-        const float us = (float)((blocks + 255) / 256) * f.us;
+        const bool tiles = f.form == kW8Tiles128 || f.form == kW8Tiles256;
+        const float r = tiles ? (float)((blocks + 255) / 256) : (float)blocks / 256.f, us = f.a + f.b * k + (f.c + f.d * k) * r;
         if (us < least) {
             least = us;
             best = f.form;
