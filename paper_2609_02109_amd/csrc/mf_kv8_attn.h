@@ -374,9 +374,9 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn8_rows_kernel(KvAttnAr
 {
     static_assert(kAttnWaves == 4, "quarters");
     constexpr int WG_ROWS = attn_rows(RT, true), NC = D / 64, KEYS = 4 * NC, ALL = 8 * NC;   // operands of 32 tokens
-    // 64 tokens a step (2 x 1024 query tokens, 16 heads of 64 over 12000: 200 us, 32 a step 214, 128 a step 209; 32 over 8 heads of
-    // 128 over 11000: 395 and 402); of heads of 256, 64 leave room for one workgroup
-    constexpr int S = D < 256 ? 2 : 1;
+    // 64 tokens a step for heads of 64 (2 x 1024 query tokens, 16 heads over 12000: 194 us, 32 a step 200, 128 a step 248) and two tiles
+    // a wave (32 over 8 heads of 128 over 11000: 395 and 403), 32 else (one tile: 1 x 1000 over 1000: 33.1, 64 a step 34.7)
+    constexpr int S = D == 64 || RT == 2 ? 2 : 1;
     __shared__ u32x4 lds[2][S][ALL][64];
     const int wg = a.first + (int)blockIdx.x, split = wg % a.splits, item = wg / a.splits;
     const int tile = item % a.row_tiles, sh = item / a.row_tiles, h = sh % a.g.n_kv_heads, s = sh / a.g.n_kv_heads;
@@ -495,7 +495,11 @@ hipError_t pick_attn8(const KvAttnArgs &a, const KvPlan &p, hipStream_t s)
 {
     const auto go = [&](void (*kernel)(KvAttnArgs), int waves) { return each_launch(kernel, a, p.workgroups, waves * 64, s); };
     constexpr int TWO = D < 256 ? 2 : 1;
-    if (p.rows_by_wave) return go(attn8_rows_kernel<F16, D, TWO>, kAttnWaves);
+    if (p.rows_by_wave) {
+        if constexpr (D == 128)
+            if (p.rt == 2) return go(attn8_rows_kernel<F16, D, 2>, kAttnWaves);
+        return go(attn8_rows_kernel<F16, D, 1>, kAttnWaves);
+    }
     if (p.rt == 2) {
         if (!p.whole) return go(attn8_tokens_kernel<F16, D, TWO, 4, false>, 4);
         return p.waves == 8 ? go(attn8_tokens_kernel<F16, D, TWO, 8, true>, 8) : go(attn8_tokens_kernel<F16, D, TWO, 4, true>, 4);

@@ -8,6 +8,28 @@ hipError_t launch_attn8_d64(const KvAttnArgs &a, const KvPlan &p, bool f16, hipS
 hipError_t launch_attn8_d128(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
 hipError_t launch_attn8_d256(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
 
+// By rows: tiles of 64 rt rows, each over `splits` parts of its tokens.  As many parts as leave all workgroups on the card at
+// once (two a compute unit; of heads of 64 four), of about eight steps of 32 tokens at the least.  us: about what that takes.
+struct RowsPlan {
+    long long row_tiles, items, splits;
+    float us;
+};
+static RowsPlan rows_plan(int rt, long long rows, long long heads, int head_dim, long long span, long long max_new)
+{
+    const int wg_rows = attn_rows(rt, true);
+    RowsPlan p;
+    p.row_tiles = (rows + wg_rows - 1) / wg_rows;
+    p.items = p.row_tiles * heads;
+    const long long steps = (span + kAttnStep - 1) / kAttnStep, mean = steps - max_new / 2 / kAttnStep, room = head_dim == 64 ? 1024 : 512;
+    long long splits = p.items > 0 ? room / p.items : 1;
+    if (splits > (mean + 4) / 8) splits = (mean + 4) / 8;
+    p.splits = splits > 1 ? splits : 1;
+    const float rounds = (float)((p.items * p.splits + room - 1) / room), parts = (float)(p.items * p.splits * wg_rows) * (float)(head_dim + 2) * 4.f;
+    // a beginning, the steps, and where there are parts their writing, reading and a launch
+    p.us = rounds * (9.f + (float)steps / (float)p.splits * (rt == 1 ? 0.84f : 1.15f)) + (p.splits > 1 ? 4.f + 2.f * parts / 4e6f : 0.f);
+    return p;
+}
+
 KvPlan kv8_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window)
 {
     KvPlan p;
@@ -23,19 +45,26 @@ KvPlan kv8_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window)
     p.whole = false;
     p.waves = kAttnWaves;
     if (p.rows_by_wave) {
-        const int wg_rows = attn_rows(p.rt, true);
-        p.row_tiles = (rows + wg_rows - 1) / wg_rows;
-        const long long items = p.row_tiles * heads, steps = (span + kAttnStep - 1) / kAttnStep;
-        long long splits = items > 0 ? (512 + items - 1) / items : 1;
-        if (splits > (steps + 31) / 32) splits = (steps + 31) / 32;
-        if (splits > 1) {
-            const long long per = (steps + splits - 1) / splits;
+        // Of heads of 128 a wave takes one tile of 16 rows or two, which share operands (us, one and two, in the best number of parts; 32
+        // over 8 heads): 1 x 16 query tokens over 4000: 18, 21; 1 x 300 over 3000: 46, 48; 4 x 64 over 3000: 41, 43; 1 x 1000 over 1000: 37, 47;
+        // 4 x 100 over 3000: 61, 57; 1 x 512 over 8000: 127, 112; 2 x 1500 over 3000: 236, 217; 2 x 1024 over 11000: 590, 440.  Of heads of 64
+        // one (16 heads, 2 x 500 over 2000: 34, 37; 2 x 1024 over 12000: 190, 197), of heads of 256 two have no room.
+        RowsPlan r = rows_plan(1, rows, heads, g.head_dim, span, b.max_new);
+        p.rt = 1;
+        if (g.head_dim == 128) {
+            const RowsPlan two = rows_plan(2, rows, heads, g.head_dim, span, b.max_new);
+            if (two.us < r.us) r = two, p.rt = 2;
+        }
+        const long long steps = (span + kAttnStep - 1) / kAttnStep;
+        p.row_tiles = r.row_tiles;
+        if (r.splits > 1) {
+            const long long per = (steps + r.splits - 1) / r.splits;
             p.chunk = (int)(per * kAttnStep);
             p.splits = (int)((steps + per - 1) / per);
         }
-        p.workgroups = items * p.splits;
+        p.workgroups = r.items * p.splits;
         p.slots = p.splits > 1 ? p.workgroups : 0;
-        p.slot_rows = wg_rows;
+        p.slot_rows = attn_rows(p.rt, true);
     } else {
         p.row_tiles = 1;
         // Whole heads have neither shares to find nor parts to join, which is 3 us and more, but the longest decides, and

@@ -418,7 +418,7 @@ def test_attention_rows_split_over_tokens(serve):
 @pytest.mark.parametrize("kv,window", [([1057, 33], 0), ([1570, 1100], 0), ([3000, 40], 1100)])
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_attention_rows_in_parts_of_odd_lengths(serve, D, kv, window):
-    # parts of 17 and 25 times 32 tokens: a step of 64 goes past the end of one
+    # parts of an odd number of times 32 tokens: a step of 64 goes past the end of one
     c = Case(serve, kv, [33, 21], heads=2, D=D, page=32, dt="bf16", seed=sum(kv))
     c.fill(1)
     check(c, 2, window=window)
