@@ -210,8 +210,8 @@ __global__ __launch_bounds__(NW * 64) void w8_few_kernel(W8Args a)
 // a step, in three buffers: a step reads one, the next one is whole, and the one after is being written, so that a wave's
 // operands are read ahead over the barrier between steps.  The weights come as operands from memory, 64
 // inputs fetched where those before them in the registers have been used.  Bound by the matrix instructions: 4096 x 8192 x
-// 8192 in 217 us, 2.5 POP/s (a library's product of 8192^3: 2.1), which are busy 55 % of the cycles, vector
-// instructions 23 %; a compute unit holds one workgroup (96 KB of LDS), which waits at a barrier a step.
+// 8192 in 217 us, 2.5 POP/s (a library's product of 8192^3: 2.1), which are busy 61 % of the cycles, vector
+// instructions 25 %; a compute unit holds one workgroup (96 KB of LDS), which waits at a barrier a step.
 template <bool F16, int MT, int NT, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, WM * WN <= 4 ? 1 : 2) void w8_tiles_kernel(W8Args a)
 {
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(WM * WN * 64, WM * WN <= 4 ? 1 : 2) void w8_tiles_k
 // of 16 outputs.  The waves of a part share the rows: 128 inputs of them go into LDS (pieces as in w8_tiles_kernel) while the
 // inputs before are computed, so that they come from memory once for 16 TW outputs; rows and weights are DEEP steps
 // ahead in registers (loads return in order: the one that is awaited has to be as old as all the
-// others).  At the end the parts add up through LDS.  blockIdx.y: the block of rows.  77 x 5003 x 4112: 11.3 us, of which 4.4
+// others).  At the end the parts add up through LDS.  blockIdx.y: the block of rows.  77 x 5003 x 4112: 10.3 us, of which 4.4
 // are the bytes.
 template <bool F16, int MT, int KP, int TW, int DEEP>
 __global__ __launch_bounds__(KP * TW * 64) void w8_rows_kernel(W8Args a)
