@@ -9,8 +9,8 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// Rows in 16 bits that a product for few rows puts into 8 itself: as many as are computed anew by every workgroup in the
-// time that the first weights take, and as their codes have room in LDS.
+// Rows in 16 bits that a product for few rows puts into 8 itself, which every workgroup does: up to four (4 x 4096 x 4096: 8.2 us, by a
+// launch of their own 5.0 and 2.6 and a gap), and as many as their codes have room in LDS.
 constexpr int kW8Rows16 = 4, kW8Lds = 32768;
 
 // 16 bytes from any address.
@@ -91,6 +91,43 @@ struct Ends {
     }
 };
 
+// Up to 1 << SH rows in 16 bits into 8, in LDS: as many of the NW waves to each, 4 values a thread and turn.
+template <bool F16, int NW, int SH>
+__device__ __forceinline__ void rows_to_8(const W8Args &a, i32x4 *codes, uint32_t *tops, float *scales)
+{
+    constexpr int WAVES = NW >> SH, PER = WAVES * 64, MOST = (kW8Lds >> SH) / 4 / PER;   // w8_takes_16
+    const int lane = threadIdx.x & 63, wave = wave_id(), m = wave / WAVES, t = (int)threadIdx.x % PER;
+    const bool row_here = m < a.rows;
+    const uint16_t *row = (const uint16_t *)a.x16 + (long long)m * a.x_stride;
+    uint32_t v[MOST][2], top = 0;
+#pragma unroll
+    for (int i = 0; i < MOST; i++) {
+        const int k = 4 * (t + i * PER);
+        v[i][0] = v[i][1] = 0;
+        if (row_here && k < a.n_in) __builtin_memcpy(v[i], __builtin_assume_aligned(row + k, 2), 8);
+    }
+    const auto value = [&](int i, int j) { return to_float<F16>((uint16_t)(v[i][j >> 1] >> (16 * (j & 1)))); };
+#pragma unroll
+    for (int i = 0; i < MOST; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) top = max(top, __float_as_uint(value(i, j)) & 0x7fffffffu);
+    top = over_wave(top, [](uint32_t p, uint32_t q) { return max(p, q); });
+    if (lane == 0) tops[wave] = top;
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) top = max(top, tops[m * WAVES + i]);
+    const Row8 r = row8_of(top);
+    if (t == 0 && row_here) scales[m] = r.scale;
+#pragma unroll
+    for (int i = 0; i < MOST; i++) {
+        const int k = 4 * (t + i * PER);
+        uint32_t c = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++) c |= code8(r, value(i, j)) << (8 * j);
+        if (row_here && k < a.n_in) ((uint32_t *)codes)[(m * a.n_in + k) / 4] = c;
+    }
+}
+
 // Few rows (up to 16; bound by the weights' bytes, and below some 32 MB of them by two trips to memory and the sum through
 // LDS).  A workgroup takes NT tiles of 16 outputs; its NW waves take every NW-th D chunks of 64 inputs, each chunk's place in
 // the registers fetched again where it has been used, and add up through LDS.  1 x 4096 x 4096: 5.0 us for 16.8 MB, 3.4 TB/s;
@@ -143,39 +180,9 @@ __global__ __launch_bounds__(NW * 64) void w8_few_kernel(W8Args a)
         ends[q].fetch(a, em[q], en[q]);
     }
     if constexpr (X16) {
-        // a row at a time, 4 values a thread and turn
-        for (int m = 0; m < a.rows; m++) {
-            const uint16_t *row = (const uint16_t *)a.x16 + (long long)m * a.x_stride;
-            constexpr int MOST = (kW8Lds / 4 + NW * 64 - 1) / (NW * 64);
-            uint32_t v[MOST][2], top = 0;
-#pragma unroll
-            for (int i = 0; i < MOST; i++) {
-                const int k = 4 * ((int)threadIdx.x + i * NW * 64);
-                v[i][0] = v[i][1] = 0;
-                if (k < a.n_in) __builtin_memcpy(v[i], __builtin_assume_aligned(row + k, 2), 8);
-            }
-            const auto value = [&](int i, int j) { return to_float<F16>((uint16_t)(v[i][j >> 1] >> (16 * (j & 1)))); };
-#pragma unroll
-            for (int i = 0; i < MOST; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) top = max(top, __float_as_uint(value(i, j)) & 0x7fffffffu);
-            top = over_wave(top, [](uint32_t p, uint32_t q) { return max(p, q); });
-            if (m > 0) lds_barrier();   // the row before has read its own
-            if (lane == 0) tops[wave] = top;
-            lds_barrier();
-#pragma unroll
-            for (int i = 0; i < NW; i++) top = max(top, tops[i]);
-            const Row8 r = row8_of(top);
-            if (threadIdx.x == 0) scales[m] = r.scale;
-#pragma unroll
-            for (int i = 0; i < MOST; i++) {
-                const int k = 4 * ((int)threadIdx.x + i * NW * 64);
-                uint32_t c = 0;
-#pragma unroll
-                for (int j = 0; j < 4; j++) c |= code8(r, value(i, j)) << (8 * j);
-                if (k < a.n_in) ((uint32_t *)codes)[(m * a.n_in + k) / 4] = c;
-            }
-        }
+        if (a.rows == 1) rows_to_8<F16, NW, 0>(a, codes, tops, scales);
+        else if (a.rows == 2) rows_to_8<F16, NW, 1>(a, codes, tops, scales);
+        else rows_to_8<F16, NW, 2>(a, codes, tops, scales);
         lds_barrier();
 #pragma unroll
         for (int d = 0; d < D; d++) load_x(wave * D, d);
@@ -544,7 +551,8 @@ W8Form w8_form(int rows, int n_out, int n_in)
     return best;
 }
 
-bool w8_takes_16(int rows, int n_in) { return rows <= kW8Rows16 && (long long)rows * n_in <= kW8Lds; }
+// Three rows have the threads of four.
+bool w8_takes_16(int rows, int n_in) { return rows <= kW8Rows16 && (rows == 3 ? 4ll : rows) * n_in <= kW8Lds; }
 
 hipError_t launch_w8(const W8Args &a, bool f16, hipStream_t s) { return f16 ? pick<true>(a, s) : pick<false>(a, s); }
 

@@ -264,6 +264,17 @@ def test_product_strides_and_shapes(serve, m):
     assert torch.equal(W.matmul(serve.quantise_rows(x[0, 1:1 + k].cuda())), W.matmul(x[0, 1:1 + k].cuda()))
 
 
+@pytest.mark.parametrize("m,k", [(1, 32768), (1, 32784), (2, 16384), (2, 16400), (3, 8192), (3, 8208), (3, 10912), (3, 10928), (4, 8192), (4, 8208), (4, 16), (3, 48), (2, 4112)])
+def test_rows_in_16_bits_up_to_what_a_product_takes(serve, m, k):
+    wc, ws = _weights(37, k, 15)
+    W = serve.W8Weight(wc.cuda(), ws.cuda())
+    x = torch.randn(m, k, generator=_gen(16)).bfloat16()
+    x[:, -1] = torch.arange(1, m + 1) * 20   # the largest, at the end
+    codes, scales = quantised(x.float())
+    _check(W.matmul(x.cuda()), codes, scales, wc, ws, None, "bf16")
+    assert torch.equal(W.matmul(x.cuda()), W.matmul(serve.quantise_rows(x.cuda())))
+
+
 @pytest.mark.parametrize("m", [1, 6, 40])
 def test_outputs_beside_inputs_and_over_them(serve, m):
     from paper_2609_02109_amd import mf

@@ -120,6 +120,7 @@ def test_product_workspace():
     assert size(rows=5000) == 0 and size(rows=0, scales=None) == 0 and size(rows=4, scales=None) == 0 and size(rows=4, k=8192, scales=None) == 0
     assert size(rows=5, scales=None) == 5 * 256 + 5 * 4
     assert size(rows=3, k=16 * 1000, scales=None) == (3 * 16000 + 255) // 256 * 256 + 12
+    assert size(rows=3, k=8192, scales=None) == 0 and size(rows=3, k=8208, scales=None) == (3 * 8208 + 255) // 256 * 256 + 12
     assert size(rows=1, k=32784, scales=None) == (32784 + 255) // 256 * 256 + 4
     a = _w8(rows=5, scales=None)
     need = _bytes(mf.lib.mf_w8_workspace_size, a)
