@@ -9,8 +9,9 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-// Rows in 16 bits that a product for few rows puts into 8 itself, which every workgroup does: up to four (4 x 4096 x 4096: 8.2 us, by a
-// launch of their own 5.0 and 2.6 and a gap), and as many as their codes have room in LDS.
+// Rows in 16 bits that a product for few rows puts into 8 itself, which every workgroup does, as far as their codes have room in
+// LDS: up to four (4 x 4096 x 4096: 7.8 us; by a launch of their own about as much in a graph, and 3 us more to call); eight
+// are slower (8 x 28672 x 4096: 28.4, by a launch of their own 25.4).
 constexpr int kW8Rows16 = 4, kW8Lds = 32768;
 
 // 16 bytes from any address.

@@ -264,7 +264,8 @@ def test_product_strides_and_shapes(serve, m):
     assert torch.equal(W.matmul(serve.quantise_rows(x[0, 1:1 + k].cuda())), W.matmul(x[0, 1:1 + k].cuda()))
 
 
-@pytest.mark.parametrize("m,k", [(1, 32768), (1, 32784), (2, 16384), (2, 16400), (3, 8192), (3, 8208), (3, 10912), (3, 10928), (4, 8192), (4, 8208), (4, 16), (3, 48), (2, 4112)])
+@pytest.mark.parametrize("m,k", [(1, 32768), (1, 32784), (2, 16384), (2, 16400), (3, 8192), (3, 8208), (3, 10912), (3, 10928), (4, 8192), (4, 8208), (4, 16), (3, 48), (2, 4112),
+                                 (5, 4096), (8, 4096), (8, 4112), (7, 16), (6, 2000), (9, 4096)])
 def test_rows_in_16_bits_up_to_what_a_product_takes(serve, m, k):
     wc, ws = _weights(37, k, 15)
     W = serve.W8Weight(wc.cuda(), ws.cuda())
