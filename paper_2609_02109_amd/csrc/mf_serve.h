@@ -244,7 +244,7 @@ struct W8PackArgs {
 hipError_t launch_w8_pack(const W8PackArgs &a, hipStream_t s);
 enum W8Form {
     kW8Few16, kW8Few8x2,                                    // up to 16 rows: waves of a workgroup (x tiles of outputs)
-    kW8Rows32, kW8Rows32x4,                                 // up to 32
+    kW8Rows32x1, kW8Rows32, kW8Rows32x4,                    // up to 32
     kW8Block32, kW8Block64, kW8Block64x4, kW8Block128x4,    // rows of a block (x tiles of outputs, else two)
     kW8Tiles128, kW8Tiles256                                // by 256 outputs
 };

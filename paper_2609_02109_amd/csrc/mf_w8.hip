@@ -493,6 +493,7 @@ hipError_t pick(const W8Args &a, hipStream_t s)
     switch (w8_form(a.rows, a.n_out, a.n_in)) {
         case kW8Few16: return go_few<F16, 1, 16, 2>(a, s);
         case kW8Few8x2: return go_few<F16, 2, 8, 2>(a, s);
+        case kW8Rows32x1: return go_rows<F16, 2, 4, 1, 4>(a, s);
         case kW8Rows32: return go_rows<F16, 2, 2, 2, 4>(a, s);
         case kW8Rows32x4: return go_rows<F16, 2, 2, 4, 4>(a, s);
         case kW8Block32: return go_rows<F16, 2, 4, 2, 2>(a, s);
@@ -517,26 +518,27 @@ hipError_t launch_w8_pack(const W8PackArgs &a, hipStream_t s)
 // Forms, with both sides measured (us, outputs x inputs, weights from memory):
 // * up to 16 rows a workgroup a tile of outputs, 16 waves (1 x 4096 x 4096: 5.0, 8 waves 5.6); of many outputs two tiles, so
 //   that the rows are read half as often (16 x 8192 x 8192: 13.3, one 16.2; 16 x 28672 x 4096: 24.2, one 28.5).
-// * up to 32 the rows go through LDS, for two tiles (32 x 4096 x 4096: 7.1, the form for 16 rows with two of them 7.8; 32 x 8192 x
+// * up to 32 the rows go through LDS, of few outputs for one tile with the inputs in four parts (32 x 4096 x 4096: 6.7; 22 x 1970 x
+//   16320: 15.4, two tiles and two parts 18.9), for two tiles (32 x 4096 x 4096: 7.1, the form for 16 rows with two of them 7.8; 32 x 8192 x
 //   8192: 15.2 and 23), or four of many outputs (32 x 28672 x 4096: 25.8, two 28.7).
 // * past that blocks of rows and outputs, by what each form would take: a + b k + (c + d k) r us, k its inputs over 4096, r its
 //   blocks over the 256 compute units (tiles, of which a unit holds one: rounded up).  Fitted to 75 sizes of 33 to 4096 rows, 260
 //   to 29000 outputs and 400 to 14000 inputs, timed with every form: within 10 to 15 % of them, and the form that it takes is
-//   2.4 % behind the best at the mean and 23 % at most.  Blocks of 32 x 32, 64 x 32, 64 x 64, 128 x 64, 128 x 256, 256 x 256:
+//   1.8 % behind the best at the mean and 23 % at most.  Blocks of 32 x 32, 64 x 32, 64 x 64, 128 x 64, 128 x 256, 256 x 256:
 //   64 x 4096 x 4096: 6.7, 8.5, 9.5, 14, 27, 45; 512 x 4096 x 4096: 32, 27, 18, 18, 29, 46; 1032 x 14180 x 1600: 128, 108, 60, 67, 38, 54;
 //   4096 x 8192 x 8192: 1350, 750, 490, 410, 260, 217.
 W8Form w8_form(int rows, int n_out, int n_in)
 {
     const long long tiles = (n_out + kW8Tile - 1) / kW8Tile;
     if (rows <= 16) return tiles <= 256 ? kW8Few16 : kW8Few8x2;
-    if (rows <= 32) return tiles <= 1024 ? kW8Rows32 : kW8Rows32x4;
+    if (rows <= 32) return tiles <= 256 ? kW8Rows32x1 : tiles <= 1024 ? kW8Rows32 : kW8Rows32x4;
     const struct {
         W8Form form;
         int rows, outputs;
         float a, b, c, d;
-    } forms[] = {{kW8Block32, 32, 32, 2.9f, 1.3f, 0.6f, 3.7f},    {kW8Block64, 64, 32, 3.3f, 2.9f, 1.3f, 5.3f},
-                 {kW8Block64x4, 64, 64, 3.3f, 4.5f, 1.3f, 6.6f},  {kW8Block128x4, 128, 64, 3.7f, 8.5f, 4.1f, 8.2f},
-                 {kW8Tiles128, 128, 256, 0.f, 0.f, 6.3f, 25.f},   {kW8Tiles256, 256, 256, 0.f, 0.f, 9.4f, 40.f}};
+    } forms[] = {{kW8Block32, 32, 32, 2.8f, 1.5f, 0.6f, 4.1f},    {kW8Block64, 64, 32, 2.8f, 2.9f, 1.3f, 5.3f},
+                 {kW8Block64x4, 64, 64, 3.4f, 4.5f, 1.3f, 6.6f},  {kW8Block128x4, 128, 64, 3.6f, 8.7f, 3.3f, 8.1f},
+                 {kW8Tiles128, 128, 256, 0.f, 0.f, 6.6f, 25.9f},  {kW8Tiles256, 256, 256, 0.f, 0.f, 9.2f, 39.2f}};
     W8Form best = kW8Block32;
     float least = INFINITY;
     const float k = (float)n_in / 4096.f;

@@ -208,7 +208,8 @@ SIZES = [(1, 16, 16), (1, 1, 64), (2, 17, 80), (3, 515, 160), (16, 64, 256), (17
          (65, 48, 2048), (77, 333, 4112), (128, 128, 128), (129, 257, 144), (200, 33, 96), (300, 700, 1040), (5, 31, 16384), (16, 20000, 128),
          (513, 1025, 272), (4, 8, 131056),
          # the forms for many rows or outputs
-         (20, 17000, 80), (4, 6000, 8192), (5, 300, 8208), (130, 5000, 400), (500, 4100, 272), (3000, 2500, 144), (4090, 4090, 208)]
+         (20, 17000, 80), (4, 6000, 8192), (5, 300, 8208), (130, 5000, 400), (500, 4100, 272), (3000, 2500, 144), (4090, 4090, 208),
+         (25, 5001, 272), (30, 4099, 144), (43, 6600, 368), (64, 4100, 4096), (512, 4093, 4096), (600, 5003, 272)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
