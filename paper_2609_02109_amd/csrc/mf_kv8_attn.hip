@@ -9,7 +9,9 @@ hipError_t launch_attn8_d128(const KvAttnArgs &a, const KvPlan &p, bool f16, hip
 hipError_t launch_attn8_d256(const KvAttnArgs &a, const KvPlan &p, bool f16, hipStream_t s);
 
 // By rows: tiles of 64 rt rows, each over `splits` parts of its tokens.  As many parts as leave all workgroups on the card at
-// once (two a compute unit; of heads of 64 four), of about eight steps of 32 tokens at the least.  us: about what that takes.
+// once (two a compute unit; of heads of 64 four), of about eight steps of 32 tokens at the least; a half of that and so on where it
+// takes less: parts are written and read (9 x 213 query tokens over 466, 8 over 2 heads of 256: two parts 35 us, one 25).
+// us: about what that takes.
 struct RowsPlan {
     long long row_tiles, items, splits;
     float us;
@@ -20,13 +22,20 @@ static RowsPlan rows_plan(int rt, long long rows, long long heads, int head_dim,
     RowsPlan p;
     p.row_tiles = (rows + wg_rows - 1) / wg_rows;
     p.items = p.row_tiles * heads;
+    p.us = INFINITY;
     const long long steps = (span + kAttnStep - 1) / kAttnStep, mean = steps - max_new / 2 / kAttnStep, room = head_dim == 64 ? 1024 : 512;
     long long splits = p.items > 0 ? room / p.items : 1;
     if (splits > (mean + 4) / 8) splits = (mean + 4) / 8;
-    p.splits = splits > 1 ? splits : 1;
-    const float rounds = (float)((p.items * p.splits + room - 1) / room), parts = (float)(p.items * p.splits * wg_rows) * (float)(head_dim + 2) * 4.f;
-    // a beginning, the steps, and where there are parts their writing, reading and a launch
-    p.us = rounds * (9.f + (float)steps / (float)p.splits * (rt == 1 ? 0.84f : 1.15f)) + (p.splits > 1 ? 4.f + 2.f * parts / 4e6f : 0.f);
+    if (splits < 1) splits = 1;
+    for (; splits >= 1; splits /= 2) {
+        const float rounds = (float)((p.items * splits + room - 1) / room), parts = (float)(p.items * splits * wg_rows) * (float)(head_dim + 2) * 4.f;
+        // a beginning, the steps, and where there are parts their writing, reading and a launch
+        const float us = rounds * (9.f + (float)steps / (float)splits * (rt == 1 ? 0.84f : 1.15f)) + (splits > 1 ? 4.f + 2.f * parts / 4e6f : 0.f);
+        if (us < p.us) {
+            p.us = us;
+            p.splits = splits;
+        }
+    }
     return p;
 }
 
