@@ -669,8 +669,9 @@ mf_status mf_kv8_cache_bytes(const mf_kv8_cache *cache, size_t *bytes);
  * the same batches and arguments.  What a page number that is not the cache's, or a
  * token that is not there, does is the same.  Attention: the weights of the values,
  * times their scales, are rounded to binary16 (down to 2^-34 of a row's largest such
- * product), queries to 2^-39 of a row's largest value where they are below 2^-28 of it;
- * scale times that value is to stay below 2^90.  No
+ * product, 2^-24 in rows whose largest score is past 2^19), queries to 2^-39 of a row's
+ * largest value where they are below 2^-28 of it; scale times that value is to stay
+ * below 2^90.  Scores are fp32, whatever their size: off by 2^-24 of themselves and more.  No
  * bit of a row's result depends on blocks of which it sees no token; of a block
  * that it sees a part of, the scales are all its tokens'.  Blocks of zeros in memory are
  * tokens of zeros (to attention, their values are below 2^-32). */

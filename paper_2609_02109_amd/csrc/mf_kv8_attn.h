@@ -19,9 +19,14 @@
 // largest has bits left, whatever sizes the blocks' values are of.  The sum of p adds w / scale.
 // The largest is looked for only where the weights show that it is needed: when four
 // together reach 2^14 the base goes to the largest so far less 10 (both as powers of two), and the step's
-// weights are computed again.
+// weights are computed again.  Rows whose base is 2^20 or more, of either sign, take the largest so far as the
+// base at every step and have weights up to 1, of scores that are rounded before the base is taken off: the sum in
+// one step, s + (log2 scale - base), is off by some of fp32's places at the base, which from 2^26 on
+// is more than binary16 has above the base.
 // Values' operands are whole numbers: 1024 + u, a number of binary16's with the bits 0x6400 | u, less 1152.
 #pragma once
+
+#include <type_traits>
 
 #include "mf_kv_attn.h"
 
@@ -96,16 +101,17 @@ __device__ __forceinline__ int again(int x)
 }
 
 // What S times 32 tokens from t0 on add to the rows, by their scores.  full: every row sees every token.
+// far: some row of the wave has a base of 2^20 or more.
 template <int D, int RT, int S, class AV>
 __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Sight (&see)[RT], const float (&c)[RT], float (&base)[RT], float (&l)[RT],
-                                           f32x4 (&o)[RT][D / 16], bool full, const Step8 (&now)[S], int t0, const AV &value_at)
+                                           f32x4 (&o)[RT][D / 16], bool full, const Step8 (&now)[S], int t0, bool &far, const AV &value_at)
 {
     const int qt = (threadIdx.x & 63) >> 4;
     u32x4 w[S][RT];
     float sum[S][RT][2];   // of a block's weights
     float highest[RT];
     constexpr float most = 16384.f;
-    const auto weigh = [&] {
+    const auto weigh = [&](auto any_base) {
         float over = 0.f;
 #pragma unroll
         for (int t = 0; t < RT; t++) {
@@ -114,8 +120,11 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
             for (int k = 0; k < S; k++) {
                 float e[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    e[i] = __builtin_amdgcn_exp2f(fmaf(sc[k][t][i >> 2][i & 3], now[k].ks[i >> 2] * c[t], now[k].lv[i >> 2] - base[t]));
+                for (int i = 0; i < 8; i++) {
+                    float x = fmaf(sc[k][t][i >> 2][i & 3], now[k].ks[i >> 2] * c[t], now[k].lv[i >> 2] - base[t]);
+                    if (decltype(any_base)::value && is_far(base[t])) x = fmaf(sc[k][t][i >> 2][i & 3], now[k].ks[i >> 2] * c[t], now[k].lv[i >> 2]) - base[t];
+                    e[i] = __builtin_amdgcn_exp2f(x);
+                }
                 if (!full) {
                     const int at = again(t0 + 32 * k);   // else the comparisons are made for every step
 #pragma unroll
@@ -134,11 +143,12 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
         }
         return __any(over >= most);
     };
-    if (weigh()) {
+    if (weigh(std::false_type()) || far) {
+        bool any = false;
 #pragma unroll
         for (int t = 0; t < RT; t++) {
             // only the rows that need it, so that no row's result depends on another's
-            const bool hit = quarters_max(highest[t]) >= most;
+            const bool over = quarters_max(highest[t]) >= most, hit = over || is_far(base[t]);
             float mx = kNoBase;
 #pragma unroll
             for (int k = 0; k < S; k++)
@@ -147,14 +157,17 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
                     const float s = fmaf(sc[k][t][i >> 2][i & 3], now[k].ks[i >> 2] * c[t], now[k].lv[i >> 2]);
                     if (full || sees8(see[t], now[k].ok, t0 + 32 * k, qt, i)) mx = fmaxf(mx, s);
                 }
-            mx = quarters_max(mx) - 10.f;
+            mx = quarters_max(mx);
+            if (!is_far(mx)) mx -= 10.f;
             const float to = hit ? fmaxf(mx, base[t]) : base[t], a = __builtin_amdgcn_exp2f(base[t] - to);
             base[t] = to;
+            any |= is_far(to) && to != kNoBase;
             l[t] *= a;
 #pragma unroll
             for (int d = 0; d < D / 16; d++) o[t][d] *= a;
         }
-        weigh();
+        far = __any(any);
+        weigh(std::true_type());
     }
 #pragma unroll
     for (int k = 0; k < S; k++)
@@ -301,6 +314,7 @@ __device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, co
     Sight see[RT];
     float c[RT], first[RT], base[RT], l[RT];
     f32x4 o[RT][D / 16];
+    bool far = false;
     load_queries<F16, D, RT>(a, h, sr, row0, last, q, see);
     const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
 
@@ -348,7 +362,7 @@ __device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, co
         attn8_scores<D, RT>(q, first, sc[0], [&](int u, int n) { return key_operand(x.kc[u][n >> 1][2 * (n & 1)], x.kc[u][n >> 1][2 * (n & 1) + 1]); });
         // the next step's keys and values are fetched where this one has no more use for its own
         keys(i);
-        attn8_step<D, RT, 1>(sc, see, c, base, l, o, full, now, t0, value_at);
+        attn8_step<D, RT, 1>(sc, see, c, base, l, o, full, now, t0, far, value_at);
         values(i);
         now[0] = next;
         t0 += STRIDE;
@@ -391,6 +405,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn8_rows_kernel(KvAttnAr
     Sight see[RT];
     float c[RT], first[RT], base[RT], l[RT];
     f32x4 o[RT][D / 16];
+    bool far = false;
     load_queries<F16, D, RT>(a, h, sr, row0, last, q, see);
     const Sight see0 = sight_of(sr.first_p + row0 / a.per_kv, a.window, limit), see1 = sight_of(sr.first_p + last / a.per_kv, a.window, limit);
     const Range t = range_of(sr, wg0 / a.per_kv, (row_end - 1) / a.per_kv, a.window);
@@ -463,7 +478,7 @@ __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn8_rows_kernel(KvAttnAr
                 attn8_scores<D, RT>(q, first, sc[k], [&](int u, int n) { return lds[buf][k][u * 2 * NC + n][lane]; });
                 ok &= now[k].ok;
             }
-            attn8_step<D, RT, S>(sc, see, c, base, l, o, ok == 3 && t0 >= see1.lo && t0 + STEP - 1 <= see0.hi, now, t0,
+            attn8_step<D, RT, S>(sc, see, c, base, l, o, ok == 3 && t0 >= see1.lo && t0 + STEP - 1 <= see0.hi, now, t0, far,
                                  [&](int k, int n) { return lds[buf][k][KEYS + n][lane]; });
         }
 #pragma unroll

@@ -19,7 +19,12 @@ __device__ __forceinline__ Sight sight_of(long long p, int window, int limit)
     return v;
 }
 
-constexpr float kNoBase = -1e30f;   // before the first token; finite, so that differences of bases are
+constexpr float kNoBase = -1e38f;   // before the first token: below all scores; finite, so that differences of bases are
+// From this base on a score's place in fp32 is 2^-3 and more.  What a step adds to the base and to a score in another
+// order no longer meets: weights go by scores that are rounded as the base was, from the largest down, which
+// then is the base itself.
+constexpr float kFarBase = 0x1p20f;
+__device__ __forceinline__ bool is_far(float base) { return fabsf(base) >= kFarBase; }
 
 // A sequence of the batch as far as it lies in the step's rows and the cache,
 // whatever the device arrays hold.
