@@ -146,8 +146,9 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_rows_kernel(KvAttnArgs a
                      h * a.per_kv + (int)(row - (long long)i * a.per_kv));
 }
 
-// Few parts, up to what join_row takes at a time: D / 4 threads a row add them up in the order that it does, four dims
-// each, and a workgroup takes several rows (1 x 2000 over 2000, 32 heads over 8 of 128, two parts of the 8-bit cache: 122 us in all, by a workgroup a row 173).
+// Few parts, up to what join_row takes at a time: D / 4 threads a row add them up as it does, bit for bit, four dims
+// each, and a workgroup takes several rows (1 x 2000 over 2000 of the 4-bit cache, 32 heads over 8 of 128, two parts: 121 us in
+// all, by a workgroup a row 171).
 template <bool F16, int D>
 __global__ __launch_bounds__(kJoinWaves * 64) void join_few_kernel(KvAttnArgs a)
 {
@@ -164,6 +165,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_few_kernel(KvAttnArgs a)
     float base = kNoBase, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < a.splits; i++) base = fmaxf(base, ml[first + (long long)i * a.slot_rows][0]);
+    const float end = ml[first + (long long)(a.splits - 1) * a.slot_rows][0];
     for (int i = 0; i < a.splits; i += 4) {
         f32x2 m[4];
         f32x4 v[4];
@@ -176,9 +178,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void join_few_kernel(KvAttnArgs a)
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             if (i + j >= a.splits) break;
-            const float x = __builtin_amdgcn_exp2f(m[j][0] - base);
-            l += m[j][1] * x;
-            o += v[j] * x;
+            // by way of the last part's base, as join_row has it: the same bits
+            const float to = fmaxf(m[j][0], end), y = __builtin_amdgcn_exp2f(m[j][0] - to), x = __builtin_amdgcn_exp2f(to - base);
+            l += m[j][1] * y * x;
+            o += v[j] * y * x;
         }
     }
     const int i = (int)(row / a.per_kv), head = h * a.per_kv + (int)(row - (long long)i * a.per_kv);
