@@ -222,7 +222,10 @@ hipError_t go_join(const KvAttnArgs &a, const KvPlan &p, bool f16, long long ite
 {
     const auto go = [&](void (*kernel)(KvAttnArgs)) { return each_launch(kernel, a, items * a.slot_rows, kJoinWaves * 64, s); };
     constexpr int few = kJoinWaves * 64 / (D / 4);
-    if (p.rows_by_wave && a.splits <= few)
+    // a thread goes over its row's parts one after another, which pays where there are rows for all compute units: a workgroup a row
+    // and several rows to one, us, of the 4-bit cache (rows that tiles have x parts): 1024 x 8: 30.4, 33.7; 2048 x 8: 32.2, 34.6; 4096 x 3:
+    // 33.1, 30.9; 8192 x 8: 55.3, 51.4; of the 8-bit one: 4096 x 16: 38.0, 42.3; 7168 x 9: 33.3, 31.3; 1024 x 16: 14.0, 21.2
+    if (p.rows_by_wave && a.splits <= few && items * a.slot_rows > 512 * (long long)a.splits)
         return each_launch(f16 ? join_few_kernel<true, D> : join_few_kernel<false, D>, a, items * a.slot_rows / few, kJoinWaves * 64, s);
     if (p.rows_by_wave) return f16 ? go(join_rows_kernel<true, D>) : go(join_rows_kernel<false, D>);
     return f16 ? go(join_tokens_kernel<true, D>) : go(join_tokens_kernel<false, D>);
