@@ -23,8 +23,15 @@
 // to the largest score so far (in powers of two) less 10 and the step's weights
 // are computed again.  Binary16 then holds weights down to 2^-34 of the largest,
 // and the small weights of long contexts are not lost; a step's w are brought to
-// the same range by a power of two where scales are not of ordinary size.
+// the same range by a power of two where scales are not of ordinary size.  Rows
+// whose base is 2^20 or more, of either sign, take the largest score so far as the base at
+// every step, and weights up to 1, of scores that are rounded before the base is taken off: the
+// product and the difference in one step are off by some of fp32's places at the base, which from
+// 2^27 on is more than binary16 has above the base.
 #pragma once
+
+#include <type_traits>
+
 
 #include "mf_kv_attn.h"
 
@@ -37,6 +44,7 @@ struct AttnState {
     f32x4 o[RT][DT];      // sum w c, 2^-24 (even t) or 2^-20 times: dims 16 t + 4 (l / 16) + r
     f32x4 om[RT];         // sum p off: element r is group (4 (l / 16) + r) % NG
     float base[RT], l[RT];   // weights are relative to 2^base; sum of p over the lane's tokens
+    bool far;             // some row of the wave has a base of 2^20 or more
 };
 
 // A step's 32 tokens as a lane holds them (mf_serve.h; u: the block of 16).
@@ -178,13 +186,18 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
     }
     u32x4 w[RT];
     float e[RT][8];
-    for (bool raised = false;; raised = true) {   // twice at most
-        int highest[RT], over = 0;
-        constexpr int most = (15 + 14) << 10;   // 2^14 in binary16
+    int highest[RT];
+    constexpr int most = (15 + 14) << 10;   // 2^14 in binary16
+    const auto weigh = [&](auto any_base) {
+        int over = 0;
 #pragma unroll
         for (int t = 0; t < RT; t++) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) e[t][i] = __builtin_amdgcn_exp2f(fmaf(p[t][i >> 2][i & 3], c[t], -st.base[t]));
+            for (int i = 0; i < 8; i++) {
+                float x = fmaf(p[t][i >> 2][i & 3], c[t], -st.base[t]);
+                if (decltype(any_base)::value && is_far(st.base[t])) x = p[t][i >> 2][i & 3] * c[t] - st.base[t];
+                e[t][i] = __builtin_amdgcn_exp2f(x);
+            }
 #pragma unroll
             for (int i = 0; i < 4; i++) w[t][i] = pack2<true>(e[t][2 * i], e[t][2 * i + 1]);
             // none is negative: as whole numbers they are in the same order
@@ -193,22 +206,29 @@ __device__ __forceinline__ void attn_step(AttnState<D, G, RT> &st, const u32x4 (
             highest[t] = max(high[0], high[1]);
             over = max(over, highest[t]);
         }
-        if (raised || !__any(over >= most)) break;
+        return __any(over >= most);
+    };
+    if (weigh(std::false_type()) || st.far) {
+        bool any = false;
 #pragma unroll
         for (int t = 0; t < RT; t++) {
             // only the rows that need it, so that no row's result depends on another's
-            const bool hit = quarters_max((float)highest[t]) >= (float)most;
+            const bool over = quarters_max((float)highest[t]) >= (float)most, hit = over || is_far(st.base[t]);
             float mx = p[t][0][0];
 #pragma unroll
             for (int i = 1; i < 8; i++) mx = fmaxf(mx, p[t][i >> 2][i & 3]);
-            mx = fmaf(quarters_max(mx), c[t], -10.f);
+            mx = quarters_max(mx);
+            mx = is_far(mx * c[t]) ? mx * c[t] : fmaf(mx, c[t], -10.f);
             const float base = hit ? fmaxf(mx, st.base[t]) : st.base[t], a = __builtin_amdgcn_exp2f(st.base[t] - base);
             st.base[t] = base;
+            any |= is_far(base) && base != kNoBase;
             st.l[t] *= a;
             st.om[t] *= a;
 #pragma unroll
             for (int d = 0; d < D / 16; d++) st.o[t][d] *= a;
         }
+        st.far = __any(any);
+        weigh(std::true_type());
     }
 #pragma unroll
     for (int t = 0; t < RT; t++)
@@ -371,6 +391,7 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
     u32x2 qsum[RT];        // sum q as the right operand of the offsets' product: its pieces
     float c[RT];
     AttnState<D, G, RT> st;
+    st.far = false;
 #pragma unroll
     for (int t = 0; t < RT; t++) {
         float qs[NG], big = 0.f;
