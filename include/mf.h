@@ -564,9 +564,9 @@ typedef struct {
     int64_t n;              /* values of a row, 1 .. 2^17 */
     const void *d_x;        /* [rows][n], row stride x_stride >= n */
     int64_t x_stride;
-    int8_t *d_codes;        /* [rows][n], row stride codes_stride >= n; not over d_x */
+    int8_t *d_codes;        /* [rows][n], row stride codes_stride >= n */
     int64_t codes_stride;
-    float *d_scales;        /* [rows] */
+    float *d_scales;        /* [rows]; neither is over anything else that the call reads or writes (EINVAL) */
 } mf_rows8_args;
 
 /* y = x. */
@@ -580,7 +580,7 @@ typedef struct {
     const void *d_residual; /* [rows][n], row stride residual_stride >= n, or NULL */
     int64_t residual_stride;
     void *d_sum;            /* h, with a residual only: [rows][n], row stride sum_stride >= n; may be d_x or
-                               d_residual itself with the same stride, else over neither */
+                               d_residual itself with the same stride, else over neither, nor over d_weight (EINVAL) */
     int64_t sum_stride;
     const void *d_weight;   /* [n] */
     float eps;              /* finite, >= 0 */
@@ -595,7 +595,8 @@ typedef struct {
 } mf_gate8_args;
 mf_status mf_gate8(const mf_gate8_args *args, void *stream);
 
-/* What rows stand for, rounded to dtype (MF_F32, MF_BF16 or MF_F16): d_out [rows][n], row stride out_stride >= n. */
+/* What rows stand for, rounded to dtype (MF_F32, MF_BF16 or MF_F16): d_out [rows][n], row stride out_stride >= n,
+ * not over d_codes or d_scales (EINVAL). */
 mf_status mf_rows8_values(mf_dtype dtype, int64_t rows, int64_t n, const int8_t *d_codes, int64_t codes_stride,
                           const float *d_scales, void *d_out, int64_t out_stride, void *stream);
 
@@ -614,7 +615,7 @@ typedef struct {
 mf_status mf_w8_pack_bytes(const mf_w8_desc *desc, size_t *bytes);
 
 /* Lays weights out for mf_w8_matmul, once, when they are loaded.  d_codes: int8
- * [N][K]; d_scales: float [N].  d_packed: mf_w8_pack_bytes, 256-byte aligned. */
+ * [N][K]; d_scales: float [N].  d_packed: mf_w8_pack_bytes, 256-byte aligned, not over the others (EINVAL). */
 mf_status mf_w8_pack(const mf_w8_desc *desc, const int8_t *d_codes, const float *d_scales, void *d_packed, size_t packed_bytes,
                      void *stream);
 
@@ -624,7 +625,7 @@ typedef struct {
     const void *d_x;        /* [rows][K], row stride x_stride >= K: codes, or values of dtype where d_x_scales is NULL */
     const float *d_x_scales;/* [rows] or NULL */
     const void *d_bias;     /* [N] or NULL */
-    void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x (EINVAL) */
+    void *d_y;              /* [rows][N], row stride y_stride >= N; not over anything that is read (EINVAL) */
     int64_t rows;           /* 0 (nothing is done) .. 2^20, times N at most 2^37 */
     int64_t x_stride, y_stride;
 } mf_w8_args;
@@ -632,7 +633,8 @@ typedef struct {
 /* Bytes of workspace (possibly 0), a function of the sizes and of whether x is in 8 bits. */
 mf_status mf_w8_workspace_size(const mf_w8_args *args, size_t *bytes);
 
-/* Any number of rows.  Deterministic.  d_ws: mf_w8_workspace_size bytes, 256-byte aligned; need not be initialised. */
+/* Any number of rows.  Deterministic.  d_ws: mf_w8_workspace_size bytes, 256-byte aligned, not over the operands (EINVAL);
+ * need not be initialised. */
 mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void *stream);
 
 /* --- the paged cache in 8 bits

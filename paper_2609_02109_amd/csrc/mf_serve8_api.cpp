@@ -9,17 +9,8 @@ namespace {
 // Row strides of `n` elements each that a call's rows may have.
 bool row_stride(int64_t rows, int64_t stride, int64_t n, bool out) { return strides_fit(rows, stride, 1, 0, n, out) && (rows <= 1 || stride >= n); }
 
-// Whether `rows` rows of x_row bytes from x on, x_step bytes apart, and of y have no byte together; ones that lie between one
-// another at different steps are taken to have.
-bool apart(int64_t rows, const void *x, int64_t x_step, int64_t x_row, const void *y, int64_t y_step, int64_t y_row)
-{
-    typedef __int128 wide;   // a row may begin 2^70 bytes behind the first
-    const wide x0 = (uintptr_t)x, y0 = (uintptr_t)y, x1 = x0 + (wide)(rows - 1) * x_step + x_row, y1 = y0 + (wide)(rows - 1) * y_step + y_row;
-    if (x1 <= y0 || y1 <= x0) return true;
-    if (rows == 1 || x_step != y_step || x_step == 0) return false;
-    const wide in = ((y0 - x0) % x_step + x_step) % x_step;   // of y's rows in the steps from x on
-    return in >= x_row && in + y_row <= x_step;
-}
+// Rows of n values of `size` bytes.
+Place rows_at(const void *p, int64_t rows, int64_t stride, int64_t n, int64_t size) { return place(p, n * size, rows, stride * size); }
 
 // What every call over rows has.
 mf_status check_rows8(const mf_rows8_args *r)
@@ -29,7 +20,14 @@ mf_status check_rows8(const mf_rows8_args *r)
     if (r->rows == 0) return MF_OK;
     if (!r->d_x || !r->d_codes || !r->d_scales || !aligned(r->d_x, 2) || !aligned(r->d_scales, 4)) return MF_EINVAL;
     if (!row_stride(r->rows, r->x_stride, r->n, false) || !row_stride(r->rows, r->codes_stride, r->n, true)) return MF_EINVAL;
-    return apart(r->rows, r->d_x, 2 * r->x_stride, 2 * r->n, r->d_codes, r->codes_stride, r->n) ? MF_OK : MF_EINVAL;
+    return MF_OK;
+}
+
+// Whether the codes and the scales lie over none of the row's x and what else a call reads and writes, nor over one another.
+bool rows8_apart(const mf_rows8_args &r, const Place &one = {}, const Place &two = {}, const Place &three = {})
+{
+    const Place x = rows_at(r.d_x, r.rows, r.x_stride, r.n, 2), codes = rows_at(r.d_codes, r.rows, r.codes_stride, r.n, 1), scales = place(r.d_scales, r.rows * 4);
+    return apart(codes, {scales, x, one, two, three}) && apart(scales, {x, one, two, three});
 }
 
 Rows8Args rows8_of(const mf_rows8_args &r)
@@ -99,6 +97,7 @@ mf_status mf_rows8(const mf_rows8_args *args, void *stream)
     if (!args) return MF_EINVAL;
     const mf_status st = check_rows8(args);
     if (st != MF_OK || args->rows == 0) return st;
+    if (!rows8_apart(*args)) return MF_EINVAL;
     return of(launch_rows8(rows8_of(*args), kRowsPlain, as_int(args->dtype) == MF_F16, (hipStream_t)stream));
 }
 
@@ -112,20 +111,24 @@ mf_status mf_norm8(const mf_norm8_args *args, void *stream)
     if (r.rows == 0) return MF_OK;
     if (!args->d_weight || !aligned(args->d_weight, 2)) return MF_EINVAL;
     Rows8Args a = rows8_of(r);
+    const Place weight = place(args->d_weight, 2 * r.n);
+    Place residual = {}, sum = {};
     if (args->d_residual) {
         if (!args->d_sum || !aligned(args->d_residual, 2) || !aligned(args->d_sum, 2)) return MF_EINVAL;
         if (!row_stride(r.rows, args->residual_stride, r.n, false) || !row_stride(r.rows, args->sum_stride, r.n, true)) return MF_EINVAL;
+        residual = rows_at(args->d_residual, r.rows, args->residual_stride, r.n, 2);
+        sum = rows_at(args->d_sum, r.rows, args->sum_stride, r.n, 2);
         // over a row itself, which has to lie as it does, or over none
         const auto itself_or_apart = [&](const void *x, int64_t stride) {
-            if (x == args->d_sum && (r.rows == 1 || stride == args->sum_stride)) return true;
-            return apart(r.rows, x, 2 * stride, 2 * r.n, args->d_sum, 2 * args->sum_stride, 2 * r.n);
+            return (x == args->d_sum && (r.rows == 1 || stride == args->sum_stride)) || apart(sum, rows_at(x, r.rows, stride, r.n, 2));
         };
-        if (!itself_or_apart(r.d_x, r.x_stride) || !itself_or_apart(args->d_residual, args->residual_stride)) return MF_EINVAL;
+        if (!itself_or_apart(r.d_x, r.x_stride) || !itself_or_apart(args->d_residual, args->residual_stride) || !apart(sum, weight)) return MF_EINVAL;
         a.y = args->d_residual;
         a.sum = args->d_sum;
         a.y_stride = args->residual_stride;
         a.sum_stride = args->sum_stride;
     }
+    if (!rows8_apart(r, residual, sum, weight)) return MF_EINVAL;
     a.weight = args->d_weight;
     a.eps = args->eps;
     return of(launch_rows8(a, kRowsNorm, as_int(r.dtype) == MF_F16, (hipStream_t)stream));
@@ -138,6 +141,7 @@ mf_status mf_gate8(const mf_gate8_args *args, void *stream)
     const mf_status st = check_rows8(&r);
     if (st != MF_OK || r.rows == 0) return st;
     if (!args->d_up || !aligned(args->d_up, 2) || !row_stride(r.rows, args->up_stride, r.n, false)) return MF_EINVAL;
+    if (!rows8_apart(r, rows_at(args->d_up, r.rows, args->up_stride, r.n, 2))) return MF_EINVAL;
     Rows8Args a = rows8_of(r);
     a.y = args->d_up;
     a.y_stride = args->up_stride;
@@ -153,6 +157,7 @@ mf_status mf_rows8_values(mf_dtype dtype, int64_t rows, int64_t n, const int8_t 
     if (rows == 0) return MF_OK;
     if (!d_codes || !d_scales || !d_out || !aligned(d_scales, 4) || !aligned(d_out, ty == MF_F32 ? 4 : 2)) return MF_EINVAL;
     if (!row_stride(rows, codes_stride, n, false) || !row_stride(rows, out_stride, n, true)) return MF_EINVAL;
+    if (!apart(rows_at(d_out, rows, out_stride, n, ty == MF_F32 ? 4 : 2), {rows_at(d_codes, rows, codes_stride, n, 1), place(d_scales, rows * 4)})) return MF_EINVAL;
     Values8Args a;
     a.codes = d_codes;
     a.scales = d_scales;
@@ -178,6 +183,7 @@ mf_status mf_w8_pack(const mf_w8_desc *desc, const int8_t *d_codes, const float 
     if (st != MF_OK) return st;
     if (!d_codes || !d_scales || !d_packed || !aligned(d_scales, 4) || !aligned(d_packed, 256)) return MF_EINVAL;
     if (packed_bytes < w8_bytes(*desc)) return MF_ENOMEM;
+    if (!apart(place(d_packed, (int64_t)w8_bytes(*desc)), {place(d_codes, desc->n_out * desc->n_in), place(d_scales, desc->n_out * 4)})) return MF_EINVAL;
     W8PackArgs a;
     a.codes = d_codes;
     a.scales = d_scales;
@@ -207,10 +213,12 @@ mf_status mf_w8_matmul(const mf_w8_args *args, void *d_ws, size_t ws_bytes, void
         return MF_EINVAL;
     if (!row_stride(args->rows, args->x_stride, w.n_in, false) || !row_stride(args->rows, args->y_stride, w.n_out, true)) return MF_EINVAL;
     const int64_t size = args->d_x_scales ? 1 : 2;
-    if (!apart(args->rows, args->d_x, size * args->x_stride, size * w.n_in, args->d_y, 2 * args->y_stride, 2 * w.n_out)) return MF_EINVAL;
+    const Place x = rows_at(args->d_x, args->rows, args->x_stride, w.n_in, size), y = rows_at(args->d_y, args->rows, args->y_stride, w.n_out, 2);
+    const Place scales = place(args->d_x_scales, args->rows * 4), bias = place(args->d_bias, w.n_out * 2), packed = place(args->d_packed, (int64_t)w8_bytes(w));
+    if (!apart(y, {x, scales, bias, packed})) return MF_EINVAL;
     const size_t need = w8_ws(*args);
     if (need > 0 && (ws_bytes < need || !d_ws)) return MF_ENOMEM;
-    if (need > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
+    if (need > 0 && (!aligned(d_ws, 256) || !apart(place(d_ws, (int64_t)need), {x, bias, packed, y}))) return MF_EINVAL;
     W8Args a;
     a.packed = (const uint8_t *)args->d_packed;
     a.w_scales = (const float *)(a.packed + w8_records(w));
