@@ -495,7 +495,8 @@ typedef struct {
  * rot_dim / 2, (a, b) -> (a cos[p][t] - b sin[p][t], b cos[p][t] + a sin[p][t]),
  * the pair being dims (t, t + rot_dim / 2), or (2t, 2t + 1) when interleaved;
  * dims from rot_dim on stay.  With d_q the queries are turned the same way into
- * d_q_out (rounded once; may be d_q itself with the same strides). */
+ * d_q_out (rounded once; may be d_q itself with the same strides).  Neither d_q_out nor
+ * the pages are over anything else that the call reads or writes (EINVAL). */
 typedef struct {
     mf_dtype dtype;         /* MF_BF16 or MF_F16 */
     const void *d_k, *d_v;  /* [rows][n_kv_heads][D] */
@@ -514,7 +515,7 @@ mf_status mf_kv4_append(const mf_kv4_cache *cache, const mf_kv4_batch *batch, co
 
 /* The values that the cache holds for the rows of a batch (n_s = kv_len[s]:
  * whole sequences), rounded to dtype (MF_F32, MF_BF16 or MF_F16): d_k and d_v
- * [rows][n_kv_heads][D], contiguous; either may be NULL. */
+ * [rows][n_kv_heads][D], contiguous, not over one another, the pages or the batch (EINVAL); either may be NULL. */
 mf_status mf_kv4_read(const mf_kv4_cache *cache, const mf_kv4_batch *batch, mf_dtype dtype, void *d_k, void *d_v,
                       void *stream);
 
@@ -532,8 +533,8 @@ typedef struct {
     mf_dtype dtype;         /* MF_BF16 or MF_F16: of q and out */
     int32_t n_heads;        /* a multiple of n_kv_heads, at most 4096 */
     const void *d_q;        /* [rows][n_heads][D] */
-    void *d_out;            /* [rows][n_heads][D] */
-    float *d_lse;           /* [rows][n_heads] contiguous, or NULL */
+    void *d_out;            /* [rows][n_heads][D]; may be d_q itself with the same strides */
+    float *d_lse;           /* [rows][n_heads] contiguous, or NULL; outputs and workspace are over nothing else of the call's (EINVAL) */
     int64_t q_stride, q_head_stride, out_stride, out_head_stride;
     float scale;            /* finite, > 0 */
     int32_t window;         /* 0: every earlier token */

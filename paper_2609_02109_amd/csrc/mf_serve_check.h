@@ -122,6 +122,26 @@ inline mf_status check_batch(int page_size, const void *d_pages, const mf_kv4_ba
     return MF_OK;
 }
 
+// Where a step's rows of `heads` times D elements lie, a cache's pages, and what a batch has on the device.
+inline Place place_of_rows(const void *p, int64_t rows, int64_t stride, int64_t heads, int64_t head, int64_t d, int64_t size = 2)
+{
+    return place(p, d * size, rows, stride * size, heads, head * size);
+}
+inline Place place_of_pages(const KvGeom &g, const void *d_pages)
+{
+    return place(d_pages, (int64_t)g.n_pages * g.n_kv_heads * g.blocks_per_page * (g.rec + (g.group ? 0 : (int64_t)sizeof(KvScales))));
+}
+inline bool apart_from_batch(const Place &x, const mf_kv4_batch *b)
+{
+    const int64_t n = b->n_seq;
+    return apart(x, {place(b->d_q_start, (n + 1) * 4), place(b->d_kv_len, n * 4), place(b->table_cols > 0 ? b->d_page_table : nullptr, b->table_cols * 4ll, n, b->table_stride * 4)});
+}
+// Whether rows of results lie over their source itself: each element is read by those who write it, and before that.
+inline bool itself(const void *in, int64_t stride, int64_t head, const void *out, int64_t out_stride, int64_t out_head, int64_t rows, int64_t heads)
+{
+    return in == out && (rows <= 1 || stride == out_stride) && (heads <= 1 || head == out_head);
+}
+
 // The arguments of an append to a cache of geometry a.g; none: there is nothing to do.
 inline mf_status check_append(const void *d_pages, const mf_kv4_batch *batch, const mf_kv4_append_args *args, KvAppendArgs &a, bool &none)
 {
@@ -148,6 +168,18 @@ inline mf_status check_append(const void *d_pages, const mf_kv4_batch *batch, co
     if (args->d_q && (!strides_fit(rows, args->q_stride, args->n_heads, args->q_head_stride, d, false) ||
                       !strides_fit(rows, args->qo_stride, args->n_heads, args->qo_head_stride, d, true)))
         return MF_EINVAL;
+    const Place pages = place_of_pages(a.g, d_pages), k = place_of_rows(args->d_k, rows, args->k_stride, a.g.n_kv_heads, args->k_head_stride, d),
+                v = place_of_rows(args->d_v, rows, args->v_stride, a.g.n_kv_heads, args->v_head_stride, d);
+    const int64_t angles = args->d_cos ? (int64_t)args->n_pos * (args->rot_dim / 2) * 4 : 0;
+    const Place cos = place(args->d_cos, angles), sin = place(args->d_sin, angles);
+    if (!apart(pages, {k, v, cos, sin}) || !apart_from_batch(pages, batch)) return MF_EINVAL;
+    if (args->d_q) {
+        const Place q = place_of_rows(args->d_q, rows, args->q_stride, args->n_heads, args->q_head_stride, d),
+                    out = place_of_rows(args->d_q_out, rows, args->qo_stride, args->n_heads, args->qo_head_stride, d);
+        if (!apart(out, {pages, k, v, cos, sin}) || !apart_from_batch(out, batch) || !apart(pages, q)) return MF_EINVAL;
+        if (!itself(args->d_q, args->q_stride, args->q_head_stride, args->d_q_out, args->qo_stride, args->qo_head_stride, rows, args->n_heads) && !apart(out, q))
+            return MF_EINVAL;
+    }
     a.k = args->d_k;
     a.v = args->d_v;
     a.q = args->d_q;
@@ -176,6 +208,12 @@ inline mf_status check_read(const void *d_pages, const mf_kv4_batch *batch, int 
     const size_t el = ty == MF_F32 ? 4 : 2;
     if (!aligned(d_k, el) || !aligned(d_v, el)) return MF_EINVAL;
     none = batch->rows == 0 || batch->n_seq == 0 || batch->max_new == 0 || (!d_k && !d_v);
+    if (none) return MF_OK;
+    const int64_t bytes = batch->rows * a.g.n_kv_heads * a.g.head_dim * (int64_t)el;
+    const Place k = place(d_k, bytes), v = place(d_v, bytes), pages = place_of_pages(a.g, d_pages);
+    if (!apart(k, {v, pages}) || !apart(v, {pages})) return MF_EINVAL;
+    for (const Place &x : {k, v})
+        if (x.at != 0 && !apart_from_batch(x, batch)) return MF_EINVAL;
     a.k = d_k;
     a.v = d_v;
     return MF_OK;
@@ -224,8 +262,15 @@ inline mf_status check_attn_run(const mf_kv4_batch *batch, const mf_kv4_attn_arg
     if (!strides_fit(batch->rows, args->q_stride, args->n_heads, args->q_head_stride, d, false) ||
         !strides_fit(batch->rows, args->out_stride, args->n_heads, args->out_head_stride, d, true))
         return MF_EINVAL;
+    const Place q = place_of_rows(args->d_q, batch->rows, args->q_stride, args->n_heads, args->q_head_stride, d),
+                out = place_of_rows(args->d_out, batch->rows, args->out_stride, args->n_heads, args->out_head_stride, d),
+                lse = place(args->d_lse, batch->rows * args->n_heads * 4), pages = place_of_pages(a.g, a.g.pages);
+    if (!itself(args->d_q, args->q_stride, args->q_head_stride, args->d_out, args->out_stride, args->out_head_stride, batch->rows, args->n_heads) && !apart(out, q))
+        return MF_EINVAL;
+    if (!apart(out, {pages, lse}) || !apart(lse, {pages, q})) return MF_EINVAL;
     if (ws_bytes < p.ws_bytes || (p.ws_bytes > 0 && !d_ws)) return MF_ENOMEM;
-    if (p.ws_bytes > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
+    if (p.ws_bytes > 0 && (!aligned(d_ws, 256) || !apart(place(d_ws, (int64_t)p.ws_bytes), {q, out, lse, pages}))) return MF_EINVAL;
+    if (!apart_from_batch(out, batch) || (args->d_lse && !apart_from_batch(lse, batch))) return MF_EINVAL;
     a.q = args->d_q;
     a.out = args->d_out;
     a.lse = args->d_lse;

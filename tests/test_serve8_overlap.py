@@ -87,3 +87,72 @@ def test_weights_laid_out_over_themselves():
     d = serve.W8Desc(16, 128, BF)   # 2048 bytes of codes and 64 of scales, as laid out too
     for codes, scales, packed in ((X, Y, X), (X + 2048, Y, X), (X, Y, X + 1792), (X, Y + 2108, Y), (X, Y, Y)):
         assert mf.lib.mf_w8_pack(C.byref(d), codes, scales, packed, C.c_size_t(2112), None) == mf.MF_EINVAL
+
+
+# ------------------------------------------------------------------ the caches
+
+PAGES, STARTS, LENS, TABLE, COS, SIN = 16 << 20, 32 << 20, 33 << 20, 34 << 20, 35 << 20, 36 << 20
+CACHES = [(mf.lib.mf_kv4_append, mf.lib.mf_kv4_read, mf.lib.mf_kv4_attention, lambda: serve.Cache(4, 16, 2, 64, 64, PAGES), 4 * 2 * (16 * 64 + 128)),
+          (mf.lib.mf_kv8_append, mf.lib.mf_kv8_read, mf.lib.mf_kv8_attention, lambda: serve.Cache8(4, 16, 2, 64, PAGES), 4 * 2 * (32 * 64 + 8))]
+kinds = pytest.mark.parametrize("kind", [0, 1], ids=["4-bit", "8-bit"])
+
+
+def _batch(rows=3, n=1, cols=4, kv=20):
+    return serve.Batch(n, rows, kv, rows, STARTS, LENS, TABLE, cols, cols)
+
+
+def _append(kind, rows=3, k=X, ks=(128, 64), v=Y, vs=(128, 64), q=Z, qs=(256, 64), out=CODES, os=(256, 64), heads=4):
+    call, _, _, cache, _ = CACHES[kind]
+    a = serve.AppendArgs(BF, k, v, *ks, *vs, COS, SIN, 64, 64, 0, heads, q, out, *qs, *os)
+    return call(C.byref(cache()), C.byref(_batch(rows)), C.byref(a), None)
+
+
+@kinds
+@pytest.mark.parametrize("kw", [
+    dict(out=X), dict(out=Y), dict(out=X - 1534), dict(out=Y + 766), dict(out=COS + 2), dict(out=SIN), dict(out=COS + 20 * 32 * 4 - 2), dict(out=PAGES),
+    dict(out=STARTS), dict(out=LENS), dict(out=TABLE), dict(out=Z + 2), dict(out=Z + 512), dict(out=Z, os=(512, 64)), dict(out=Z, os=(64, 192)),
+    # one buffer of columns, 4 heads of q, 2 of k, 2 of v: the output over some of k's
+    dict(q=Z, qs=(512, 64), k=Z + 512, ks=(512, 64), v=Z + 768, vs=(512, 64), out=Z + 128, os=(512, 64)),
+    # the pages over what is read
+    dict(k=PAGES), dict(v=PAGES + 64), dict(q=PAGES), dict(k=PAGES - 2)])
+def test_append_over_what_it_reads(kind, kw):
+    assert _append(kind, **kw) == mf.MF_EINVAL
+
+
+def _attn(kind, rows=3, q=X, qs=(256, 64), out=Y, os=(256, 64), lse=None, heads=4, ws=None, room=0, kv=20, cols=4):
+    _, _, call, cache, _ = CACHES[kind]
+    a = serve.AttnArgs(BF, heads, q, out, lse, *qs, *os, 0.125, 0)
+    return call(C.byref(cache()), C.byref(_batch(rows, cols=cols, kv=kv)), C.byref(a), ws, room, None)
+
+
+@kinds
+def test_attention_over_what_it_reads(kind):
+    size = CACHES[kind][4]
+    for kw in (dict(out=X + 2), dict(out=X + 512), dict(out=X - 1534), dict(out=X, os=(512, 64)), dict(out=X, os=(64, 192)), dict(out=PAGES), dict(out=PAGES + size - 2),
+               dict(out=STARTS), dict(out=LENS + 2), dict(out=TABLE + 14), dict(lse=X), dict(lse=Y + 1532), dict(lse=PAGES), dict(lse=TABLE), dict(q=PAGES, out=PAGES)):
+        assert _attn(kind, **kw) == mf.MF_EINVAL, kw
+
+
+@kinds
+def test_attention_beside_what_it_reads(kind):
+    """These pass, and are stopped by a workspace that is not there."""
+    size, long = CACHES[kind][4], dict(kv=60000, cols=4000, rows=1)
+    for kw in (dict(), dict(out=X), dict(out=X, os=(777, 64)), dict(out=X + 512), dict(out=PAGES + size), dict(out=PAGES - 512), dict(lse=X + 512), dict(lse=Y + 512),
+               dict(qs=(256, 192), out=X + 128, os=(256, 192)), dict(qs=(256, 192), out=X + 256, os=(256, 192)), dict(out=LENS + 4)):
+        assert _attn(kind, **long, **kw) == mf.MF_ENOMEM, kw
+    three = dict(kv=60000, cols=4000, rows=3)
+    # rows inside heads, and columns of one buffer
+    for kw in (dict(qs=(64, 192), os=(64, 192)), dict(qs=(512, 64), out=X + 512, os=(512, 64)), dict(out=X, os=(256, 64)), dict(qs=(768, 192), out=X + 128, os=(768, 192))):
+        assert _attn(kind, **three, **kw) == mf.MF_ENOMEM, kw
+    assert _attn(kind, **long, ws=X, room=1 << 30) == mf.MF_EINVAL
+    assert _attn(kind, **long, ws=Y - 256, room=1 << 30) == mf.MF_EINVAL
+
+
+@kinds
+def test_read_over_what_it_reads(kind):
+    _, call, _, cache, size = CACHES[kind]
+    c, b = cache(), _batch()
+    for ty, el in ((mf.MF_F32, 4), (BF, 2)):
+        most = 3 * 2 * 64 * el
+        for k, v in ((PAGES, X), (X, PAGES + size - 4), (X, PAGES - most + 4), (STARTS, X), (X, LENS), (TABLE + 12, None), (X, X), (X, X + most - 4), (X + most - 4, X)):
+            assert call(C.byref(c), C.byref(b), ty, k, v, None) == mf.MF_EINVAL
