@@ -41,20 +41,25 @@ inline bool strides_fit(int64_t rows, int64_t stride, int64_t heads, int64_t hea
 // Pieces of len bytes in up to two levels of steps, the larger one first; at 0: none.
 struct Place {
     typedef __int128 wide;   // a piece may begin 2^70 bytes behind the first
-    wide at;
+    wide at, end;
     int64_t len, n[2], step[2];
     int levels;
-    wide extent() const { return len + (levels > 0 ? wide(n[0] - 1) * step[0] : 0) + (levels > 1 ? wide(n[1] - 1) * step[1] : 0); }
     // Piece i of the first level.
-    Place piece(wide i) const { return {at + i * step[0], len, {n[1], 0}, {step[1], 0}, levels - 1}; }
+    Place piece(wide i) const
+    {
+        const wide from = at + i * step[0];
+        return {from, from + len + (levels > 1 ? wide(n[1] - 1) * step[1] : 0), len, {n[1], 0}, {step[1], 0}, levels - 1};
+    }
 };
 inline Place place(const void *p, int64_t len, int64_t n = 1, int64_t step = 0, int64_t n2 = 1, int64_t step2 = 0)
 {
-    Place r = {(Place::wide)(uintptr_t)p, len, {0, 0}, {0, 0}, 0};
+    const Place::wide at = (Place::wide)(uintptr_t)p;
+    Place r = {at, at + len, len, {0, 0}, {0, 0}, 0};
     const bool swap = step2 > step;
     for (int i = 0; i < 2; i++) {
         const int64_t many = (i == 0) == swap ? n2 : n, by = (i == 0) == swap ? step2 : step;
         if (many <= 1 || by == 0) continue;   // the same bytes again
+        r.end += (Place::wide)(many - 1) * by;
         r.n[r.levels] = many;
         r.step[r.levels++] = by;
     }
@@ -67,16 +72,15 @@ inline Place::wide floor_of(Place::wide a, int64_t b) { return a >= 0 ? a / b : 
 inline bool apart(const Place &x, const Place &y)
 {
     typedef Place::wide wide;
-    const wide ex = x.extent(), ey = y.extent();
-    if (x.at + ex <= y.at || y.at + ey <= x.at) return true;
+    if (x.end <= y.at || y.end <= x.at) return true;
     if (x.levels == 0 && y.levels == 0) return false;
     const auto most = [](wide p, wide q) { return p > q ? p : q; };
     if (x.levels > 0 && y.levels > 0 && x.step[0] == y.step[0]) {
         // piece i of x and j of y meet or not by j - i alone
         const int64_t step = x.step[0];
         const Place p = x.piece(0), q = y.piece(0);
-        const wide lo = most(floor_of(p.at - q.extent() - q.at, step) + 1, -wide(x.n[0] - 1));
-        const wide hi = -most(floor_of(q.at - p.extent() - p.at, step) + 1, -wide(y.n[0] - 1));
+        const wide lo = most(floor_of(p.at - q.end, step) + 1, -wide(x.n[0] - 1));
+        const wide hi = -most(floor_of(q.at - p.end, step) + 1, -wide(y.n[0] - 1));
         if (hi - lo >= 16) return false;
         for (wide d = lo; d <= hi; d++)
             if (!apart(p, y.piece(d))) return false;
@@ -84,8 +88,8 @@ inline bool apart(const Place &x, const Place &y)
     }
     const bool of_x = y.levels == 0 || (x.levels > 0 && x.step[0] > y.step[0]);
     const Place &a = of_x ? x : y, &b = of_x ? y : x, first = a.piece(0);
-    const wide lo = most(floor_of(b.at - first.extent() - a.at, a.step[0]) + 1, 0);
-    const wide hi = -most(floor_of(a.at - b.extent() - b.at, a.step[0]) + 1, -wide(a.n[0] - 1));
+    const wide lo = most(floor_of(b.at - first.end, a.step[0]) + 1, 0);
+    const wide hi = -most(floor_of(a.at - b.end, a.step[0]) + 1, -wide(a.n[0] - 1));
     if (hi - lo >= 16) return false;
     for (wide i = lo; i <= hi; i++)
         if (!apart(a.piece(i), b)) return false;
