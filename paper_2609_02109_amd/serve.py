@@ -14,7 +14,8 @@ As in `mf`, this is marshalling only: torch supplies device memory and the
 stream, the kernels of libmf.so do the work.  Calls enqueue on `stream` (None:
 torch's current one), copies of what is not contiguous too, and do not
 synchronise; include/mf.h has the definitions.  They are for inference: an
-operand that requires a gradient is refused while gradients are recorded.
+operand that requires a gradient is refused while gradients are recorded, and so is
+one with a tangent of forward mode.
 """
 from __future__ import annotations
 
@@ -24,6 +25,7 @@ import threading
 from typing import NamedTuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import mf
 from .mf import _check, _ptr
@@ -162,10 +164,13 @@ def _int32(x, name):
     return x
 
 
-def _no_gradient():
-    """For an operand that requires a gradient: the operators have no backward, and a result without one would lose it silently."""
-    if torch.is_grad_enabled():
+def _no_gradient(t):
+    """For a t that requires a gradient, or any where tangents may be (a call looks at no more than these two): the operators have
+    no backward and no forward mode, and a result without either would lose t's gradient or tangent silently."""
+    if t.requires_grad and torch.is_grad_enabled():
         raise ValueError("an operand requires a gradient, and there is none through this call: torch.no_grad() or detach() is wanted")
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError("an operand has a tangent, and there is none through this call: detach() is wanted")
 
 
 def _rows(t, name, shape, dtype, device):
@@ -184,8 +189,8 @@ def _into(t, name, shape, dtype, device):
     """An output of the caller's."""
     _require(isinstance(t, torch.Tensor) and tuple(t.shape) == tuple(shape) and t.dtype is dtype and t.device == device
              and (t.stride(-1) == 1 or t.shape[-1] <= 1), f"{name}: {tuple(shape)} {dtype} on {device} with a contiguous last dimension is wanted")
-    if t.requires_grad:
-        _no_gradient()
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _no_gradient(t)
     return t
 
 
@@ -204,6 +209,8 @@ class W4Weight:
                  and scales.shape[0] == codes.shape[0] and scales.device == codes.device and scales.shape[1] > 0
                  and (2 * codes.shape[1]) % scales.shape[1] == 0,
                  "scales: bfloat16 or float16 [N, K // G] beside the codes is wanted")
+        if scales.requires_grad or forward_ad._current_level >= 0:
+            _no_gradient(scales)
         _require(zeros is None or (isinstance(zeros, torch.Tensor) and zeros.dtype is torch.uint8
                                    and zeros.shape == scales.shape and zeros.device == codes.device),
                  "zeros: uint8 of the scales' shape is wanted")
@@ -236,10 +243,10 @@ class W4Weight:
         if bias is not None:
             _require(bias.dtype is self.dtype and bias.device == self.device and tuple(bias.shape) == (self.n_out,)
                      and bias.is_contiguous(), f"bias: contiguous [{self.n_out}] {self.dtype} is wanted")
-            if bias.requires_grad:
-                _no_gradient()
-        if x.requires_grad:
-            _no_gradient()
+            if bias.requires_grad or forward_ad._current_level >= 0:
+                _no_gradient(bias)
+        if x.requires_grad or forward_ad._current_level >= 0:
+            _no_gradient(x)
         if len(lead) != 1:
             x = x.reshape(-1, self.n_in)
         m = x.shape[0]
@@ -269,8 +276,8 @@ def _matrix(t, name, n, dtype, device):
     """[.., n] as rows of n with a contiguous last dimension (a copy where they are none)."""
     if not isinstance(t, torch.Tensor) or t.dim() == 0 or t.shape[-1] != n or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name}: [.., {n}] {dtype} on {device} is wanted")
-    if t.requires_grad:
-        _no_gradient()
+    if t.requires_grad or forward_ad._current_level >= 0:
+        _no_gradient(t)
     if t.dim() != 2:
         t = t.reshape(-1, n)
     if t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < n):
@@ -293,8 +300,8 @@ class Rows8(NamedTuple):
         if (not isinstance(scales, torch.Tensor) or scales.dtype is not torch.float32 or scales.device != codes.device
                 or scales.shape != codes.shape[:-1]):
             raise ValueError("scales: float32 [..] beside the codes is wanted")
-        if scales.requires_grad:
-            _no_gradient()
+        if scales.requires_grad or forward_ad._current_level >= 0:
+            _no_gradient(scales)
         if codes.dim() != 2 or not codes.is_contiguous():
             codes = _matrix(codes, "codes", codes.shape[-1], torch.int8, codes.device)
         return codes, scales if scales.is_contiguous() else scales.contiguous()
@@ -320,7 +327,7 @@ def _rows8_of(x, name):
         raise ValueError(f"{name}: bfloat16 or float16 [.., N] on the GPU is wanted")
     shape, dt = x.shape, x.dtype
     n = shape[-1]
-    if len(shape) == 2 and x.is_contiguous() and not x.requires_grad:
+    if len(shape) == 2 and x.is_contiguous() and not (x.requires_grad or forward_ad._current_level >= 0):
         m, codes, rows, stride = x, torch.empty_like(x, dtype=torch.int8), shape[0], n
     else:
         m, codes = _matrix(x, name, n, dt, x.device), x.new_empty(shape, dtype=torch.int8)
@@ -357,8 +364,8 @@ def norm_rows(x, weight, residual=None, eps=1e-6, out=None, stream=None):
     n, dt, dev = a.n, x.dtype, x.device
     if not isinstance(weight, torch.Tensor) or weight.shape != (n,) or weight.dtype is not dt or weight.device != dev:
         raise ValueError(f"weight: [{n}] {dt} on {dev} is wanted")
-    if weight.requires_grad:
-        _no_gradient()
+    if weight.requires_grad or forward_ad._current_level >= 0:
+        _no_gradient(weight)
     if not weight.is_contiguous():
         weight = weight.contiguous()
     if residual is None:
@@ -406,8 +413,8 @@ class W8Weight:
                  "codes: an int8 [N, K] tensor on the GPU is wanted")
         _require(isinstance(scales, torch.Tensor) and scales.dtype is torch.float32 and scales.dim() == 1
                  and scales.shape[0] == codes.shape[0] and scales.device == codes.device, "scales: float32 [N] beside the codes is wanted")
-        if scales.requires_grad:
-            _no_gradient()
+        if scales.requires_grad or forward_ad._current_level >= 0:
+            _no_gradient(scales)
         _require(dtype in _HALF, "dtype: bfloat16 or float16 is wanted")
         self.n_out, self.n_in, self.dtype, self.device = int(codes.shape[0]), int(codes.shape[1]), dtype, codes.device
         self.desc = W8Desc(self.n_out, self.n_in, _DTYPES[dtype])
@@ -446,8 +453,8 @@ class W8Weight:
         if bias is not None:
             _require(bias.dtype is dt and bias.device == dev and tuple(bias.shape) == (n,) and bias.is_contiguous(),
                      f"bias: contiguous [{n}] {dt} on {dev} is wanted")
-            if bias.requires_grad:
-                _no_gradient()
+            if bias.requires_grad or forward_ad._current_level >= 0:
+                _no_gradient(bias)
         m = x.shape[0]
         if out is None:
             y = x.new_empty((m, n), dtype=dt)
@@ -537,8 +544,9 @@ class _KVCache:
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (k, v, cos, sin, q, q_out, self.pages, batch.tensors),
                        lambda: self.append(batch, k, v, cos, sin, q, interleaved, q_out))
-        if k.requires_grad or v.requires_grad:
-            _no_gradient()
+        if k.requires_grad or v.requires_grad or forward_ad._current_level >= 0:
+            _no_gradient(k)
+            _no_gradient(v)
         dt, dev = k.dtype, self.device
         _require(dt in _HALF, "k: bfloat16 or float16 is wanted")
         shape = (batch.rows, self.n_kv_heads, self.head_dim)
@@ -553,14 +561,17 @@ class _KVCache:
             n_pos, half = cos.shape
             _require(cos.shape == sin.shape and cos.dtype is sin.dtype is torch.float32 and cos.device == sin.device == dev
                      and cos.is_contiguous() and sin.is_contiguous(), f"cos, sin: contiguous float32 [n_pos, rot_dim // 2] on {dev} is wanted")
+            if cos.requires_grad or sin.requires_grad or forward_ad._current_level >= 0:
+                _no_gradient(cos)
+                _no_gradient(sin)
             turn = (cos.data_ptr(), sin.data_ptr(), n_pos, 2 * half, 1 if interleaved else 0)
             if q is None:
                 a = AppendArgs(_DTYPES[dt], k.data_ptr(), v.data_ptr(), ks[0], ks[1], vs[0], vs[1], *turn)
             else:
                 _require(q.dim() == 3, "q: [rows, n_heads, head_dim] is wanted")
                 heads = q.shape[1]
-                if q.requires_grad:
-                    _no_gradient()
+                if q.requires_grad or forward_ad._current_level >= 0:
+                    _no_gradient(q)
                 q = _rows(q, "q", (batch.rows, heads, self.head_dim), dt, dev)
                 q_out = _like(q) if q_out is None else _into(q_out, "q_out", q.shape, dt, dev)
                 qs, os = q.stride(), q_out.stride()
@@ -596,8 +607,8 @@ class _KVCache:
         if stream is not None or self.device.index != _current_device():
             return _on(self.device, stream, (q, out, self.pages, batch.tensors), lambda: self.attention(batch, q, scale, window, lse, out))
         _require(q.dim() == 3 and q.dtype in _HALF, "q: bfloat16 or float16 [rows, n_heads, head_dim] is wanted")
-        if q.requires_grad:
-            _no_gradient()
+        if q.requires_grad or forward_ad._current_level >= 0:
+            _no_gradient(q)
         heads = q.shape[1]
         q = _rows(q, "q", (batch.rows, heads, self.head_dim), q.dtype, self.device)
         out = _like(q) if out is None else _into(out, "out", q.shape, q.dtype, self.device)
