@@ -167,7 +167,8 @@ __device__ __forceinline__ void attn8_step(const f32x4 (&sc)[S][RT][2], const Si
             for (int d = 0; d < D / 16; d++) o[t][d] *= a;
         }
         far = __any(any);
-        weigh(std::true_type());
+        if (far) weigh(std::true_type());
+        else weigh(std::false_type());
     }
 #pragma unroll
     for (int k = 0; k < S; k++)
