@@ -492,8 +492,8 @@ __device__ __forceinline__ void attn_item(const KvAttnArgs &a, int s, int h, con
 }
 
 // By rows (many query tokens; bound by vector instructions, 68 % of the SIMDs' cycles
-// beside 34 % of matrix ones: 2 x 1024 query tokens of 32 heads over 12345 tokens take 545 us,
-// 721 TFLOP/s; a third tile of rows a wave would share the codes' work further and has no
+// beside 34 % of matrix ones: 2 x 1024 query tokens of 32 heads over 12345 tokens take 554 us,
+// 709 TFLOP/s; a third tile of rows a wave would share the codes' work further and has no
 // registers): a workgroup takes a tile of attn_rows rows, its
 // waves 16 RT of them each, over a part of their tokens.
 template <bool F16, int D, int G, int RT>

@@ -381,9 +381,9 @@ __device__ __forceinline__ void attn8_item(const KvAttnArgs &a, int s, int h, co
 // By rows (many query tokens): a workgroup takes a tile of attn_rows rows, its waves 16 RT of them each, over a part of
 // their tokens.  The waves go over the same tokens: each makes a quarter of a step's operands and leaves
 // them in LDS for all, for the step after the one that is computed.  Bound by issue: of the SIMDs' cycles vector
-// instructions take 46 % (a weight's factor, power of two, sum, rounding and check) and matrix instructions 33 %, with two
+// instructions take 46 % (a weight's factor, power of two, sum, rounding and check) and matrix instructions 32 %, with two
 // waves a SIMD by registers to put one over the other (2 x 1000 to 1024 query tokens over 8000 to 12000, 32 heads over 8 of
-// 128: 413 us, 850 TFLOP/s).
+// 128: 430 us, 814 TFLOP/s).
 template <bool F16, int D, int RT>
 __global__ __launch_bounds__(kAttnWaves * 64, 2) void attn8_rows_kernel(KvAttnArgs a)
 {

@@ -10,8 +10,10 @@ hipError_t launch_attn8_d256(const KvAttnArgs &a, const KvPlan &p, bool f16, hip
 
 // By rows: tiles of 64 rt rows, each over `splits` parts of its tokens.  As many parts as leave all workgroups on the card at
 // once (two a compute unit; of heads of 64 four), of about eight steps of 32 tokens at the least; a half of that and so on where it
-// takes less: parts are written and read (9 x 213 query tokens over 466, 8 over 2 heads of 256: two parts 35 us, one 25).
-// us: about what that takes.
+// takes less: parts are written and read (9 x 213 query tokens over 466, 8 over 2 heads of 256: two parts 34 us, one 25).
+// us: about what that takes, by figures of heads of 128 that were set by hand beside those below; heads of 64 and of 256 go by them
+// too, though a step of theirs has half the work and twice.  Every sequence counts as one of max_new tokens: one long piece of
+// a prompt beside decodes leaves no parts (512 over 20000 beside three of one token: 698 us, apart 205 and 30).
 struct RowsPlan {
     long long row_tiles, items, splits;
     float us;
@@ -55,8 +57,8 @@ KvPlan kv8_plan(const KvGeom &g, const KvBatch &b, int n_heads, int window)
     p.waves = kAttnWaves;
     if (p.rows_by_wave) {
         // Of heads of 128 a wave takes one tile of 16 rows or two, which share operands (us, one and two, in the best number of parts; 32
-        // over 8 heads): 1 x 16 query tokens over 4000: 18, 21; 1 x 300 over 3000: 46, 48; 4 x 64 over 3000: 41, 43; 1 x 1000 over 1000: 37, 47;
-        // 4 x 100 over 3000: 61, 57; 1 x 512 over 8000: 127, 112; 2 x 1500 over 3000: 236, 217; 2 x 1024 over 11000: 590, 440.  Of heads of 64
+        // over 8 heads): 1 x 16 query tokens over 4000: 17, 21; 1 x 300 over 3000: 45, 46; 4 x 64 over 3000: 38, 41; 1 x 1000 over 1000: 34, 40;
+        // 4 x 100 over 3000: 55, 53; 1 x 512 over 8000: 121, 100; 2 x 1500 over 3000: 189, 193; 2 x 1024 over 11000: 473, 396.  Of heads of 64
         // one (16 heads, 2 x 500 over 2000: 34, 37; 2 x 1024 over 12000: 190, 197), of heads of 256 two have no room.
         RowsPlan r = rows_plan(1, rows, heads, g.head_dim, span, b.max_new);
         p.rt = 1;

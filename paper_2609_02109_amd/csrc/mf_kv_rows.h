@@ -140,7 +140,7 @@ __device__ __forceinline__ void turn_queries(const KvAppendArgs &a, const Span &
                 continue;
             }
             // the result may be over its source, so that no load goes ahead of a store by itself: four heads are fetched, then turned
-            // (4 x 8192 rows of 32 heads of 128 beside 8: 146 us, one by one 167; 2 x 1024 of 16 heads of 256: 25 and 45)
+            // (4 x 8192 rows of 32 heads of 128 beside 8: 146 us, one by one 167; 2 x 1024 of 16 heads of 256 beside 16: 33 and 46)
             for (int h = h0; h < h1; h += 4) {
                 u32x4 raw[4][2];
 #pragma unroll

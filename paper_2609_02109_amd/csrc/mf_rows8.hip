@@ -5,9 +5,10 @@
 // A row belongs to T threads, which hold it in registers as fp32 (8 V values each)
 // between the sum of squares, the largest value and the codes: what comes from
 // memory comes once.  Bound by the bytes from some hundred rows on (8192 rows of
-// 8192, norm with a residual: 85 us for 470 MB, 5.5 TB/s; 4500 of 10240, gate:
-// 37 us for 230 MB, 6.2 TB/s; what they stand for: 34 us for 201 MB), below that by the trip to memory
-// and the waves' meetings (one row of 4096: 2.9 us).
+// 8192, norm with a residual: 87 us for 470 MB, 5.4 TB/s; 4500 of 10240, gate:
+// 42 to 44 us for 230 MB, 5.2 to 5.5 TB/s, and 37 where the 256 MB cache has them from the call before; what
+// they stand for, 8192 of 8192: 36 us for 201 MB), below that by the trip to memory and the waves' meetings (one row of
+// 4096: 2.9 us).
 #include "mf_serve_dev.h"
 
 namespace mfs {
@@ -40,7 +41,7 @@ __device__ __forceinline__ void widen8(u32x4 raw, float *v)
     for (int j = 0; j < 8; j++) v[j] = to_float<F16>((uint16_t)(raw[j >> 1] >> (16 * (j & 1))));
 }
 
-// g sigmoid(g) u, within (4 + |g|) 2^-24 of itself: far below half a code.  Below -88 the quotient's end is reached, 0.
+// g sigmoid(g) u, within (4 + 1.3 |g|) 2^-24 of itself: far below half a code.  Below -88 the quotient's end is reached, 0.
 __device__ __forceinline__ float gated(float g, float u)
 {
     return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)) * u;
@@ -257,9 +258,11 @@ hipError_t go(const Rows8Args &a, hipStream_t s)
 }
 
 // As many threads to a row as leave each one or two pieces of eight, whether rows are few or many (us, norm with a residual and
-// gate; T threads of V pieces): 1 x 4096: 512 of one 2.9 and 2.5, 256 of two 3.4 and 2.9; 8192 x 4096: 36.5 and 26.2, 38.3 and 26.5;
+// gate, the same rows again, of which the caches have a part; T threads of V pieces): 1 x 4096: 512 of one 2.9 and 2.5, 256 of two 3.4 and 2.9; 8192 x 4096: 36.5 and 26.2, 38.3 and 26.5;
 // 8192 x 8192: 512 of two 85 and 61, 256 of four 94 and 62, 1024 of one 86 and 63; 4500 x 10240: 1024 of two 82 and 37,
 // 256 of eight 116 and 47.  Short rows: 8192 x 1024: 64 of two 12.1 and 9.1, 256 of one 13.6 and 11.4; 1 x 1024: 3.0, 2.5.
+// Wider ones, which go over their rows two and three times, from memory: 1 x 28672: 7.7 and 8.2; 512 x 28672: 29 and 21 for 103 and 73 MB;
+// 4096 x 28672: 182 and 152 for 822 and 587 MB, 4.5 and 3.9 TB/s; 512 x 131072: 132 and 110.
 template <bool F16, int OP>
 hipError_t pick(const Rows8Args &a, hipStream_t s)
 {

@@ -15,7 +15,9 @@ stream, the kernels of libmf.so do the work.  Calls enqueue on `stream` (None:
 torch's current one), copies of what is not contiguous too, and do not
 synchronise; include/mf.h has the definitions.  They are for inference: an
 operand that requires a gradient is refused while gradients are recorded, and so is
-one with a tangent of forward mode.
+one with a tangent of forward mode.  So are outputs that lie over operands other than
+their own rows (a norm's h over x or the residual, turned queries and attention's
+results over the queries).
 """
 from __future__ import annotations
 
