@@ -258,9 +258,10 @@ hipError_t go(const Rows8Args &a, hipStream_t s)
 }
 
 // As many threads to a row as leave each one or two pieces of eight, whether rows are few or many (us, norm with a residual and
-// gate, the same rows again, of which the caches have a part; T threads of V pieces): 1 x 4096: 512 of one 2.9 and 2.5, 256 of two 3.4 and 2.9; 8192 x 4096: 36.5 and 26.2, 38.3 and 26.5;
-// 8192 x 8192: 512 of two 85 and 61, 256 of four 94 and 62, 1024 of one 86 and 63; 4500 x 10240: 1024 of two 82 and 37,
-// 256 of eight 116 and 47.  Short rows: 8192 x 1024: 64 of two 12.1 and 9.1, 256 of one 13.6 and 11.4; 1 x 1024: 3.0, 2.5.
+// gate, the same rows again, of which the caches have a part; T threads of V pieces): 1 x 4096: 512 of one 2.9 and 2.5, 256 of two
+// 3.4 and 2.9; 8192 x 4096: 36.5 and 26.2, 38.3 and 26.5; 8192 x 8192: 512 of two 85 and 61, 256 of four 94 and 62, 1024 of one 86
+// and 63; 4500 x 10240: 1024 of two 82 and 37, 256 of eight 116 and 47.  Short rows: 8192 x 1024: 64 of two 12.1 and 9.1, 256 of one
+// 13.6 and 11.4; 1 x 1024: 3.0, 2.5.
 // Wider ones, which go over their rows two and three times, from memory: 1 x 28672: 7.7 and 8.2; 512 x 28672: 29 and 21 for 103 and 73 MB;
 // 4096 x 28672: 182 and 152 for 822 and 587 MB, 4.5 and 3.9 TB/s; 512 x 131072: 132 and 110.
 template <bool F16, int OP>
