@@ -423,7 +423,7 @@ mf_status mf_w4_pack_bytes(const mf_w4_desc *desc, size_t *bytes);
 /* Lays weights out for mf_w4_matmul, once, when they are loaded.  d_codes:
  * uint8 [N][K / 2], the even k in the low four bits; d_scales [N][K / G];
  * d_zeros uint8 [N][K / G], low four bits read, or NULL: 8 everywhere.
- * d_packed: mf_w4_pack_bytes, 256-byte aligned. */
+ * d_packed: mf_w4_pack_bytes, 256-byte aligned, not over the others (EINVAL). */
 mf_status mf_w4_pack(const mf_w4_desc *desc, const uint8_t *d_codes, const void *d_scales, const uint8_t *d_zeros,
                      void *d_packed, size_t packed_bytes, void *stream);
 
@@ -432,7 +432,7 @@ typedef struct {
     const void *d_packed;   /* as mf_w4_pack wrote it */
     const void *d_x;        /* [rows][K], row stride x_stride >= K */
     const void *d_bias;     /* [N] or NULL */
-    void *d_y;              /* [rows][N], row stride y_stride >= N; not over d_x */
+    void *d_y;              /* [rows][N], row stride y_stride >= N; not over anything that is read (EINVAL) */
     int64_t rows;           /* 0 (nothing is done) .. 2^20 */
     int64_t x_stride, y_stride;
 } mf_w4_args;
@@ -442,7 +442,7 @@ mf_status mf_w4_workspace_size(const mf_w4_args *args, size_t *bytes);
 
 /* Any number of rows; made for the few (up to 64) of a decode step, which read
  * the weights once.  Deterministic.  d_ws: mf_w4_workspace_size bytes, 256-byte
- * aligned; need not be initialised. */
+ * aligned, not over the operands (EINVAL); need not be initialised. */
 mf_status mf_w4_matmul(const mf_w4_args *args, void *d_ws, size_t ws_bytes, void *stream);
 
 /* --- the paged cache in 4 bits

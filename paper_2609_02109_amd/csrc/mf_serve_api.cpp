@@ -68,6 +68,8 @@ mf_status mf_w4_pack(const mf_w4_desc *desc, const uint8_t *d_codes, const void 
     if (st != MF_OK) return st;
     if (!d_codes || !d_scales || !d_packed || !aligned(d_scales, 2) || !aligned(d_packed, 256)) return MF_EINVAL;
     if (packed_bytes < w4_bytes(*desc)) return MF_ENOMEM;
+    const int64_t groups = desc->n_out * (desc->n_in / desc->group);
+    if (!apart(place(d_packed, (int64_t)w4_bytes(*desc)), {place(d_codes, desc->n_out * (desc->n_in / 2)), place(d_scales, groups * 2), place(d_zeros, groups)})) return MF_EINVAL;
     W4PackArgs a;
     a.codes = d_codes;
     a.zeros = d_zeros;
@@ -114,6 +116,9 @@ mf_status mf_w4_matmul(const mf_w4_args *args, void *d_ws, size_t ws_bytes, void
     const W4Plan p = w4_plan(a.rows, a.n_out, a.n_in);
     if (p.ws_bytes > 0 && (ws_bytes < p.ws_bytes || !d_ws)) return MF_ENOMEM;
     if (p.ws_bytes > 0 && !aligned(d_ws, 256)) return MF_EINVAL;
+    const Place x = place(args->d_x, w.n_in * 2, args->rows, args->x_stride * 2), y = place(args->d_y, w.n_out * 2, args->rows, args->y_stride * 2);
+    const Place bias = place(args->d_bias, w.n_out * 2), packed = place(args->d_packed, (int64_t)w4_bytes(w));
+    if (!apart(y, {x, bias, packed}) || (p.ws_bytes > 0 && !apart(place(d_ws, (int64_t)p.ws_bytes), {x, bias, packed, y}))) return MF_EINVAL;
     return of(launch_w4(a, p, w.group, as_int(w.dtype) == MF_F16, (float *)d_ws, (hipStream_t)stream));
 }
 

@@ -156,3 +156,29 @@ def test_read_over_what_it_reads(kind):
         most = 3 * 2 * 64 * el
         for k, v in ((PAGES, X), (X, PAGES + size - 4), (X, PAGES - most + 4), (STARTS, X), (X, LENS), (TABLE + 12, None), (X, X), (X, X + most - 4), (X + most - 4, X)):
             assert call(C.byref(c), C.byref(b), ty, k, v, None) == mf.MF_EINVAL
+
+
+# ------------------------------------------------------------- 4-bit products
+
+def _w4(y=Y, bias=None, x=X, rows=3, n=64, k=256, packed=Z, ys=64, xs=None):
+    return serve.W4Args(serve.W4Desc(n, k, 64, BF), packed, x, bias, y, rows, k if xs is None else xs, ys)
+
+
+def test_4_bit_products_over_what_they_are_made_of():
+    # packed: 4 tiles of 2 records of 1024 bytes of codes and 128 of scales
+    size = 4 * 2 * (1024 + 128)
+    for a in (_w4(y=X), _w4(y=X + 1534), _w4(y=X - 382), _w4(bias=Y), _w4(bias=Y + 382), _w4(bias=Y - 126), _w4(y=Z), _w4(y=Z + size - 2), _w4(y=Z - 382),
+              _w4(y=X + 128, ys=256), _w4(y=X + 512, ys=512)):
+        assert mf.lib.mf_w4_matmul(C.byref(a), 7 << 20, 1 << 20, None) == mf.MF_EINVAL
+    nb = C.c_size_t(0)
+    many = dict(n=4096, k=8192, rows=40, x=1 << 30, y=2 << 30, packed=3 << 30, ys=4096)
+    a = _w4(**many)
+    assert mf.lib.mf_w4_workspace_size(C.byref(a), C.byref(nb)) == mf.MF_OK and nb.value > 0
+    for at in (1 << 30, (2 << 30) + 256, 3 << 30, (2 << 30) - nb.value // 512 * 256):
+        assert mf.lib.mf_w4_matmul(C.byref(a), at, nb.value, None) == mf.MF_EINVAL
+
+
+def test_4_bit_weights_laid_out_over_themselves():
+    d = serve.W4Desc(16, 128, 64, BF)   # 1024 bytes of codes, 64 of scales, 32 of zero points; 1152 laid out
+    for codes, scales, zeros, packed in ((X, Y, None, X), (X + 1150, Y, None, X), (X, Y, None, Y), (X, Y + 1150, Z, Y), (X, Y, Z, Z), (X, Y, Z - 30, Z)):
+        assert mf.lib.mf_w4_pack(C.byref(d), codes, scales, zeros, packed, C.c_size_t(1152), None) == mf.MF_EINVAL
